@@ -230,6 +230,28 @@ kvq_status kvq_merge_adapter(const void* W, int d_in, int d_q, int d_kv, const v
 kvq_status kvq_append(kvq_cache* cache, const void* K, const void* V, int n_new,
                       const kvq_format* fmt, void* stream);
 
+/* Copy sequences between caches: sequence b of dst becomes the first n tokens
+ * of sequence rows[b] of src, for every b (forking a prompt's cache into
+ * samples, reordering beams, moving the survivors of a batch together).
+ *   rows  HOST array of dst's B entries, read during the call: a sequence of
+ *         src, or -1 to leave the bytes of sequence b as they are.
+ *   dst   src itself (any map: copies, permutations and mixtures of both; no
+ *         staging memory is needed, and sequences with rows[b] == b are not
+ *         touched), or a cache of the same format, H_kv and D in storage that
+ *         does not overlap src's.  B and T_max may differ.
+ *   n     0 <= n <= src's length; formats with an fp16 window need n equal to
+ *         src's length (KVQ_ERR_FORMAT otherwise), as for kvq_cache_rewind.
+ * Afterwards dst's length is n.  What is copied, byte for byte: the whole
+ * 32-token blocks that hold coded tokens of the first n, their scales and
+ * offsets, and the fp16 rows of the window and sink tokens; every other byte
+ * of dst stays as it was.  A copied sequence behaves like its source: further
+ * appends give the bytes that they would have given there.  Sequences left
+ * with -1 count as n tokens long like the others; what they hold is up to the
+ * caller.
+ * KVQ_ERR_CAPACITY when n exceeds dst's T_max; KVQ_ERR_ARG for an entry
+ * outside [-1, B of src), overlapping storage or different H_kv or D. */
+kvq_status kvq_cache_gather(kvq_cache* dst, const kvq_cache* src, const int32_t* rows, int n, void* stream);
+
 /* Workspace bytes kvq_decode_attn needs for H_q query heads at any length
  * up to the cache's T_max (split-K partial results; contents need no
  * initialization).  Calls that share a workspace must not overlap. */

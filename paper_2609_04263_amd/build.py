@@ -35,7 +35,8 @@ _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 # from one source, once per (head size, metadata width, key axis) family, the
 # prefill kernels once per head size.
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
-         ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", [])]
+         ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
+         ("gather.hip", "gather", [])]
 UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64, 128, 256)]
 UNITS += [("attn_part.hip", f"attn_{d}_{m}_{pc}",
            _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_M16={m}", f"-DKVQ_PART_PC={pc}"])

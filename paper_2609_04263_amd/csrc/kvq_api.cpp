@@ -6,7 +6,9 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <memory>
 #include <mutex>
+#include <new>
 
 #include "kvq_internal.h"
 
@@ -616,6 +618,178 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, con
     return KVQ_OK;
 }
 
+}  // extern "C"
+
+namespace {
+
+// The operations of kvq_cache_gather, in batches of kGatherBatch (`ops`, up to
+// `cap` entries, gaps with dst = -1).  In place, an operation comes after all
+// that read what it overwrites, or in the same batch: first the sequences that
+// nobody (still) reads, then the cycles that are left.  A cycle of more than a
+// batch is taken as shorter ones: after a_1 <- a_2 <- .. <- a_k <- a_1, a_k
+// holds the old a_1, and a_k <- a_(k+1) <- .. <- a_L <- a_k finishes the cycle.
+// Returns the entries used; *ordered tells whether batches depend on each other.
+// work: dst.B + src.B ints.
+int gather_ops(const int32_t* rows, int Bd, int Bs, bool in_place, kvq::GatherOp* ops, int* work, bool* ordered)
+{
+    constexpr int NB = kvq::kGatherBatch;
+    int n = 0;
+    *ordered = false;
+    if (!in_place) {
+        // by source (a counting sort), so that operations of one source share its load
+        int* start = work + Bd;
+        memset(start, 0, sizeof(int) * (size_t)Bs);
+        for (int b = 0; b < Bd; ++b)
+            if (rows[b] >= 0) {
+                ++start[rows[b]];
+                ++n;
+            }
+        for (int s = 0, at = 0; s < Bs; ++s) {
+            const int count = start[s];
+            start[s] = at;
+            at += count;
+        }
+        for (int b = 0; b < Bd; ++b)
+            if (rows[b] >= 0)
+                ops[start[rows[b]]++] = {rows[b], b};
+    } else {
+        int *queue = work, *reads = work + Bd, head = 0, tail = 0;
+        memset(reads, 0, sizeof(int) * (size_t)Bs);
+        const auto moves = [&](int b) { return rows[b] >= 0 && rows[b] != b; };
+        for (int b = 0; b < Bd; ++b)
+            if (moves(b))
+                ++reads[rows[b]];
+        for (int b = 0; b < Bd; ++b) {
+            if (moves(b) && reads[b] > 0)
+                *ordered = true;
+            if (moves(b) && reads[b] == 0)
+                queue[tail++] = b;
+        }
+        if (!*ordered) {
+            // no sequence is both read and written: by source, as above
+            int* start = reads;
+            for (int s = 0, at = 0; s < Bs; ++s) {
+                const int count = start[s];
+                start[s] = at;
+                at += count;
+            }
+            for (int b = 0; b < Bd; ++b)
+                if (moves(b))
+                    ops[start[rows[b]]++] = {rows[b], b};
+            n = tail;
+        } else {
+            while (head < tail) {
+                const int b = queue[head++], s = rows[b];
+                ops[n++] = {s, b};
+                reads[b] = -1;  // done
+                if (--reads[s] == 0 && moves(s))
+                    queue[tail++] = s;
+            }
+            for (int b = 0; b < Bd; ++b) {
+                if (!moves(b) || reads[b] < 0)
+                    continue;
+                // the cycle of b: every member is read once, by its predecessor
+                int len = 0;
+                for (int x = b; reads[x] >= 0; x = rows[x]) {
+                    queue[len++] = x;  // queue[i] <- queue[i + 1], the last <- the first
+                    reads[x] = -1;
+                }
+                for (int i = 0; i + 1 < len;) {
+                    const int k = len - i < NB ? len - i : NB;  // members i .. i + k - 1
+                    if (n % NB + k > NB)
+                        while (n % NB)
+                            ops[n++] = {0, -1};
+                    for (int j = 0; j < k; ++j)
+                        ops[n++] = {queue[i + (j + 1) % k], queue[i + j]};
+                    i += k - 1;
+                }
+            }
+        }
+    }
+    while (n % NB)
+        ops[n++] = {0, -1};
+    return n;
+}
+
+// Entries gather_ops needs for Bd destinations: a cycle of L sequences takes
+// at most L + (L - 1) / (batch - 1) operations, in parts of k operations that
+// each leave a gap of less than k before them.
+size_t gather_ops_bound(int Bd)
+{
+    return 3 * (size_t)Bd + 2 * kvq::kGatherBatch;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvq_status kvq_cache_gather(kvq_cache* dst, const kvq_cache* src, const int32_t* rows, int n, void* stream)
+{
+    if (!dst || !src || !rows || n < 0 || n > src->n || dst->H != src->H || dst->D != src->D)
+        return KVQ_ERR_ARG;
+    const bool in_place = dst == src;
+    if (!in_place && dst->base < src->base + src->off[9] + src->len[9] &&
+        src->base < dst->base + dst->off[9] + dst->len[9])
+        return KVQ_ERR_ARG;
+    for (int b = 0; b < dst->B; ++b)
+        if (rows[b] < -1 || rows[b] >= src->B)
+            return KVQ_ERR_ARG;
+    if (!same_format(dst->fmt, src->fmt) || (src->fmt.flush != 0 && n != src->n))
+        return KVQ_ERR_FORMAT;
+    if (n > dst->T_max)
+        return KVQ_ERR_CAPACITY;
+    const kvq_format& f = src->fmt;
+    const int nq = kvq::num_coded(f, n), tail = kvq::num_tail(f, n), n_sink = n - tail;
+    const size_t blocks = (size_t)(nq + 31) / 32, row = (size_t)src->D * 2;
+    kvq::GatherParams p = {};
+    p.src = src->base;
+    p.dst = dst->base;
+    p.H = src->H;
+    // `bytes` of every slab of a section, from `at` on
+    const auto span = [&](int section, size_t at, size_t bytes) {
+        if (bytes == 0)
+            return;
+        kvq::GatherSpan& s = p.span[p.spans++];
+        s.src_stride = src->len[section] / ((size_t)src->B * src->H);
+        s.dst_stride = dst->len[section] / ((size_t)dst->B * dst->H);
+        s.src_off = src->off[section] + at;
+        s.dst_off = dst->off[section] + at;
+        s.len16 = bytes / 16;
+    };
+    if (src->T_alloc > 0)
+        for (int s = 0; s < 6; ++s)  // whole 32-token blocks
+            span(s, 0, blocks * (src->len[s] / ((size_t)src->B * src->H * (src->T_alloc / 32))));
+    if (f.flush > 0 && tail > nq) {
+        // window tokens nq .. tail - 1, in slots t mod ring: one part, or two
+        const int ring = f.residual + f.flush, s0 = nq % ring, len = tail - nq;
+        const int first = len < ring - s0 ? len : ring - s0;
+        for (int s = 6; s < 8; ++s) {
+            span(s, s0 * row, first * row);
+            span(s, 0, (len - first) * row);
+        }
+    }
+    for (int s = 8; s < 10; ++s)
+        span(s, 0, n_sink * row);
+    if (p.spans > 0) {
+        std::unique_ptr<kvq::GatherOp[]> ops(new (std::nothrow) kvq::GatherOp[gather_ops_bound(dst->B)]);
+        std::unique_ptr<int[]> work(new (std::nothrow) int[(size_t)dst->B + src->B]);
+        if (!ops || !work)
+            return KVQ_ERR_ARG;
+        bool ordered;
+        const int count = gather_ops(rows, dst->B, src->B, in_place, ops.get(), work.get(), &ordered);
+        constexpr int per = kvq::kGatherBatches * kvq::kGatherBatch;
+        for (int i = 0; i < count; i += per) {
+            const int m = count - i < per ? count - i : per;
+            p.batches = m / kvq::kGatherBatch;
+            memcpy(p.op, ops.get() + i, sizeof(kvq::GatherOp) * (size_t)m);
+            if (kvq::launch_gather(p, ordered, (hipStream_t)stream) != hipSuccess)
+                return KVQ_ERR_DEVICE;
+        }
+    }
+    dst->n = n;
+    return KVQ_OK;
+}
+
 kvq_status kvq_decode_workspace_bytes(const kvq_cache* c, int H_q, size_t* bytes)
 {
     if (!c || !bytes || H_q < c->H || H_q % c->H != 0 || H_q / c->H > 16)
@@ -837,6 +1011,19 @@ int kvq_internal_prefill_ranges(const kvq_cache* c, int C, int H_q)
 int kvq_internal_prefill_tile_rows(const kvq_cache* c, int C, int H_q)
 {
     return kvq::prefill_tile_rows(prefill_params(c, C, H_q, 1.0f), c->D);
+}
+
+int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src, int in_place, int32_t* pairs, int* ordered)
+{
+    std::unique_ptr<kvq::GatherOp[]> ops(new (std::nothrow) kvq::GatherOp[gather_ops_bound(B_dst)]);
+    std::unique_ptr<int[]> work(new (std::nothrow) int[(size_t)B_dst + B_src]);
+    if (!ops || !work)
+        return -1;
+    bool dep;
+    const int n = gather_ops(rows, B_dst, B_src, in_place != 0, ops.get(), work.get(), &dep);
+    memcpy(pairs, ops.get(), sizeof(kvq::GatherOp) * (size_t)n);
+    *ordered = dep;
+    return n;
 }
 
 int kvq_internal_project_tile(int M, int N)

@@ -74,6 +74,33 @@ hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 // p.ring, from input token t - p.n0 (the sink tokens: ring = sink).
 hipError_t launch_append_rows(const AppendParams& p, int D, int hi, hipStream_t stream);
 
+// ---------------------------------------------------------------- gather
+constexpr int kGatherBatch = 8;     // operations a thread loads before it stores
+constexpr int kGatherBatches = 32;  // batches of one launch (2 KiB of kernel arguments)
+constexpr int kGatherSpans = 12;    // six coded sections, the window's two in two parts each, the sink's two
+
+// Live bytes of one section: 16 len16 bytes from the start (or an offset) of
+// every (sequence, head) slab.
+struct GatherSpan {
+    size_t src_off, dst_off;        // of sequence 0, head 0
+    size_t src_stride, dst_stride;  // bytes of a (sequence, head) slab
+    size_t len16;
+    int wg0;                        // first workgroup, and workgroups per head (set at launch)
+    uint32_t wgs;
+};
+struct GatherOp {
+    int src, dst;                   // sequences; dst < 0: nothing
+};
+struct GatherParams {
+    const uint8_t* src;
+    uint8_t* dst;
+    int H, spans, batches;
+    GatherSpan span[kGatherSpans];
+    GatherOp op[kGatherBatches * kGatherBatch];
+};
+// Batches run in order in each thread (ordered), or in any order.
+hipError_t launch_gather(GatherParams p, bool ordered, hipStream_t stream);
+
 // ------------------------------------------------------------- projection
 struct ProjParams {
     const uint16_t* x;    // bf16 [M][K]  (hidden states)
@@ -209,5 +236,9 @@ hipError_t launch_prefill(const AttnParams& p, int D, size_t ws_bytes, hipStream
 // The dispatch rules, for tests that have to know which kernels a call takes.
 // Host only; not part of the C ABI.
 extern "C" int kvq_internal_project_tile(int M, int N);
+// The (source, destination) pairs of a gather in batches of kGatherBatch (gaps:
+// destination -1), at most 3 B_dst + 2 kGatherBatch of them; returns their number.
+extern "C" int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src, int in_place, int32_t* pairs,
+                                       int* ordered);
 extern "C" int kvq_internal_prefill_ranges(const kvq_cache* cache, int C, int H_q);
 extern "C" int kvq_internal_prefill_tile_rows(const kvq_cache* cache, int C, int H_q);

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -62,6 +63,7 @@ def _load() -> C.CDLL:
     L.kvq_merge_adapter.argtypes = [P, I, I, I, P, P, I, C.c_float, P, P]
     L.kvq_project_append.argtypes = [P, I, I, P, I, I, P, P, I, C.c_float, P, P, I, P, S, P]
     L.kvq_append.argtypes = [P, P, P, I, Fp, P]
+    L.kvq_cache_gather.argtypes = [P, P, C.POINTER(C.c_int32), I, P]
     L.kvq_decode_workspace_bytes.argtypes = [P, I, C.POINTER(S)]
     L.kvq_decode_attn.argtypes = [P, P, I, C.c_float, P, P, S, P]
     L.kvq_decode_attn_noalloc.argtypes = [P, P, I, C.c_float, P, P]
@@ -71,7 +73,7 @@ def _load() -> C.CDLL:
     for name in ("kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section", "kvq_cache_reset",
                  "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_project_workspace_bytes",
                  "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
-                 "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
+                 "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
                  "kvq_prefill_workspace_bytes",
                  "kvq_time_launches"):
         getattr(L, name).restype = I
@@ -82,7 +84,7 @@ _lib = _load()
 EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section",
             "kvq_cache_reset", "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_cache_destroy",
             "kvq_project_workspace_bytes", "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
-            "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
+            "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
             "kvq_prefill_workspace_bytes", "kvq_time_launches")
 
 
@@ -117,6 +119,15 @@ def _stream(stream) -> int:
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _ints(values, count: int, what: str):
+    """A host int32 array of `count` entries (anything numpy takes, but no device tensor)."""
+    a = np.ascontiguousarray(values)
+    if a.shape != (count,) or not np.issubdtype(a.dtype, np.integer):
+        raise ValueError(f"{what}: {count} integers expected, got {a.dtype} of shape {a.shape}")
+    a = a.astype(np.int64).clip(-(1 << 31), (1 << 31) - 1).astype(np.int32)
+    return a, a.ctypes.data_as(C.POINTER(C.c_int32))
 
 
 # ------------------------------------------------------------------ cache
@@ -182,6 +193,15 @@ class Cache:
         st = _lib.kvq_append(self.handle, K.data_ptr(), V.data_ptr(), n_new, f, _stream(stream))
         if st:
             _check(st, "append")
+
+    def gather(self, src: "Cache", rows, n: int | None = None, stream=None) -> None:
+        """Sequence b becomes the first n tokens (all by default) of src's
+        sequence rows[b]; -1 leaves b's bytes.  src may be this cache.  rows
+        is host data: a list, an array or a CPU tensor of B integers."""
+        keep, ptr = _ints(rows, self.B, "gather")
+        st = _lib.kvq_cache_gather(self.handle, src.handle, ptr, src.n if n is None else n, _stream(stream))
+        if st:
+            _check(st, "gather")
 
     def decode_workspace_bytes(self, H_q: int) -> int:
         out = C.c_size_t()
