@@ -327,6 +327,47 @@ kvq_status kvq_prefill_attn(const kvq_cache* cache, const void* Q, int C, int H_
  * (all units in one pass). */
 kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
 
+/* ---- Attention of a batch whose sequences share prefixes (samples or beams
+ * of one prompt, users behind one system prompt).  Two caches of one layer, of
+ * the same format, H_kv and D:
+ *   prefix  P sequences (P <= 256): the shared tokens;
+ *   suffix  B sequences: each sequence's own tokens, which come after those of
+ *           its prefix.
+ *   first   HOST array of P + 1 entries, read during the call: sequences
+ *           first[g] .. first[g + 1] - 1 of the suffix cache share prefix g
+ *           (first[0] = 0, first[P] = B, no entry below the one before it; a
+ *           prefix may have no sequences).  NULL: equal groups, B a multiple
+ *           of P.
+ * A prefix and its suffix are attended as if they were one cache (sinks,
+ * window and coded groups are those of the two caches as they are: a suffix
+ * has sink tokens and a window of its own).  The codes of a prefix are read
+ * once per 32 query rows of its group instead of once per sequence.  H_q as
+ * for kvq_decode_attn (H_q / H_kv <= 16); products and their limits as there,
+ * and the reconstructed keys of per-channel formats below 65504 in magnitude.
+ * The sums run in an order that depends on the shapes and lengths alone, so a
+ * call gives the same bits every time. */
+
+/* Workspace bytes for calls of up to C queries per sequence at any lengths and
+ * groups of these caches (contents need no initialization; calls that share a
+ * workspace must not overlap). */
+kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* suffix, int C, int H_q, size_t* bytes);
+
+/* Decode attention for one new query per sequence over its prefix and suffix.
+ *   Q  bf16 [B][H_q][D],  O  fp32 [B][H_q][D], as for kvq_decode_attn.
+ * Either cache may be empty, not both (KVQ_ERR_ARG). */
+kvq_status kvq_decode_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                  int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, void* stream);
+
+/* Chunked attention: the newest C tokens of every suffix (appended before the
+ * call, 1 <= C <= the suffix's length) attend to the whole prefix and, causally,
+ * to their own suffix: query i to suffix tokens 0 .. n - C + i.  For prompts
+ * behind a shared prefix and for several drafted tokens at once.
+ *   Q  bf16 [B][C][H_q][D],  O  fp32 [B][C][H_q][D].
+ * The prefix may be empty. */
+kvq_status kvq_prefill_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
+                                   const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
+                                   size_t ws_bytes, void* stream);
+
 /* Measurement hook for benchmarks (not part of the method).  While set
  * (both events non-null), every kernel the library launches from this host
  * thread records stop_event when it completes, and the first of them after

@@ -33,14 +33,17 @@ ROOT = os.path.dirname(HERE)
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 # (source, object name, extra flags).  The decode split kernels are built
 # from one source, once per (head size, metadata width, key axis) family, the
-# prefill kernels once per head size.
+# prefill kernels once per head size, the shared-prefix kernels once per head
+# size for plain and for rotated queries.
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
          ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
-         ("gather.hip", "gather", [])]
+         ("gather.hip", "gather", []), ("shared.hip", "shared", [])]
 UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64, 128, 256)]
 UNITS += [("attn_part.hip", f"attn_{d}_{m}_{pc}",
            _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_M16={m}", f"-DKVQ_PART_PC={pc}"])
           for d in (64, 128, 256) for m in (0, 1) for pc in (0, 1)]
+UNITS += [("shared_part.hip", f"shared_{d}_{r}", _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_ROT={r}"])
+          for d in (64, 128, 256) for r in (0, 1)]
 SOURCES = sorted({u[0] for u in UNITS})
 
 

@@ -950,6 +950,134 @@ kvq_status kvq_decode_attn_noalloc(const kvq_cache* c, const void* Q, int H_q, f
     return kvq::launch_decode(p, c->D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
+// ------------------------------------------------- shared-prefix attention
+
+// Sections, dimensions and format of a segment's cache.
+static kvq::AttnParams shared_segment(const kvq_cache* c, int H_q, float sm_scale)
+{
+    const kvq_format& f = c->fmt;
+    kvq::AttnParams p = {};
+    p.nq = kvq::num_coded(f, c->n);
+    p.kc = at<uint32_t>(c, 0);
+    p.ks = at<float>(c, 1);
+    p.kz = at<float>(c, 2);
+    p.vc = at<uint32_t>(c, 3);
+    p.vs = at<float>(c, 4);
+    p.vz = at<float>(c, 5);
+    p.kr = at<uint16_t>(c, 6);
+    p.vr = at<uint16_t>(c, 7);
+    p.kq = at<uint16_t>(c, 8);
+    p.vq = at<uint16_t>(c, 9);
+    p.B = c->B;
+    p.H = c->H;
+    p.H_q = H_q;
+    p.G = H_q / c->H;
+    p.T = c->T_alloc;
+    p.n = c->n - f.sink;  // negative when the cache ends inside the sink
+    p.ring = f.residual + f.flush;
+    p.sink = f.sink;
+    p.n_sink = c->n < f.sink ? c->n : f.sink;
+    p.k_bits = f.k_bits;
+    p.v_bits = f.v_bits;
+    p.k_mode = f.k_mode;
+    p.v_mode = f.v_mode;
+    p.k_axis = f.k_axis;
+    p.k_group = f.k_group;
+    p.v_group = f.v_group;
+    p.rotate = f.rotate;
+    p.sm_log2 = sm_scale * 1.4426950408889634f;
+    p.rot_c = rotation_constant(c->D);
+    p.meta16 = f.meta_fp16;
+    return p;
+}
+
+// The two caches of a shared call serve one attention layer.
+static kvq_status shared_caches(const kvq_cache* prefix, const kvq_cache* suffix, int C, int H_q)
+{
+    if (!prefix || !suffix || prefix->H != suffix->H || prefix->D != suffix->D)
+        return KVQ_ERR_ARG;
+    if (H_q < suffix->H || H_q % suffix->H != 0 || H_q / suffix->H > 16 || C < 1)
+        return KVQ_ERR_ARG;
+    if (prefix->B > kvq::kSharedPrefixes || (long long)suffix->B * C > INT32_MAX / H_q)
+        return KVQ_ERR_ARG;
+    return same_format(prefix->fmt, suffix->fmt) ? KVQ_OK : KVQ_ERR_FORMAT;
+}
+
+static size_t shared_workspace_layout(const kvq_cache* suffix, int C, int H_q, size_t* off_ml)
+{
+    const size_t rows = (size_t)suffix->B * C * H_q;
+    const size_t S = kvq::shared_split_bound(suffix->B, suffix->H, suffix->D, C, H_q / suffix->H);
+    const size_t o_ml = round_up(rows * S * suffix->D * sizeof(float), 256);
+    if (off_ml)
+        *off_ml = o_ml;
+    return o_ml + rows * S * 2 * sizeof(float);
+}
+
+kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* suffix, int C, int H_q, size_t* bytes)
+{
+    const kvq_status st = shared_caches(prefix, suffix, C, H_q);
+    if (st != KVQ_OK)
+        return st;
+    if (!bytes)
+        return KVQ_ERR_ARG;
+    *bytes = shared_workspace_layout(suffix, C, H_q, nullptr);
+    return KVQ_OK;
+}
+
+// The queries of the newest C tokens of every sequence; `self` tells whether
+// those tokens have to be in the suffix.
+static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                              int C, int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, bool self,
+                              void* stream)
+{
+    const kvq_status st = shared_caches(prefix, suffix, C, H_q);
+    if (st != KVQ_OK)
+        return st;
+    if (!Q || !O || !workspace || !aligned16(Q) || !aligned16(O) || !aligned16(workspace) || !isfinite(sm_scale))
+        return KVQ_ERR_ARG;
+    const int P = prefix->B, B = suffix->B;
+    if (self ? suffix->n < C : prefix->n + suffix->n < 1)
+        return KVQ_ERR_ARG;
+    if (first ? first[0] != 0 || first[P] != B : B % P != 0)
+        return KVQ_ERR_ARG;
+    for (int g = 0; first && g < P; ++g)
+        if (first[g] > first[g + 1])
+            return KVQ_ERR_ARG;
+    size_t off_ml;
+    if (ws_bytes < shared_workspace_layout(suffix, C, H_q, &off_ml))
+        return KVQ_ERR_WORKSPACE;
+    kvq::SharedParams p = {};
+    p.seg[0] = shared_segment(prefix, H_q, sm_scale);
+    p.seg[1] = shared_segment(suffix, H_q, sm_scale);
+    p.q = (const uint16_t*)Q;
+    p.out = (float*)O;
+    p.part_o = (float*)workspace;
+    p.part_ml = (float*)((uint8_t*)workspace + off_ml);
+    p.rows = (size_t)B * C * H_q;
+    p.C = C;
+    p.H_q = H_q;
+    p.P = P;
+    p.rotate = suffix->fmt.rotate;
+    p.rot_c = rotation_constant(suffix->D);
+    for (int g = 0; g <= P; ++g)
+        p.first[g] = first ? first[g] : B / P * g;
+    const int items = kvq::shared_plan(&p, suffix->D, B);
+    return kvq::launch_shared(p, suffix->D, items, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+}
+
+kvq_status kvq_decode_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                  int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, void* stream)
+{
+    return shared_attn(prefix, suffix, first, Q, 1, H_q, sm_scale, O, workspace, ws_bytes, false, stream);
+}
+
+kvq_status kvq_prefill_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
+                                   const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
+                                   size_t ws_bytes, void* stream)
+{
+    return shared_attn(prefix, suffix, first, Q, C, H_q, sm_scale, O, workspace, ws_bytes, true, stream);
+}
+
 // Block images per (b, h) unit that a chunked prefill reconstructs: the sink
 // blocks holding tokens, then the tail's 32-token blocks.
 static void prefill_blocks(const kvq_cache* c, int* nsb, int* nvb)

@@ -231,6 +231,31 @@ int prefill_tile_rows(const AttnParams& p, int D);
 // Chunked prefill over units in groups that fit ws_bytes (at least one unit).
 hipError_t launch_prefill(const AttnParams& p, int D, size_t ws_bytes, hipStream_t stream);
 
+// ------------------------------------------------- shared-prefix attention
+constexpr int kSharedPrefixes = 256;  // groups of a call (their tables are kernel arguments)
+
+struct SharedParams {
+    AttnParams seg[2];   // the prefix and the suffix cache: sections and format; n = tokens - sink (may be negative)
+    const uint16_t* q;   // bf16 [B][C][H_q][D]
+    float* out;          // fp32 [B][C][H_q][D]
+    float* part_o;       // fp32 [S0 + S1][rows][D]  unnormalized partial outputs
+    float* part_ml;      // fp32 [S0 + S1][rows][2]  (running max in log2 units, sum)
+    size_t rows;         // B C H_q
+    int C, H_q, P;
+    int tile_rows;       // query rows of a work item, at most
+    int S[2], bps[2];    // ranges of a tile, 32-token blocks per range
+    int tiles0, items0;  // prefix tiles, prefix items (tiles0 S[0])
+    int rotate;
+    float rot_c;
+    int first[kSharedPrefixes + 1];  // first sequence of each group
+    int tile0[kSharedPrefixes + 1];  // first tile of each group
+};
+// Fills tile_rows, S, bps, tiles0, items0 and tile0 from the rest; returns the work items.
+int shared_plan(SharedParams* p, int D, int B);
+// Upper bound of S0 + S1 for any lengths and groups.
+int shared_split_bound(int B, int H, int D, int C, int G);
+hipError_t launch_shared(const SharedParams& p, int D, int items, hipStream_t stream);
+
 }  // namespace kvq
 
 // The dispatch rules, for tests that have to know which kernels a call takes.

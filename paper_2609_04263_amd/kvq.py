@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 import numpy as np
 import torch
@@ -69,13 +70,17 @@ def _load() -> C.CDLL:
     L.kvq_decode_attn_noalloc.argtypes = [P, P, I, C.c_float, P, P]
     L.kvq_prefill_attn.argtypes = [P, P, I, I, C.c_float, P, P, S, P]
     L.kvq_prefill_workspace_bytes.argtypes = [P, C.POINTER(S)]
+    Ip = C.POINTER(C.c_int32)
+    L.kvq_shared_workspace_bytes.argtypes = [P, P, I, I, C.POINTER(S)]
+    L.kvq_decode_attn_shared.argtypes = [P, P, Ip, P, I, C.c_float, P, P, S, P]
+    L.kvq_prefill_attn_shared.argtypes = [P, P, Ip, P, I, I, C.c_float, P, P, S, P]
     L.kvq_time_launches.argtypes = [P, P]
     for name in ("kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section", "kvq_cache_reset",
                  "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_project_workspace_bytes",
                  "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
                  "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
-                 "kvq_prefill_workspace_bytes",
-                 "kvq_time_launches"):
+                 "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
+                 "kvq_prefill_attn_shared", "kvq_time_launches"):
         getattr(L, name).restype = I
     return L
 
@@ -85,7 +90,8 @@ EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_sect
             "kvq_cache_reset", "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_cache_destroy",
             "kvq_project_workspace_bytes", "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
             "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
-            "kvq_prefill_workspace_bytes", "kvq_time_launches")
+            "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
+            "kvq_prefill_attn_shared", "kvq_time_launches")
 
 
 def lib() -> C.CDLL:
@@ -122,12 +128,21 @@ def _stream(stream) -> int:
 
 
 def _ints(values, count: int, what: str):
-    """A host int32 array of `count` entries (anything numpy takes, but no device tensor)."""
-    a = np.ascontiguousarray(values)
-    if a.shape != (count,) or not np.issubdtype(a.dtype, np.integer):
-        raise ValueError(f"{what}: {count} integers expected, got {a.dtype} of shape {a.shape}")
-    a = a.astype(np.int64).clip(-(1 << 31), (1 << 31) - 1).astype(np.int32)
-    return a, a.ctypes.data_as(C.POINTER(C.c_int32))
+    """Host int32 array of `count` entries from a list, an array or a CPU tensor: (its owner, pointer)."""
+    try:
+        if not isinstance(values, (list, tuple)):
+            values = np.ascontiguousarray(values)
+            if not np.issubdtype(values.dtype, np.integer) or values.ndim != 1:
+                raise TypeError
+            values = values.tolist()
+        a = array("i", values)
+    except TypeError:
+        raise ValueError(f"{what}: {count} integers expected") from None
+    except OverflowError:
+        raise KvqError(ERR_ARG, what) from None
+    if len(a) != count:
+        raise ValueError(f"{what}: {count} integers expected, got {len(a)}")
+    return a, C.cast(a.buffer_info()[0], C.POINTER(C.c_int32))
 
 
 # ------------------------------------------------------------------ cache
@@ -244,6 +259,44 @@ class Cache:
                                    workspace.data_ptr(), nbytes, _stream(stream))
         if st:
             _check(st, "prefill_attn")
+
+
+    # This cache as the suffix of a shared one: `prefix` holds P sequences, and
+    # sequences first[g] .. first[g + 1] - 1 of this cache come after prefix g
+    # (first: P + 1 host integers, or None for equal groups).
+
+    def shared_workspace_bytes(self, prefix: "Cache", H_q: int, C_len: int = 1) -> int:
+        out = C.c_size_t()
+        _check(_lib.kvq_shared_workspace_bytes(prefix.handle, self.handle, C_len, H_q, C.byref(out)),
+               "shared_workspace_bytes")
+        return out.value
+
+    def shared_workspace(self, prefix: "Cache", H_q: int, C_len: int = 1, device="cuda"):
+        """A workspace for calls of up to C_len queries per sequence (reuse it across calls)."""
+        return torch.empty(self.shared_workspace_bytes(prefix, H_q, C_len), dtype=torch.uint8, device=device)
+
+    def decode_attn_shared(self, prefix: "Cache", Q, H_q: int, sm_scale: float, O, workspace, first=None,
+                           stream=None) -> None:
+        """O[B, H_q, D] (fp32) <- attention of bf16 Q[B, H_q, D] over each
+        sequence's prefix and its own tokens here."""
+        keep, ptr = (None, None) if first is None else _ints(first, prefix.B + 1, "first")
+        nbytes = workspace.numel() * workspace.element_size()
+        st = _lib.kvq_decode_attn_shared(prefix.handle, self.handle, ptr, Q.data_ptr(), H_q, sm_scale, O.data_ptr(),
+                                         workspace.data_ptr(), nbytes, _stream(stream))
+        if st:
+            _check(st, "decode_attn_shared")
+
+    def prefill_attn_shared(self, prefix: "Cache", Q, C_len: int, H_q: int, sm_scale: float, O, workspace, first=None,
+                            stream=None) -> None:
+        """O[B, C, H_q, D] (fp32) <- attention of the newest C_len tokens' bf16
+        queries Q[B, C, H_q, D] over each sequence's prefix and, causally, its
+        own tokens here."""
+        keep, ptr = (None, None) if first is None else _ints(first, prefix.B + 1, "first")
+        nbytes = workspace.numel() * workspace.element_size()
+        st = _lib.kvq_prefill_attn_shared(prefix.handle, self.handle, ptr, Q.data_ptr(), C_len, H_q, sm_scale,
+                                          O.data_ptr(), workspace.data_ptr(), nbytes, _stream(stream))
+        if st:
+            _check(st, "prefill_attn_shared")
 
 
 # ------------------------------------------------------------- projection
