@@ -33,8 +33,8 @@ ROOT = os.path.dirname(HERE)
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 # (source, object name, extra flags).  The decode split kernels are built
 # from one source, once per (head size, metadata width, key axis) family, the
-# prefill kernels once per head size, the shared-prefix kernels once per head
-# size for plain and for rotated queries.
+# prefill kernels once per head size, the shared-prefix kernels once per (head
+# size, key group / 32, 0 for per-channel keys).
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
          ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
          ("gather.hip", "gather", []), ("shared.hip", "shared", [])]
@@ -42,8 +42,8 @@ UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64
 UNITS += [("attn_part.hip", f"attn_{d}_{m}_{pc}",
            _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_M16={m}", f"-DKVQ_PART_PC={pc}"])
           for d in (64, 128, 256) for m in (0, 1) for pc in (0, 1)]
-UNITS += [("shared_part.hip", f"shared_{d}_{r}", _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_ROT={r}"])
-          for d in (64, 128, 256) for r in (0, 1)]
+UNITS += [("shared_part.hip", f"shared_{d}_{g}", _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_KG={g}"])
+          for d in (64, 128, 256) for g in (0, 1, 2, 4, 8) if 32 * g <= d]
 SOURCES = sorted({u[0] for u in UNITS})
 
 

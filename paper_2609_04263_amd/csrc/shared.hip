@@ -5,12 +5,11 @@
 
 namespace kvq {
 
-hipError_t launch_shared_64_0(const SharedParams& p, int items, hipStream_t stream);
-hipError_t launch_shared_64_1(const SharedParams& p, int items, hipStream_t stream);
-hipError_t launch_shared_128_0(const SharedParams& p, int items, hipStream_t stream);
-hipError_t launch_shared_128_1(const SharedParams& p, int items, hipStream_t stream);
-hipError_t launch_shared_256_0(const SharedParams& p, int items, hipStream_t stream);
-hipError_t launch_shared_256_1(const SharedParams& p, int items, hipStream_t stream);
+#define KVQ_FAMILY(D, KG) hipError_t launch_shared_##D##_##KG(const SharedParams& p, int items, hipStream_t stream);
+KVQ_FAMILY(64, 0) KVQ_FAMILY(64, 1) KVQ_FAMILY(64, 2)
+KVQ_FAMILY(128, 0) KVQ_FAMILY(128, 1) KVQ_FAMILY(128, 2) KVQ_FAMILY(128, 4)
+KVQ_FAMILY(256, 0) KVQ_FAMILY(256, 1) KVQ_FAMILY(256, 2) KVQ_FAMILY(256, 4) KVQ_FAMILY(256, 8)
+#undef KVQ_FAMILY
 
 namespace {
 
@@ -123,26 +122,37 @@ int shared_split_bound(int B, int H, int D, int C, int G)
 
 hipError_t launch_shared(const SharedParams& p, int D, int items, hipStream_t stream)
 {
-    const bool rot = p.rotate != 0;
+    const AttnParams& a = p.seg[0];
+    const int kg = a.k_axis == KVQ_PER_CHANNEL ? 0 : a.k_group / 32;
     hipError_t e = hipErrorInvalidValue;
-    switch (D) {
-    case 64:
-        e = rot ? launch_shared_64_1(p, items, stream) : launch_shared_64_0(p, items, stream);
-        if (e == hipSuccess)
-            launch_join<64>(p, stream);
+    switch (1000 * D + kg) {
+#define KVQ_FAMILY(D, KG)                           \
+    case 1000 * D + KG:                             \
+        e = launch_shared_##D##_##KG(p, items, stream); \
         break;
-    case 128:
-        e = rot ? launch_shared_128_1(p, items, stream) : launch_shared_128_0(p, items, stream);
-        if (e == hipSuccess)
-            launch_join<128>(p, stream);
-        break;
-    case 256:
-        e = rot ? launch_shared_256_1(p, items, stream) : launch_shared_256_0(p, items, stream);
-        if (e == hipSuccess)
-            launch_join<256>(p, stream);
-        break;
+        KVQ_FAMILY(64, 0)
+        KVQ_FAMILY(64, 1)
+        KVQ_FAMILY(64, 2)
+        KVQ_FAMILY(128, 0)
+        KVQ_FAMILY(128, 1)
+        KVQ_FAMILY(128, 2)
+        KVQ_FAMILY(128, 4)
+        KVQ_FAMILY(256, 0)
+        KVQ_FAMILY(256, 1)
+        KVQ_FAMILY(256, 2)
+        KVQ_FAMILY(256, 4)
+        KVQ_FAMILY(256, 8)
+#undef KVQ_FAMILY
     }
-    return e == hipSuccess ? hipGetLastError() : e;
+    if (e != hipSuccess)
+        return e;
+    if (D == 64)
+        launch_join<64>(p, stream);
+    else if (D == 128)
+        launch_join<128>(p, stream);
+    else
+        launch_join<256>(p, stream);
+    return hipGetLastError();
 }
 
 }  // namespace kvq

@@ -46,6 +46,8 @@
 // blocks that no row of a wave sees are skipped.
 #pragma once
 
+#include <type_traits>
+
 #include "kvq_device.h"
 #include "kvq_internal.h"
 
@@ -237,105 +239,92 @@ __device__ __forceinline__ half8 centred(const uint32_t* w, int k, uint32_t cent
 // The loads of one wave's part of a coded block: four key pieces and four
 // value pieces per lane, and chunk `lane` (four numbers) of the block's key and
 // of its value scales and offsets.
-template <bool W8>
+template <int KB, int VB, bool M16>
 struct Raw {
-    uint32_t k[W8 ? 8 : 4], v[W8 ? 8 : 4];
+    uint32_t k[KB], v[VB];  // 4 pieces of KB / 4 words
     u32x4 ks, kz, vs, vz;
 };
 
-// Streaming loads of 2 or 4 codes' pieces (bits of a code: 2, 4 or 8).
-template <int PIECES>
-__device__ __forceinline__ void load_pieces(const uint8_t* at, const int bits, uint32_t* w)
+// N bytes (4 to 32, naturally aligned) from global memory, streaming.
+template <int N>
+__device__ __forceinline__ void load_bytes(const uint8_t* at, uint32_t* w)
 {
-    if (bits == 8) {
+    if constexpr (N == 4) {
+        w[0] = __builtin_nontemporal_load((const uint32_t*)at);
+    } else if constexpr (N == 8) {
+        const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
+        w[0] = x.x;
+        w[1] = x.y;
+    } else {
 #pragma unroll
-        for (int i = 0; i < PIECES / 2; ++i) {
+        for (int i = 0; i < N / 16; ++i) {
             const u32x4 x = __builtin_nontemporal_load((const u32x4*)at + i);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 w[4 * i + e] = x[e];
         }
-    } else if (bits == 4) {
-        if constexpr (PIECES == 4) {
-            const u32x4 x = __builtin_nontemporal_load((const u32x4*)at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = x[e];
-        } else {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
-            w[0] = x.x;
-            w[1] = x.y;
-        }
-    } else {
-        if constexpr (PIECES == 4) {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
-            w[0] = x.x;
-            w[1] = x.y;
-        } else {
-            w[0] = __builtin_nontemporal_load((const uint32_t*)at);
-        }
     }
 }
 
-// The builder's view of a segment's unit.
-template <int D, bool KH, bool W8>
+// The builder's view of a segment's unit: a wave's part of its images.
+template <int D, bool KH, int KB, int VB, bool M16>
 struct Builder {
     static constexpr int NKB = D / 32, NMB = D / 16, PB = parts(D);
     const AttnParams& p;
     int unit, part, lane;
-    size_t ub0;        // first block of the unit
     int nkc, nvc;      // chunks of a block's key and value scales
     bool kaff, vaff;
+    const uint8_t *k, *v, *ks, *vs;  // this lane's pieces and chunks of block 0
+    long dkz, dvz;                   // offsets - scales (0 when symmetric: the scales once more)
+
+    // piece i of the lane: half block and 32-channel block
+    __device__ __forceinline__ int half(int i) const { return PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1; }
+    __device__ __forceinline__ int kblock(int i) const { return PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i; }
 
     __device__ __forceinline__ Builder(const AttnParams& p_, int unit_, int part_, int lane_)
         : p(p_), unit(unit_), part(part_), lane(lane_)
     {
-        ub0 = (size_t)unit * (p.T >> 5);
+        const size_t ub0 = (size_t)unit * (p.T >> 5);
+        constexpr int ESZ = M16 ? 2 : 4;
         nkc = KH ? D / 4 : 8 * (D / p.k_group);
         nvc = 8 * (D / p.v_group);
         kaff = p.k_mode == KVQ_AFFINE;
         vaff = p.v_mode == KVQ_AFFINE;
+        k = (const uint8_t*)p.kc + ((ub0 * 2 + half(0)) * 64 + lane) * (NKB * KB) + kblock(0) * KB;
+        v = (const uint8_t*)p.vc + (ub0 * 64 + lane) * (NMB * VB) + 4 * part * VB;
+        ks = (const uint8_t*)p.ks + (ub0 * nkc + min(lane, nkc - 1)) * (4 * ESZ);
+        vs = (const uint8_t*)p.vs + (ub0 * nvc + min(lane, nvc - 1)) * (4 * ESZ);
+        dkz = kaff ? (const uint8_t*)p.kz - (const uint8_t*)p.ks : 0;
+        dvz = vaff ? (const uint8_t*)p.vz - (const uint8_t*)p.vs : 0;
     }
 
-    __device__ __forceinline__ int kbits() const { return W8 ? 8 : p.k_bits; }
-    __device__ __forceinline__ int vbits() const { return W8 ? 8 : p.v_bits; }
-
-    // Four numbers of a metadata section, widened later.
-    __device__ __forceinline__ u32x4 load_chunk(const float* sec, size_t first, int n) const
+    __device__ __forceinline__ u32x4 load_chunk(const uint8_t* at) const
     {
-        const size_t at = first * n + min(lane, n - 1);
-        if (p.meta16) {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2*)sec + at);
+        if constexpr (M16) {
+            const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
             return u32x4{x.x, x.y, 0u, 0u};
+        } else {
+            return __builtin_nontemporal_load((const u32x4*)at);
         }
-        return __builtin_nontemporal_load((const u32x4*)sec + at);
     }
 
-    __device__ __forceinline__ void load(Raw<W8>& r, int blk) const
+    // Every lane issues the same loads whatever the block.
+    __device__ __forceinline__ void load(Raw<KB, VB, M16>& r, int blk) const
     {
-        const size_t i = ub0 + blk;
-        const int kb = kbits(), vb = vbits();
-        // a lane's pieces of half block e are NKB kb bytes; the value pieces NMB vb bytes
-        const uint8_t* kc = (const uint8_t*)p.kc;
+        constexpr int ESZ = M16 ? 2 : 4;
+        const uint8_t* kb = k + (size_t)blk * (2 * 64 * NKB * KB);
         if constexpr (PB == 1) {
-            static_assert(PB > 1 || NKB == 2, "four key pieces per lane");
-            const uint8_t *k0 = kc + ((i * 2) * 64 + lane) * (NKB * kb), *k1 = k0 + 64 * (NKB * kb);
-            load_pieces<2>(k0, kb, r.k);
-            if constexpr (W8)
-                load_pieces<2>(k1, 8, r.k + 4);
-            else if (kb == 4)
-                load_pieces<2>(k1, 4, r.k + 2);
-            else
-                load_pieces<2>(k1, 2, r.k + 1);
+            load_bytes<2 * KB>(kb, r.k);
+            load_bytes<2 * KB>(kb + 64 * NKB * KB, r.k + KB / 2);
         } else {
-            const int e = PB == 2 ? part : part >> 1, kb0 = PB == 2 ? 0 : 4 * (part & 1);
-            load_pieces<4>(kc + ((i * 2 + e) * 64 + lane) * (NKB * kb) + kb0 * kb, kb, r.k);
+            load_bytes<4 * KB>(kb, r.k);
         }
-        load_pieces<4>((const uint8_t*)p.vc + (i * 64 + lane) * (NMB * vb) + 4 * part * vb, vb, r.v);
-        r.ks = load_chunk(p.ks, i, nkc);
-        r.kz = kaff ? load_chunk(p.kz, i, nkc) : u32x4{0u, 0u, 0u, 0u};
-        r.vs = load_chunk(p.vs, i, nvc);
-        r.vz = vaff ? load_chunk(p.vz, i, nvc) : u32x4{0u, 0u, 0u, 0u};
+        load_bytes<4 * VB>(v + (size_t)blk * (64 * NMB * VB), r.v);
+        const uint8_t *a = ks + (size_t)blk * (nkc * 4 * ESZ), *b = vs + (size_t)blk * (nvc * 4 * ESZ);
+        r.ks = load_chunk(a);
+        r.kz = load_chunk(a + dkz);
+        r.vs = load_chunk(b);
+        r.vz = load_chunk(b + dvz);
     }
 
     // The numbers of a chunk pair: scale, and offset of the centred code.
@@ -345,8 +334,8 @@ struct Builder {
     {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            sv[e] = p.meta16 ? f16_bits_to_f32((uint16_t)(s[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(s[e]);
-            zv[e] = p.meta16 ? f16_bits_to_f32((uint16_t)(z[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(z[e]);
+            sv[e] = M16 ? f16_bits_to_f32((uint16_t)(s[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(s[e]);
+            zv[e] = M16 ? f16_bits_to_f32((uint16_t)(z[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(z[e]);
             const bool on = whole || 4 * (lane & 7) + e < live;
             sv[e] = on ? sv[e] : 0.0f;
             zv[e] = on && aff ? fmaf(mid, sv[e], zv[e]) : 0.0f;
@@ -355,32 +344,22 @@ struct Builder {
 
     // This wave's part of the image of a coded block whose first `live` tokens
     // exist.  img: the image; meta: its scales; st: this wave's stage.
-    template <int KB, int VB>
-    __device__ __forceinline__ void coded(const Raw<W8>& r, int live, uint8_t* img, float* meta, float* st) const
+    __device__ __forceinline__ void coded_image(const Raw<KB, VB, M16>& r, int live, uint8_t* img, float* meta,
+                                                float* st) const
     {
         const int qg = lane >> 4;
-        const Coding kc = coding<KB>(kaff), vc = coding<VB>(vaff);
-        float ksv[4], kzv[4], vsv[4], vzv[4];
-        widen(r.ks, r.kz, kaff, kc.mid, live, KH, ksv, kzv);
-        widen(r.vs, r.vz, vaff, vc.mid, live, false, vsv, vzv);
-        // powers of two that bring the block's values (and reconstructed keys)
-        // to 2^12 at most: hi + lo then holds them to 2^-37 of the largest
-        float vtop = 0.0f, ktop = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            vtop = fmaxf(vtop, fmaf(vc.mid, vsv[e], fabsf(vzv[e])));
-            ktop = fmaxf(ktop, fmaf(kc.mid, ksv[e], fabsf(kzv[e])));
-        }
-        const float vf = scale_to_range(wave_max(lane < nvc ? vtop : 0.0f));
-        float kf = 1.0f;
-        if constexpr (KH)
-            kf = scale_to_range(wave_max(lane < nkc ? ktop : 0.0f));
         // ---- keys
-        half8 a[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            a[i] = centred<KB>(r.k, i, kc.centre);
+        const Coding kc = coding<KB>(kaff);
+        float ksv[4], kzv[4], kf = 1.0f;
+        widen(r.ks, r.kz, kaff, kc.mid, live, KH, ksv, kzv);
         if constexpr (KH) {
+            // times a power of two that brings the block's keys to 2^12 at most:
+            // hi + lo then holds them to 2^-37 of the largest
+            float top = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                top = fmaxf(top, fmaf(kc.mid, ksv[e], fabsf(kzv[e])));
+            kf = scale_to_range(wave_max(lane < nkc ? top : 0.0f));
             // channel c: scale at st[c], offset at st[D + c]
             if (lane < nkc) {
                 *(float4*)(st + 4 * lane) = float4{ksv[0] * kf, ksv[1] * kf, ksv[2] * kf, ksv[3] * kf};
@@ -389,90 +368,72 @@ struct Builder {
             lds_order();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int e = PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1;
-                const int kb = PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i;
+                const int kb = kblock(i);
                 const float* s = st + 32 * kb + 8 * qg;
                 const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
                 const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
                 const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
                 const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+                const half8 a = centred<KB>(r.k, i, kc.centre);
                 float x[8];
                 half8 hi, lo;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    x[j] = fmaf((float)a[i][j], sn[perm4(j)], zn[perm4(j)]);
+                    x[j] = fmaf((float)a[j], sn[perm4(j)], zn[perm4(j)]);
                 split_nearest(x, &hi, &lo);
-                uint8_t* at = img + 1024 * (e * NKB + kb) + 16 * lane;
+                uint8_t* at = img + 1024 * (half(i) * NKB + kb) + 16 * lane;
                 *(half8*)at = hi;
                 *(half8*)(at + 64 * D) = lo;
             }
             lds_order();
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1;
-                const int kb = PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i;
-                *(half8*)(img + 1024 * (e * NKB + kb) + 16 * lane) = a[i];
-            }
+            for (int i = 0; i < 4; ++i)
+                *(half8*)(img + 1024 * (half(i) * NKB + kblock(i)) + 16 * lane) = centred<KB>(r.k, i, kc.centre);
             if (part == 0 && lane < nkc) {
                 const float f = p.sm_log2;
                 *(float4*)(meta + 4 * lane) = float4{ksv[0] * f, ksv[1] * f, ksv[2] * f, ksv[3] * f};
                 *(float4*)(meta + D + 4 * lane) = float4{kzv[0] * f, kzv[1] * f, kzv[2] * f, kzv[3] * f};
             }
         }
-        // ---- values: group g's scales at st[32 g], offsets at st[D + 32 g]
+        __builtin_amdgcn_sched_barrier(0);  // (the registers of one side at a time)
+        // ---- values, likewise; group g's scales at st[32 g], offsets at st[D + 32 g]
+        const Coding vc = coding<VB>(vaff);
+        float vsv[4], vzv[4], top = 0.0f;
+        widen(r.vs, r.vz, vaff, vc.mid, live, false, vsv, vzv);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            top = fmaxf(top, fmaf(vc.mid, vsv[e], fabsf(vzv[e])));
+        const float vf = scale_to_range(wave_max(lane < nvc ? top : 0.0f));
         if (lane < nvc) {
             *(float4*)(st + 4 * lane) = float4{vsv[0] * vf, vsv[1] * vf, vsv[2] * vf, vsv[3] * vf};
             *(float4*)(st + D + 4 * lane) = float4{vzv[0] * vf, vzv[1] * vf, vzv[2] * vf, vzv[3] * vf};
         }
         lds_order();
-        float sn[8], zn[8];
+        const int lg = 31 - __builtin_clz(p.v_group);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int mb = 4 * part + i;
-            if (i == 0 || (i == 2 && p.v_group == 32)) {  // a group is two pieces or all four
-                const float* s = st + 32 * (16 * mb / p.v_group) + 8 * qg;
-                const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
-                const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
-                const float sx[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-                const float zx[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sn[j] = sx[perm4(j)];
-                    zn[j] = zx[perm4(j)];
-                }
-            }
+            const float* s = st + 32 * (16 * mb >> lg) + 8 * qg;
+            const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
+            const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
+            const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+            const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
             const half8 c = centred<VB>(r.v, i, vc.centre);
             float x[8];
             half8 hi, lo;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                x[j] = fmaf((float)c[j], sn[j], zn[j]);
+                x[j] = fmaf((float)c[j], sn[perm4(j)], zn[perm4(j)]);
             split_nearest(x, &hi, &lo);
             uint8_t* at = img + key_bytes(D, KH) + 1024 * mb + 16 * lane;
             *(half8*)at = hi;
             *(half8*)(at + 64 * D) = lo;
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (part == 0 && lane == 0) {
             meta[2 * D] = vf;
             meta[2 * D + 1] = KH ? p.sm_log2 * (1.0f / kf) : 0.0f;
-        }
-    }
-
-    __device__ __forceinline__ void coded_image(const Raw<W8>& r, int live, uint8_t* img, float* meta, float* st) const
-    {
-        if constexpr (W8) {
-            coded<8, 8>(r, live, img, meta, st);
-        } else if (p.k_bits == 4) {
-            if (p.v_bits == 4)
-                coded<4, 4>(r, live, img, meta, st);
-            else
-                coded<4, 2>(r, live, img, meta, st);
-        } else {
-            if (p.v_bits == 4)
-                coded<2, 4>(r, live, img, meta, st);
-            else
-                coded<2, 2>(r, live, img, meta, st);
         }
     }
 
@@ -483,52 +444,53 @@ struct Builder {
     {
         const int qg = lane >> 4, hh = lane & 15;
         const half8 zero = {};
+        // (dead tokens read a live row and are cleared: no load waits for a branch)
         u32x4 kw[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int e = PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1;
-            const int kb = PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i;
-            const int t = min(8 * (hh >> 2) + 4 * e + (hh & 3), live - 1);
-            kw[i] = *(const u32x4*)(kr + (size_t)((first + t) % ring) * D + 32 * kb + 8 * qg);
+            const int t = min(8 * (hh >> 2) + 4 * half(i) + (hh & 3), live - 1);
+            kw[i] = *(const u32x4*)(kr + (uint32_t)((first + t) % ring * D + 32 * kblock(i) + 8 * qg));
         }
-        // (dead tokens read a live row and are cleared: no load waits for a branch)
-        const uint16_t* row[8];
+        uint32_t row[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            row[j] = vr + (size_t)((first + min(8 * qg + perm4(j), live - 1)) % ring) * D + 64 * part + hh;
-        uint16_t h[4][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                h[i][j] = row[j][16 * i];
+            row[j] = (first + min(8 * qg + perm4(j), live - 1)) % ring * D + 64 * part + hh;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int e = PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1;
-            const int kb = PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i;
-            const bool on = 8 * (hh >> 2) + 4 * e + (hh & 3) < live;
+            const bool on = 8 * (hh >> 2) + 4 * half(i) + (hh & 3) < live;
             u32x4 a;  // dword j: channels j and j + 4
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t x = kw[i][j >> 1], y = kw[i][2 + (j >> 1)];
                 a[j] = !on ? 0u : j & 1 ? (x >> 16) | (y & 0xFFFF0000u) : (x & 0xFFFFu) | (y << 16);
             }
-            uint8_t* at = img + 1024 * (e * NKB + kb) + 16 * lane;
+            uint8_t* at = img + 1024 * (half(i) * NKB + kblock(i)) + 16 * lane;
             *(u32x4*)at = a;
             if constexpr (KH)
                 *(half8*)(at + 64 * D) = zero;
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            u32x4 w;
+        for (int i = 0; i < 4; i += 2) {
+            uint16_t h[2][8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                w[j] = 8 * qg + j < live ? h[i][2 * j] : 0u;
-                w[j] |= 8 * qg + j + 4 < live ? (uint32_t)h[i][2 * j + 1] << 16 : 0u;
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    h[u][j] = vr[row[j] + 16 * (i + u)];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = 8 * qg + j < live ? h[u][2 * j] : 0u;
+                    w[j] |= 8 * qg + j + 4 < live ? (uint32_t)h[u][2 * j + 1] << 16 : 0u;
+                }
+                uint8_t* at = img + key_bytes(D, KH) + 1024 * (4 * part + i + u) + 16 * lane;
+                *(u32x4*)at = w;
+                *(half8*)(at + 64 * D) = zero;
             }
-            uint8_t* at = img + key_bytes(D, KH) + 1024 * (4 * part + i) + 16 * lane;
-            *(u32x4*)at = w;
-            *(half8*)(at + 64 * D) = zero;
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (part == 0) {
             if (!KH && lane < nkc) {
@@ -561,16 +523,14 @@ struct Rows {
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
     int lim0, lim1;          // the least and the most of the wave's rows (uniform)
 
-    // Query rows of tile c: channels 32 kb + 8 qg .. + 7 of this lane's row, from `src` (null: no such row).
+    // Query rows of tile c, this lane's at src (channels 32 kb + 8 qg .. + 7 of it).
     __device__ __forceinline__ void load_query(int c, const uint16_t* src, float rot_c, int lane)
     {
         const int qg = lane >> 4;
         float v[NKB][8];
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
-            u32x4 w = {0u, 0u, 0u, 0u};
-            if (src)
-                w = *(const u32x4*)(src + 32 * kb + 8 * qg);
+            const u32x4 w = *(const u32x4*)(src + 32 * kb + 8 * qg);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[kb][2 * j] = __uint_as_float(w[j] << 16);
@@ -602,15 +562,17 @@ struct Rows {
                             v[kb][j] = a + b;
                             v[kb + h][j] = a - b;
                         }
+            const float s16 = qg & 1 ? -1.0f : 1.0f, s32 = qg & 2 ? -1.0f : 1.0f;
 #pragma unroll
-            for (int h = 1; h < 4; h <<= 1)
+            for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float other = __shfl_xor(v[kb][j], 16 * h);
-                        v[kb][j] = qg & h ? other - v[kb][j] : v[kb][j] + other;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t x = __float_as_uint(v[kb][j]);
+                    auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+                    const uint32_t y = __float_as_uint(fmaf(s16, __uint_as_float(a[1]), __uint_as_float(a[0])));
+                    auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+                    v[kb][j] = fmaf(s32, __uint_as_float(b[1]), __uint_as_float(b[0]));
+                }
         }
         float sum[NG];
 #pragma unroll
@@ -864,7 +826,7 @@ __device__ __forceinline__ size_t global_row(const SharedParams& p, const Item& 
     return ((size_t)it.seq0 * p.C + t) * p.H_q + (size_t)it.j * G + (r - t * G);
 }
 
-template <int D, int KG, bool W8, bool ROT>
+template <int D, int KG, int KB, int VB, bool M16, bool ROT>
 __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedParams sp)
 {
     constexpr bool KH = KG == 0;
@@ -897,60 +859,69 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedParams sp)
     const int top = it.lim + (it.causal ? (it.r0 + left - 1) / G : 0);  // the most that a row sees
     const int nv = min(nsb, (top + p.sink + 31) >> 5) + (top > 0 ? (top + 31) >> 5 : 0);
     const int v0 = min(nv, it.split * sp.bps[it.seg]), v1 = min(nv, v0 + sp.bps[it.seg]);
-    const Builder<D, KH, W8> B(p, it.unit, wave % PB, lane);
+    const Builder<D, KH, KB, VB, M16> B(p, it.unit, wave % PB, lane);
     const int own = wave / PB;  // the image of a phase that this wave builds
-    Raw<W8> raw;
-    const auto prefetch = [&](int v) {  // (fp16 blocks are read when they are built)
-        if (v < v1 && v >= nsb && 32 * (v - nsb) < p.nq)
-            B.load(raw, v - nsb);
+    // Block v's loads, or of the nearest coded block (fp16 blocks are read when
+    // they are built): without branches, so that nothing waits for them early.
+    const int ncb = (p.nq + 31) >> 5;
+    const auto prefetch = [&](int v) {
+        Raw<KB, VB, M16> r;
+        if (ncb > 0)
+            B.load(r, min(max(min(v, v1 - 1) - nsb, 0), ncb - 1));
+        return r;
     };
-    prefetch(v0 + own);
+    Raw<KB, VB, M16> raw = prefetch(v0 + own);
 
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const int r = 16 * (rw + R * c) + hh, rc = min(r, left - 1);
         T.lim[c] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
-        T.load_query(c, r < left ? sp.q + global_row(sp, it, G, it.r0 + r) * D : nullptr, p.rot_c, lane);
+        T.load_query(c, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
     }
 
     uint8_t* metas = lds + NI * BI;
     float* st = (float*)(metas + NI * BM + kStage * wave);
-    for (int v = v0; v < v1; v += NI) {
-        // ---- build
-        const int mine = v + own;
-        if (mine < v1) {
-            uint8_t* img = lds + own * BI;
-            float* meta = (float*)(metas + own * BM);
-            const int tb = mine - nsb;
-            if (mine < nsb) {
-                const size_t at = (size_t)it.unit * p.sink * D;
-                B.rows_image(p.kq + at, p.vq + at, 32 * mine, p.sink, p.n_sink - 32 * mine, img, meta);
-            } else if (32 * tb < p.nq) {
-                B.coded_image(raw, min(32, p.nq - 32 * tb), img, meta, st);
-            } else {
-                const size_t at = (size_t)it.unit * p.ring * D;
-                B.rows_image(p.kr + at, p.vr + at, 32 * tb, p.ring, p.n - 32 * tb, img, meta);
+    // (two loops, so that the registers of a wave's tiles have one place in each)
+    const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
+        constexpr int NT = decltype(tiles_now)::value;
+        for (int v = v0; v < v1; v += NI) {
+            // ---- build
+            const int mine = v + own;
+            if (mine < v1) {
+                uint8_t* img = lds + own * BI;
+                float* meta = (float*)(metas + own * BM);
+                const int tb = mine - nsb;
+                if (tb >= 0 && 32 * tb < p.nq) {
+                    B.coded_image(raw, min(32, p.nq - 32 * tb), img, meta, st);
+                } else {
+                    const bool sink = tb < 0;
+                    const int first = sink ? 32 * mine : 32 * tb, rows = sink ? p.sink : p.ring;
+                    const size_t at = (size_t)it.unit * rows * D;
+                    B.rows_image((sink ? p.kq : p.kr) + at, (sink ? p.vq : p.vr) + at, first, rows,
+                                 (sink ? p.n_sink : p.n) - first, img, meta);
+                }
             }
+            raw = prefetch(mine + NI);
+            sync_lds();
+            // ---- consume
+            for (int i = bw; i < NI && v + i < v1; i += BW) {
+                const int tb = v + i - nsb;
+                const bool sink = tb < 0;
+                const int t0 = sink ? 32 * (v + i) : 32 * tb, off = sink ? p.sink : 0;
+                if (t0 >= T.lim1 + off)
+                    continue;
+                const int live = sink ? p.n_sink - t0 : p.n - t0;
+                const uint8_t* img = lds + i * BI;
+                const float* meta = (const float*)(metas + i * BM);
+                T.template consume<NT>(img, meta, t0, off, live, lane);
+            }
+            sync_lds();
         }
-        prefetch(mine + NI);
-        sync_lds();
-        // ---- consume
-        for (int i = bw; i < NI && v + i < v1; i += BW) {
-            const int tb = v + i - nsb;
-            const bool sink = tb < 0;
-            const int t0 = sink ? 32 * (v + i) : 32 * tb, off = sink ? p.sink : 0;
-            if (t0 >= T.lim1 + off)
-                continue;
-            const int live = sink ? p.n_sink - t0 : p.n - t0;
-            const uint8_t* img = lds + i * BI;
-            const float* meta = (const float*)(metas + i * BM);
-            if (CT == 1 || nt == 1)
-                T.template consume<1>(img, meta, t0, off, live, lane);
-            else
-                T.template consume<CT>(img, meta, t0, off, live, lane);
-        }
-        sync_lds();
-    }
+    };
+    if (CT == 1 || nt <= 1)
+        walk(std::integral_constant<int, 1>{});
+    else
+        walk(std::integral_constant<int, CT>{});
 
     // ---- partials: of each wave when its rows are its own, else merged in LDS
     const float inv = T.vf == 0.0f ? 0.0f : 1.0f / T.vf;
@@ -1004,30 +975,36 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedParams sp)
     }
 }
 
-template <int D, int KG, bool W8, bool ROT>
-void launch_instance(const SharedParams& p, int items, hipStream_t stream)
+template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+hipError_t launch_instance(const SharedParams& p, int items, hipStream_t stream)
 {
-    launch_kernel(shared_kernel<D, KG, W8, ROT>, dim3(items), dim3(kThreads), (size_t)lds_bytes(D, KG == 0), stream, p);
+    launch_kernel(shared_kernel<D, KG, KB, VB, M16, ROT>, dim3(items), dim3(kThreads), (size_t)lds_bytes(D, KG == 0),
+                  stream, p);
+    return hipGetLastError();
 }
 
-template <int D, bool W8, bool ROT>
-hipError_t launch_groups(const SharedParams& p, int items, hipStream_t stream)
+template <int D, int KG, bool M16, bool ROT>
+hipError_t launch_widths(const SharedParams& p, int items, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
-    const int kg = a.k_axis == KVQ_PER_CHANNEL ? 0 : a.k_group / 32;
-    if (kg == 0)
-        launch_instance<D, 0, W8, ROT>(p, items, stream);
-    else if (kg == 1)
-        launch_instance<D, 1, W8, ROT>(p, items, stream);
-    else if (kg == 2)
-        launch_instance<D, 2, W8, ROT>(p, items, stream);
-    else if (kg == 4 && D >= 128)
-        launch_instance<D, D >= 128 ? 4 : 1, W8, ROT>(p, items, stream);
-    else if (kg == 8 && D >= 256)
-        launch_instance<D, D >= 256 ? 8 : 1, W8, ROT>(p, items, stream);
-    else
-        return hipErrorInvalidValue;
-    return hipGetLastError();
+    if (a.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
+        return launch_instance<D, KG, 8, 8, M16, ROT>(p, items, stream);
+    if (a.k_bits == 4)
+        return a.v_bits == 4 ? launch_instance<D, KG, 4, 4, M16, ROT>(p, items, stream)
+                             : launch_instance<D, KG, 4, 2, M16, ROT>(p, items, stream);
+    return a.v_bits == 4 ? launch_instance<D, KG, 2, 4, M16, ROT>(p, items, stream)
+                         : launch_instance<D, KG, 2, 2, M16, ROT>(p, items, stream);
+}
+
+// The kernels of one head size and key grouping.
+template <int D, int KG>
+hipError_t launch_family(const SharedParams& p, int items, hipStream_t stream)
+{
+    if (p.rotate)
+        return p.seg[0].meta16 ? launch_widths<D, KG, true, true>(p, items, stream)
+                               : launch_widths<D, KG, false, true>(p, items, stream);
+    return p.seg[0].meta16 ? launch_widths<D, KG, true, false>(p, items, stream)
+                           : launch_widths<D, KG, false, false>(p, items, stream);
 }
 
 }  // namespace shr

@@ -1,10 +1,10 @@
-// Shared-prefix attention kernels of one head size (KVQ_PART_D), for plain or
-// rotated queries (KVQ_PART_ROT): built once per pair, so that they compile in
-// parallel.
+// Shared-prefix attention kernels of one head size (KVQ_PART_D) and key
+// grouping (KVQ_PART_KG: per-token group size / 32, 0 for per-channel keys):
+// built once per pair, so that they compile in parallel.
 #include "shared_impl.h"
 
-#if !defined(KVQ_PART_D) || !defined(KVQ_PART_ROT)
-#error "shared_part.hip is compiled once per family with KVQ_PART_D and KVQ_PART_ROT defined"
+#if !defined(KVQ_PART_D) || !defined(KVQ_PART_KG)
+#error "shared_part.hip is compiled once per family with KVQ_PART_D and KVQ_PART_KG defined"
 #endif
 
 #define KVQ_CAT2(a, b, c) a##_##b##_##c
@@ -12,11 +12,9 @@
 
 namespace kvq {
 
-hipError_t KVQ_CAT(launch_shared, KVQ_PART_D, KVQ_PART_ROT)(const SharedParams& p, int items, hipStream_t stream)
+hipError_t KVQ_CAT(launch_shared, KVQ_PART_D, KVQ_PART_KG)(const SharedParams& p, int items, hipStream_t stream)
 {
-    // 8-bit codes come as keys and values both
-    return p.seg[0].k_bits == 8 ? shr::launch_groups<KVQ_PART_D, true, KVQ_PART_ROT != 0>(p, items, stream)
-                                : shr::launch_groups<KVQ_PART_D, false, KVQ_PART_ROT != 0>(p, items, stream);
+    return shr::launch_family<KVQ_PART_D, KVQ_PART_KG>(p, items, stream);
 }
 
 }  // namespace kvq
