@@ -31,6 +31,9 @@ ROOT = os.path.dirname(HERE)
 # MFMA accumulators in VGPRs: the attention loop rescales them with VALU
 # instructions, and AGPR accumulators cost a copy each way per block.
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+# Maxima without an operation that quiets each NaN operand first (the path's
+# inputs are finite, and no arithmetic of these kernels makes one).
+_NO_NANS = ["-fno-honor-nans"]
 # (source, object name, extra flags).  The decode split kernels are built
 # from one source, once per (head size, metadata width, key axis) family, the
 # prefill kernels once per head size, the shared-prefix kernels once per (head
@@ -42,7 +45,7 @@ UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64
 UNITS += [("attn_part.hip", f"attn_{d}_{m}_{pc}",
            _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_M16={m}", f"-DKVQ_PART_PC={pc}"])
           for d in (64, 128, 256) for m in (0, 1) for pc in (0, 1)]
-UNITS += [("shared_part.hip", f"shared_{d}_{g}", _VGPR_MFMA + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_KG={g}"])
+UNITS += [("shared_part.hip", f"shared_{d}_{g}", _VGPR_MFMA + _NO_NANS + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_KG={g}"])
           for d in (64, 128, 256) for g in (0, 1, 2, 4, 8) if 32 * g <= d]
 SOURCES = sorted({u[0] for u in UNITS})
 

@@ -142,23 +142,31 @@ __device__ __forceinline__ float wave_max(float x)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_rows(x))));
 }
 
-// The power of two f with x f in (2^11, 2^12], f kept within 2^-114 .. 2^112 (x >= 0).
+// A power of two f with x f in (2^8, 2^12], its exponent a multiple of four, so
+// that neighbouring blocks mostly share it (x >= 0; f is kept within 2^-115 .. 2^113).
 __device__ __forceinline__ float scale_to_range(float x)
 {
-    const uint32_t e = min(max((__float_as_uint(x) >> 23) + 1, 27u), 253u);  // x < 2^(e - 127)
+    const uint32_t e = min(max(((__float_as_uint(x) >> 23) + 4) & ~3u, 26u), 254u);  // x < 2^(e - 127)
     return __uint_as_float((254 + 12 - e) << 23);
 }
 
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 // fp32 -> fp16 hi + lo, both to nearest: |v - hi - lo| <= 2^-23 |v| (2^-25
-// absolute where lo is subnormal).
+// absolute where lo is subnormal).  Pairs, for the packed conversion.
 __device__ __forceinline__ void split_nearest(const float* v, half8* hi, half8* lo)
 {
+    u32x4 h, l;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const _Float16 h = (_Float16)v[e];
-        (*hi)[e] = h;
-        (*lo)[e] = (_Float16)(v[e] - (float)h);
+    for (int j = 0; j < 4; ++j) {
+        const f16x2 a = __builtin_convertvector((f32x2{v[2 * j], v[2 * j + 1]}), f16x2);
+        const f16x2 b = __builtin_convertvector((f32x2{v[2 * j] - (float)a.x, v[2 * j + 1] - (float)a.y}), f16x2);
+        h[j] = __builtin_bit_cast(uint32_t, a);
+        l[j] = __builtin_bit_cast(uint32_t, b);
     }
+    *hi = __builtin_bit_cast(half8, h);
+    *lo = __builtin_bit_cast(half8, l);
 }
 
 // LDS accesses of a wave are performed in order; the compiler keeps them in
@@ -199,8 +207,6 @@ __device__ __forceinline__ Coding coding(bool affine)
                                                    : (affine ? 0xC580C580u : 0xC600C600u);
     return c;
 }
-
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 // Piece k (eight codes) of the words -> (c_j - mid, c_{j+4} - mid) in dword j,
 // i.e. element e holds code perm4(e): the code as mantissa bits under an
@@ -624,6 +630,7 @@ struct Rows {
         const int qg = lane >> 4, hh = lane & 15;
         const uint8_t* fb = img + 16 * lane;
         const auto frag = [&](int at) { return *(const half8*)(fb + at); };
+        const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
         // ---- scores: l[c][4 e + i] is token 8 qg + 4 e + i
         float l[NT][8];
 #pragma unroll
@@ -698,22 +705,23 @@ struct Rows {
             }
         }
         // ---- the values' power of two: accumulators follow the largest values
-        const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
         float bias = kPBits, back = 1.0f;
         if (f != vf) {
-            if (vf == 0.0f || f < vf) {
-                const float r = vf == 0.0f ? 0.0f : f / vf;  // (powers of two)
+            const int d = (int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23);  // log2(f / vf)
+            const float r = __uint_as_float((uint32_t)min(max(127 + d, 0), 254) << 23);
+            if (vf == 0.0f || d < 0) {
+                if (vf != 0.0f) {
 #pragma unroll
-                for (int c = 0; c < CT; ++c)
+                    for (int c = 0; c < CT; ++c)
 #pragma unroll
-                    for (int mb = 0; mb < NMB; ++mb)
-                        oacc[c][mb] *= r;
+                        for (int mb = 0; mb < NMB; ++mb)
+                            oacc[c][mb] *= r;
+                }
                 vf = f;
             } else {
                 // smaller values: their probabilities make up for it
-                const int d = (int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23);
                 bias = kPBits - (float)d;
-                back = f / vf;
+                back = r;
             }
         }
         // ---- softmax, and the probabilities' operands
