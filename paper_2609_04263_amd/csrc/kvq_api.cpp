@@ -1061,8 +1061,8 @@ static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, 
     p.rot_c = rotation_constant(suffix->D);
     for (int g = 0; g <= P; ++g)
         p.first[g] = first ? first[g] : B / P * g;
-    const int items = kvq::shared_plan(&p, suffix->D, B);
-    return kvq::launch_shared(p, suffix->D, items, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+    kvq::shared_plan(&p, suffix->D, B);
+    return kvq::launch_shared(p, suffix->D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
 kvq_status kvq_decode_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,

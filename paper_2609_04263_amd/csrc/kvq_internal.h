@@ -242,19 +242,19 @@ struct SharedParams {
     float* part_ml;      // fp32 [S0 + S1][rows][2]  (running max in log2 units, sum)
     size_t rows;         // B C H_q
     int C, H_q, P;
-    int tile_rows;       // query rows of a work item, at most
     int S[2], bps[2];    // ranges of a tile, 32-token blocks per range
-    int tiles0, items0;  // prefix tiles, prefix items (tiles0 S[0])
+    int tiles0, items0;  // prefix tiles, prefix items (tiles0 S[0]); the suffix items come after them
+    int image_items, direct0, direct_items;  // items of the image kernel, and those of the direct one from direct0
     int rotate;
     float rot_c;
     int first[kSharedPrefixes + 1];  // first sequence of each group
     int tile0[kSharedPrefixes + 1];  // first tile of each group
 };
-// Fills tile_rows, S, bps, tiles0, items0 and tile0 from the rest; returns the work items.
-int shared_plan(SharedParams* p, int D, int B);
+// Fills S, bps, tiles0, items0, tile0 and the kernels' items from the rest.
+void shared_plan(SharedParams* p, int D, int B);
 // Upper bound of S0 + S1 for any lengths and groups.
 int shared_split_bound(int B, int H, int D, int C, int G);
-hipError_t launch_shared(const SharedParams& p, int D, int items, hipStream_t stream);
+hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream);
 
 }  // namespace kvq
 

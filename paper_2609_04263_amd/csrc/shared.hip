@@ -5,7 +5,7 @@
 
 namespace kvq {
 
-#define KVQ_FAMILY(D, KG) hipError_t launch_shared_##D##_##KG(const SharedParams& p, int items, hipStream_t stream);
+#define KVQ_FAMILY(D, KG) hipError_t launch_shared_##D##_##KG(const SharedParams& p, hipStream_t stream);
 KVQ_FAMILY(64, 0) KVQ_FAMILY(64, 1) KVQ_FAMILY(64, 2)
 KVQ_FAMILY(128, 0) KVQ_FAMILY(128, 1) KVQ_FAMILY(128, 2) KVQ_FAMILY(128, 4)
 KVQ_FAMILY(256, 0) KVQ_FAMILY(256, 1) KVQ_FAMILY(256, 2) KVQ_FAMILY(256, 4) KVQ_FAMILY(256, 8)
@@ -13,55 +13,92 @@ KVQ_FAMILY(256, 0) KVQ_FAMILY(256, 1) KVQ_FAMILY(256, 2) KVQ_FAMILY(256, 4) KVQ_
 
 namespace {
 
-// A workgroup fills a compute unit, so a round is one work item per CU.
-constexpr int kRound = 256;
+// Work items of a round: one image_kernel workgroup per CU, eight wave pairs of
+// direct_kernel workgroups.
+constexpr int kImageRound = 256, kDirectRound = 512;
 
 int ceil_div(int a, int b)
 {
     return (a + b - 1) / b;
 }
 
-// Ranges that a segment of `tiles` tiles is cut into, at most.
-int shared_splits(long long tiles)
+// How a segment's rows are taken: `rows` the most that one of its units has.
+struct Kind {
+    bool direct;
+    int per, step, round;  // rows per item, blocks that a range is a multiple of, items of a round
+};
+
+Kind kind_of(int D, int rows)
 {
-    return tiles > 0 && tiles < kRound ? (int)(kRound / tiles) : 1;
+    if (rows <= shr::kDirectRows)
+        return {true, shr::kDirectRows, shr::kDirectWaves, kDirectRound};
+    return {false, shr::item_rows(D), shr::images(D), kImageRound};
 }
 
-// Joins the partials of a row: one thread per four output channels,
-// O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, then the inverse rotation
-// of a rotating format (the normalized transform is its own inverse) in LDS.
+// Ranges that a segment of `tiles` tiles is cut into, at most.
+int shared_splits(long long tiles, int round)
+{
+    return tiles > 0 && tiles < round ? (int)(round / tiles) : 1;
+}
+
+// Joins the partials of a row: D / 4 threads, four output channels each, take
+// every J-th partial, J of them side by side,
+//     O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s,
+// then their sums meet in LDS and a rotating format's rows are rotated back
+// there (the normalized transform is its own inverse).  Bound by the read of the
+// partials, which needs many loads in flight: with one thread per four channels
+// walking all of 33 partials, 2048 rows at D = 128 took 17 us.
 constexpr int kJoinThreads = 256;
 
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p)
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p, int J)
 {
-    constexpr int R = kJoinThreads / (D / 4);  // rows per workgroup
-    __shared__ __attribute__((aligned(16))) float x[R * D];
-    const int rl = threadIdx.x / (D / 4), d = 4 * (threadIdx.x % (D / 4));
+    constexpr int TR = D / 4, SLOTS = kJoinThreads / TR;  // threads of a row, rows J = 1 would take
+    __shared__ __attribute__((aligned(16))) float x[SLOTS * D];
+    __shared__ float xl[SLOTS];
+    const int slot = threadIdx.x / TR, d = 4 * (threadIdx.x % TR);
+    const int R = SLOTS / J, rl = slot % R, j = slot / R;
     const size_t row = (size_t)blockIdx.x * R + rl;
     const int S = p.S[0] + p.S[1];
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    float M = -INFINITY, L = 0.0f;
+    float L = 0.0f;
     if (row < p.rows) {
-        for (int s = 0; s < S; ++s)
-            M = fmaxf(M, p.part_ml[2 * ((size_t)s * p.rows + row)]);
+        const float* ml = p.part_ml + 2 * row;
+        float M = -INFINITY;
 #pragma unroll 4
-        for (int s = 0; s < S; ++s) {
-            const size_t at = (size_t)s * p.rows + row;
-            const float2 ml = *(const float2*)(p.part_ml + 2 * at);
-            const floatx4 o = *(const floatx4*)(p.part_o + at * D + d);
-            const float w = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - M);
+        for (int s = 0; s < S; ++s)
+            M = fmaxf(M, ml[2 * (size_t)s * p.rows]);
+#pragma unroll 4
+        for (int s = j; s < S; s += J) {
+            const float2 v = *(const float2*)(ml + 2 * (size_t)s * p.rows);
+            const floatx4 o = *(const floatx4*)(p.part_o + ((size_t)s * p.rows + row) * D + d);
+            const float w = v.x == -INFINITY ? 0.0f : fast_exp2(v.x - M);
             acc += o * w;
-            L += ml.y * w;
+            L += v.y * w;
+        }
+    }
+    if (J > 1) {
+        *(floatx4*)(x + slot * D + d) = acc;
+        if (d == 0)
+            xl[slot] = L;
+        __syncthreads();
+        if (slot < R) {
+            for (int k = 1; k < J; ++k) {
+                acc += *(const floatx4*)(x + (slot + k * R) * D + d);
+                L += xl[slot + k * R];
+            }
         }
     }
     acc *= 1.0f / L;  // every row sees a token
     if (!p.rotate) {
-        if (row < p.rows)
+        if (slot < R && row < p.rows)
             *(floatx4*)(p.out + row * D + d) = acc;
         return;
     }
-    *(floatx4*)(x + rl * D + d) = acc;
+    if (J > 1)
+        __syncthreads();
+    if (slot < R)
+        *(floatx4*)(x + slot * D + d) = acc;
     __syncthreads();
     for (int h = 1; h < D; h <<= 1) {
         for (int i = threadIdx.x; i < R * (D / 2); i += kJoinThreads) {
@@ -72,55 +109,70 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p)
         }
         __syncthreads();
     }
-    if (row < p.rows)
-        *(floatx4*)(p.out + row * D + d) = *(const floatx4*)(x + rl * D + d) * p.rot_c;
+    if (slot < R && row < p.rows)
+        *(floatx4*)(p.out + row * D + d) = *(const floatx4*)(x + slot * D + d) * p.rot_c;
 }
 
 template <int D>
 void launch_join(const SharedParams& p, hipStream_t stream)
 {
-    constexpr int R = kJoinThreads / (D / 4);
-    launch_kernel(join_kernel<D>, dim3((unsigned)((p.rows + R - 1) / R)), dim3(kJoinThreads), 0, stream, p);
+    constexpr int SLOTS = kJoinThreads / (D / 4);
+    const int S = p.S[0] + p.S[1];
+    int J = 1;
+    while (2 * J <= SLOTS && 4 * J <= S)
+        J *= 2;
+    const size_t R = SLOTS / J;
+    launch_kernel(join_kernel<D>, dim3((unsigned)((p.rows + R - 1) / R)), dim3(kJoinThreads), 0, stream, p, J);
 }
 
 }  // namespace
 
-// Work items.  Prefix items are long (many rows) and few, suffix items short
-// and many; the former start first and the latter fill the CUs that they leave.
-// So prefix units are cut for one round of their own, at most: ranges of
-// blocks of a whole number of build phases.
-int shared_plan(SharedParams* p, int D, int B)
+// Each segment is cut into ranges for one round of its kernel's workgroups, a
+// range a multiple of the blocks that a workgroup takes at a time.  When both
+// segments go to one kernel the prefix' items, the longer ones, start first.
+void shared_plan(SharedParams* p, int D, int B)
 {
     const AttnParams &a = p->seg[0], &b = p->seg[1];
-    const int per = shr::item_rows(D), NI = shr::images(D);
-    p->tile_rows = per;
+    int most = 0;
+    for (int g = 0; g < p->P; ++g)
+        most = p->first[g + 1] - p->first[g] > most ? p->first[g + 1] - p->first[g] : most;
+    const Kind kind[2] = {kind_of(D, most * p->C * a.G), kind_of(D, p->C * a.G)};
     p->tiles0 = 0;
     for (int g = 0; g < p->P; ++g) {
         p->tile0[g] = p->tiles0;
-        p->tiles0 += a.H * ceil_div((p->first[g + 1] - p->first[g]) * p->C * a.G, per);
+        p->tiles0 += a.H * ceil_div((p->first[g + 1] - p->first[g]) * p->C * a.G, kind[0].per);
     }
     p->tile0[p->P] = p->tiles0;
-    const int tiles[2] = {p->tiles0, B * a.H * ceil_div(p->C * a.G, per)};
+    const int tiles[2] = {p->tiles0, B * a.H * ceil_div(p->C * a.G, kind[1].per)};
     for (int k = 0; k < 2; ++k) {
         const AttnParams& s = k ? b : a;
-        const int blocks = ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32);
-        const int want = shared_splits(tiles[k]);
-        p->bps[k] = blocks > 0 ? ceil_div(ceil_div(blocks, want), NI) * NI : NI;
+        const int blocks = ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32), step = kind[k].step;
+        const int want = shared_splits(tiles[k], kind[k].round);
+        p->bps[k] = blocks > 0 ? ceil_div(ceil_div(blocks, want), step) * step : step;
         p->S[k] = ceil_div(blocks, p->bps[k]);
     }
-    p->items0 = p->tiles0 * p->S[0];
-    return p->items0 + tiles[1] * p->S[1];
+    p->items0 = tiles[0] * p->S[0];
+    const int items1 = tiles[1] * p->S[1];
+    // (a suffix never has more rows per unit than the prefix of its group)
+    p->image_items = (kind[0].direct ? 0 : p->items0) + (kind[1].direct ? 0 : items1);
+    p->direct0 = p->image_items;
+    p->direct_items = p->items0 + items1 - p->image_items;
 }
 
 int shared_split_bound(int B, int H, int D, int C, int G)
 {
-    // the groups' tiles are never fewer than one group's of all rows
-    const int per = shr::item_rows(D);
-    return shared_splits((long long)H * ceil_div(B * C * G, per)) +
-           shared_splits((long long)B * H * ceil_div(C * G, per));
+    // The groups' tiles are never fewer than one group's of all rows; with fewer
+    // rows per group either kernel may take them.
+    const auto most = [&](long long units, int rows) {
+        const Kind k = kind_of(D, rows);
+        const int one = shared_splits(units * ceil_div(rows, k.per), k.round);
+        const int direct = shared_splits(units * ceil_div(rows, shr::kDirectRows), kDirectRound);
+        return one > direct ? one : direct;
+    };
+    return most(H, B * C * G) + most((long long)B * H, C * G);
 }
 
-hipError_t launch_shared(const SharedParams& p, int D, int items, hipStream_t stream)
+hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
     const int kg = a.k_axis == KVQ_PER_CHANNEL ? 0 : a.k_group / 32;
@@ -128,7 +180,7 @@ hipError_t launch_shared(const SharedParams& p, int D, int items, hipStream_t st
     switch (1000 * D + kg) {
 #define KVQ_FAMILY(D, KG)                           \
     case 1000 * D + KG:                             \
-        e = launch_shared_##D##_##KG(p, items, stream); \
+        e = launch_shared_##D##_##KG(p, stream);        \
         break;
         KVQ_FAMILY(64, 0)
         KVQ_FAMILY(64, 1)

@@ -6,39 +6,42 @@
 // The two caches are two segments.  A segment's unit (cache sequence, KV head)
 // meets a set of query rows (sequence, chunk token, head): all rows of the
 // group for a prefix unit, one sequence's rows for a suffix unit.  A work item
-// is a range of a unit's 32-token blocks and up to 16 kTiles kWaves of its
-// rows; every item writes an unnormalized partial (m, l, o) per row, and a
-// second kernel joins a row's partials of both segments:
+// is a range of a unit's 32-token blocks and a tile of its rows; every item
+// writes an unnormalized partial (m, l, o) per row, and a last kernel joins a
+// row's partials of both segments:
 //     M = max m,  O = sum 2^(m - M) o / sum 2^(m - M) l.
-// So the codes of a prefix are read once per work item of its group's rows
-// instead of once per sequence.
+// So the codes of a prefix are read once per tile of its group's rows instead
+// of once per sequence.  Two kernels:
 //
-// Inside an item eight waves, two per SIMD, alternate between two phases:
-//   build    the waves turn the next kImages blocks into images in LDS, kParts
-//            waves per block: operand fragments of
-//            v_mfma_f32_16x16x32_f16, in the order in which the cache stores
-//            its codes (a 1 KiB fragment is one 16-byte piece per lane);
-//   consume  each wave multiplies its query rows with its share of the images.
-// With R row waves (the fewest powers of two that hold the rows) a wave has up
-// to kTiles tiles of 16 rows and every kWaves / R-th image, so that few rows
-// still occupy all waves.  What a block costs to convert is paid once for all
-// rows of the item, where decode attention, which converts in registers, pays
-// it once per 16 rows.
+//   image_kernel   more than 16 rows per unit.  Eight waves, two per SIMD; up to
+//                  128 tiles(D) rows.  In turns, the waves convert the next
+//                  kImages blocks into images in LDS (kParts waves per block)
+//                  and multiply their own rows with the present ones (two
+//                  buffers, one barrier per turn; the two waves of a SIMD take
+//                  the halves of a turn in opposite order, so that one's
+//                  matrix products run beside the other's conversions).  With
+//                  R row waves a wave has up to tiles(D) tiles of 16 rows and
+//                  every kWaves / R-th image.
+//   direct_kernel  at most 16 rows per unit (a suffix's queries, few samples):
+//                  four waves, each with blocks of its own, converts codes
+//                  into operands in registers.
 //
-// An image holds
+// An image (or a converted block) holds operand fragments of
+// v_mfma_f32_16x16x32_f16 in the order in which the cache stores its codes (a 1
+// KiB fragment is one 16-byte piece per lane):
 //   keys    per-token groups: the codes, centred (c - (2^b - 1) / 2, or c -
 //           2^(b-1) when symmetric), exact in fp16, with scales and offsets s, z'
 //           beside them: S = sum_g s_g (A_g . q_g) + z'_g sum q_g, the offsets
 //           by one fp32 MFMA of four groups.  Per-channel groups: the
 //           reconstructed key times a power of two, as fp16 hi + lo (22 bits);
 //   values  the reconstructed value times a power of two, hi + lo.
-// and the product of the values with the probabilities (hi + lo as well) is
-// three MFMAs, all but the 2^-22 of lo x lo.  Values as codes with p s as the
-// other operand take two, but cost each tile 40 vector operations per value
-// group, and a bias in the codes costs precision where outputs are small
-// beside the values: 32768 tokens of flat attention were 4.7e-4 off with
-// decode attention's operands and 1e-6 with these.
-// fp16 tokens (window, sink) are images as they are, with a lo half of zero.
+// The product of the values with the probabilities (hi + lo as well) is three
+// MFMAs, all but the 2^-22 of lo x lo.  Values as codes with p s as the other
+// operand take two, but cost each tile 40 vector operations per value group,
+// and a bias in the codes costs precision where outputs are small beside the
+// values: 32768 tokens of flat attention were 4.7e-4 off with decode
+// attention's operands and 1e-6 with these.
+// fp16 tokens (window, sink) are operands as they are, with a lo half of zero.
 //
 // Softmax: online per column in base 2, the running maximum raised only when a
 // block exceeds it by more than kTau; probabilities are at most 2^(kTau +
@@ -55,10 +58,12 @@ namespace kvq {
 namespace shr {
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr float kTau = 4.0f;     // lazy rescale threshold, log2 units
 constexpr float kPBits = 10.0f;  // probabilities are kept times 2^kPBits, so that their lo half is exact
 constexpr float kNegInf = -__builtin_inff();
+
+// ---- image_kernel
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
 // 16-row tiles per wave: 32 rows' accumulators and queries fit 256 registers
 // up to D = 128.
@@ -67,10 +72,16 @@ __host__ __device__ constexpr int tiles(int D)
     return D == 256 ? 1 : 2;
 }
 
-// Images of a build phase (LDS), and waves that build one.
+__host__ __device__ constexpr int item_rows(int D)
+{
+    return 16 * tiles(D) * kWaves;
+}
+
+// Images of a turn (LDS holds two turns'), and waves that build one: two key
+// and two value pieces per lane.
 __host__ __device__ constexpr int images(int D)
 {
-    return 512 / D;
+    return 256 / D;
 }
 
 __host__ __device__ constexpr int parts(int D)
@@ -78,14 +89,9 @@ __host__ __device__ constexpr int parts(int D)
     return kWaves / images(D);
 }
 
-__host__ __device__ constexpr int item_rows(int D)
-{
-    return 16 * tiles(D) * kWaves;
-}
-
-// ---- LDS: the images, then per image its scales and offsets ([group][32]
-// each) and two scalars, then 2 KiB per wave to pass a block's metadata
-// between lanes.  The merge of the waves reuses it from the start.
+// LDS: two buffers of images, per image its scales and offsets ([group][32]
+// each) and two scalars, then per wave room to pass a block's scales and
+// offsets between lanes.  The merge of the waves reuses it from the start.
 __host__ __device__ constexpr int key_bytes(int D, bool hilo)
 {
     return 64 * D * (hilo ? 2 : 1);
@@ -101,12 +107,33 @@ __host__ __device__ constexpr int meta_bytes(int D)
     return 2 * (D / 32) * 128 + 16;
 }
 
-constexpr int kStage = 2048;
-
-__host__ __device__ constexpr int lds_bytes(int D, bool hilo)
+__host__ __device__ constexpr int stage_bytes(int D)
 {
-    const int walk = images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * kStage;
+    return 8 * D;
+}
+
+__host__ __device__ constexpr int image_lds(int D, bool hilo)
+{
+    const int walk = 2 * images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * stage_bytes(D);
     const int merge = kWaves * 16 * (D + 2) * 4;
+    return walk > merge ? walk : merge;
+}
+
+// ---- direct_kernel
+constexpr int kDirectWaves = 4, kDirectThreads = 64 * kDirectWaves, kDirectRows = 16;
+
+// Per wave: a block's key scales, offsets and scalars, then its value scales and
+// offsets, or (fp16 tokens) its values transposed, [D][kVtPitch].
+constexpr int kVtPitch = 40;  // halves
+
+__host__ __device__ constexpr int direct_region(int D, bool fp16)
+{
+    return meta_bytes(D) + (fp16 ? 2 * kVtPitch * D : stage_bytes(D));
+}
+
+__host__ __device__ constexpr int direct_lds(int D, bool fp16)
+{
+    const int walk = kDirectWaves * direct_region(D, fp16), merge = kDirectWaves * 16 * (D + 2) * 4;
     return walk > merge ? walk : merge;
 }
 
@@ -242,16 +269,16 @@ __device__ __forceinline__ half8 centred(const uint32_t* w, int k, uint32_t cent
     return __builtin_bit_cast(half8, v);
 }
 
-// The loads of one wave's part of a coded block: four key pieces and four
-// value pieces per lane, and chunk `lane` (four numbers) of the block's key and
-// of its value scales and offsets.
-template <int KB, int VB, bool M16>
+// The loads of one wave's part of a coded block: NK key pieces and NV value
+// pieces per lane, and chunk `lane` (four numbers) of the block's key and of
+// its value scales and offsets.
+template <int KB, int VB, int NK, int NV>
 struct Raw {
-    uint32_t k[KB], v[VB];  // 4 pieces of KB / 4 words
+    uint32_t k[NK * KB / 4], v[NV * VB / 4];
     u32x4 ks, kz, vs, vz;
 };
 
-// N bytes (4 to 32, naturally aligned) from global memory, streaming.
+// N bytes (4 to 128, aligned to N or 16) from global memory, streaming.
 template <int N>
 __device__ __forceinline__ void load_bytes(const uint8_t* at, uint32_t* w)
 {
@@ -272,10 +299,11 @@ __device__ __forceinline__ void load_bytes(const uint8_t* at, uint32_t* w)
     }
 }
 
-// The builder's view of a segment's unit: a wave's part of its images.
-template <int D, bool KH, int KB, int VB, bool M16>
+// Conversion of a segment's unit: part `part` of PB of every block.
+template <int D, bool KH, int KB, int VB, bool M16, int PB>
 struct Builder {
-    static constexpr int NKB = D / 32, NMB = D / 16, PB = parts(D);
+    static constexpr int NKB = D / 32, NMB = D / 16, NK = 2 * NKB / PB, NV = NMB / PB;
+    typedef Raw<KB, VB, NK, NV> Loads;
     const AttnParams& p;
     int unit, part, lane;
     int nkc, nvc;      // chunks of a block's key and value scales
@@ -283,9 +311,9 @@ struct Builder {
     const uint8_t *k, *v, *ks, *vs;  // this lane's pieces and chunks of block 0
     long dkz, dvz;                   // offsets - scales (0 when symmetric: the scales once more)
 
-    // piece i of the lane: half block and 32-channel block
-    __device__ __forceinline__ int half(int i) const { return PB == 1 ? i >> 1 : PB == 2 ? part : part >> 1; }
-    __device__ __forceinline__ int kblock(int i) const { return PB == 1 ? i & 1 : PB == 2 ? i : 4 * (part & 1) + i; }
+    // key piece i of the lane: half block and 32-channel block
+    __device__ __forceinline__ int half(int i) const { return PB == 1 ? i / NKB : (part * NK + i) / NKB; }
+    __device__ __forceinline__ int kblock(int i) const { return PB == 1 ? i % NKB : (part * NK + i) % NKB; }
 
     __device__ __forceinline__ Builder(const AttnParams& p_, int unit_, int part_, int lane_)
         : p(p_), unit(unit_), part(part_), lane(lane_)
@@ -297,7 +325,7 @@ struct Builder {
         kaff = p.k_mode == KVQ_AFFINE;
         vaff = p.v_mode == KVQ_AFFINE;
         k = (const uint8_t*)p.kc + ((ub0 * 2 + half(0)) * 64 + lane) * (NKB * KB) + kblock(0) * KB;
-        v = (const uint8_t*)p.vc + (ub0 * 64 + lane) * (NMB * VB) + 4 * part * VB;
+        v = (const uint8_t*)p.vc + (ub0 * 64 + lane) * (NMB * VB) + NV * part * VB;
         ks = (const uint8_t*)p.ks + (ub0 * nkc + min(lane, nkc - 1)) * (4 * ESZ);
         vs = (const uint8_t*)p.vs + (ub0 * nvc + min(lane, nvc - 1)) * (4 * ESZ);
         dkz = kaff ? (const uint8_t*)p.kz - (const uint8_t*)p.ks : 0;
@@ -315,17 +343,17 @@ struct Builder {
     }
 
     // Every lane issues the same loads whatever the block.
-    __device__ __forceinline__ void load(Raw<KB, VB, M16>& r, int blk) const
+    __device__ __forceinline__ void load(Loads& r, int blk) const
     {
         constexpr int ESZ = M16 ? 2 : 4;
         const uint8_t* kb = k + (size_t)blk * (2 * 64 * NKB * KB);
         if constexpr (PB == 1) {
-            load_bytes<2 * KB>(kb, r.k);
-            load_bytes<2 * KB>(kb + 64 * NKB * KB, r.k + KB / 2);
+            load_bytes<NKB * KB>(kb, r.k);
+            load_bytes<NKB * KB>(kb + 64 * NKB * KB, r.k + NKB * KB / 4);
         } else {
-            load_bytes<4 * KB>(kb, r.k);
+            load_bytes<NK * KB>(kb, r.k);
         }
-        load_bytes<4 * VB>(v + (size_t)blk * (64 * NMB * VB), r.v);
+        load_bytes<NV * VB>(v + (size_t)blk * (64 * NMB * VB), r.v);
         const uint8_t *a = ks + (size_t)blk * (nkc * 4 * ESZ), *b = vs + (size_t)blk * (nvc * 4 * ESZ);
         r.ks = load_chunk(a);
         r.kz = load_chunk(a + dkz);
@@ -348,177 +376,219 @@ struct Builder {
         }
     }
 
-    // This wave's part of the image of a coded block whose first `live` tokens
-    // exist.  img: the image; meta: its scales; st: this wave's stage.
-    __device__ __forceinline__ void coded_image(const Raw<KB, VB, M16>& r, int live, uint8_t* img, float* meta,
-                                                float* st) const
+    // A chunk pair times f to st (scales) and st + D (offsets).
+    __device__ __forceinline__ void put_chunk(float* st, const float* sv, const float* zv, float f) const
     {
-        const int qg = lane >> 4;
-        // ---- keys
-        const Coding kc = coding<KB>(kaff);
-        float ksv[4], kzv[4], kf = 1.0f;
-        widen(r.ks, r.kz, kaff, kc.mid, live, KH, ksv, kzv);
-        if constexpr (KH) {
-            // times a power of two that brings the block's keys to 2^12 at most:
-            // hi + lo then holds them to 2^-37 of the largest
-            float top = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                top = fmaxf(top, fmaf(kc.mid, ksv[e], fabsf(kzv[e])));
-            kf = scale_to_range(wave_max(lane < nkc ? top : 0.0f));
-            // channel c: scale at st[c], offset at st[D + c]
-            if (lane < nkc) {
-                *(float4*)(st + 4 * lane) = float4{ksv[0] * kf, ksv[1] * kf, ksv[2] * kf, ksv[3] * kf};
-                *(float4*)(st + D + 4 * lane) = float4{kzv[0] * kf, kzv[1] * kf, kzv[2] * kf, kzv[3] * kf};
-            }
-            lds_order();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int kb = kblock(i);
-                const float* s = st + 32 * kb + 8 * qg;
-                const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
-                const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
-                const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-                const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
-                const half8 a = centred<KB>(r.k, i, kc.centre);
-                float x[8];
-                half8 hi, lo;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = fmaf((float)a[j], sn[perm4(j)], zn[perm4(j)]);
-                split_nearest(x, &hi, &lo);
-                uint8_t* at = img + 1024 * (half(i) * NKB + kb) + 16 * lane;
-                *(half8*)at = hi;
-                *(half8*)(at + 64 * D) = lo;
-            }
-            lds_order();
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(half8*)(img + 1024 * (half(i) * NKB + kblock(i)) + 16 * lane) = centred<KB>(r.k, i, kc.centre);
-            if (part == 0 && lane < nkc) {
-                const float f = p.sm_log2;
-                *(float4*)(meta + 4 * lane) = float4{ksv[0] * f, ksv[1] * f, ksv[2] * f, ksv[3] * f};
-                *(float4*)(meta + D + 4 * lane) = float4{kzv[0] * f, kzv[1] * f, kzv[2] * f, kzv[3] * f};
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);  // (the registers of one side at a time)
-        // ---- values, likewise; group g's scales at st[32 g], offsets at st[D + 32 g]
-        const Coding vc = coding<VB>(vaff);
-        float vsv[4], vzv[4], top = 0.0f;
-        widen(r.vs, r.vz, vaff, vc.mid, live, false, vsv, vzv);
+        *(float4*)(st + 4 * lane) = float4{sv[0] * f, sv[1] * f, sv[2] * f, sv[3] * f};
+        *(float4*)(st + D + 4 * lane) = float4{zv[0] * f, zv[1] * f, zv[2] * f, zv[3] * f};
+    }
+
+    // A power of two that brings the block's largest magnitude |offset| + mid
+    // scale to 2^12 at most: hi + lo then holds every element to 2^-37 of it.
+    __device__ __forceinline__ float range_scale(const float* sv, const float* zv, float mid, int n) const
+    {
+        float top = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            top = fmaxf(top, fmaf(vc.mid, vsv[e], fabsf(vzv[e])));
-        const float vf = scale_to_range(wave_max(lane < nvc ? top : 0.0f));
-        if (lane < nvc) {
-            *(float4*)(st + 4 * lane) = float4{vsv[0] * vf, vsv[1] * vf, vsv[2] * vf, vsv[3] * vf};
-            *(float4*)(st + D + 4 * lane) = float4{vzv[0] * vf, vzv[1] * vf, vzv[2] * vf, vzv[3] * vf};
-        }
-        lds_order();
-        const int lg = 31 - __builtin_clz(p.v_group);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int mb = 4 * part + i;
-            const float* s = st + 32 * (16 * mb >> lg) + 8 * qg;
-            const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
-            const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
-            const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-            const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
-            const half8 c = centred<VB>(r.v, i, vc.centre);
-            float x[8];
-            half8 hi, lo;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                x[j] = fmaf((float)c[j], sn[perm4(j)], zn[perm4(j)]);
-            split_nearest(x, &hi, &lo);
-            uint8_t* at = img + key_bytes(D, KH) + 1024 * mb + 16 * lane;
-            *(half8*)at = hi;
-            *(half8*)(at + 64 * D) = lo;
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (part == 0 && lane == 0) {
-            meta[2 * D] = vf;
-            meta[2 * D + 1] = KH ? p.sm_log2 * (1.0f / kf) : 0.0f;
+            top = fmaxf(top, fmaf(mid, sv[e], fabsf(zv[e])));
+        return scale_to_range(wave_max(lane < n ? top : 0.0f));
+    }
+
+    // The key scales of a coded block: per-token groups (times sm_scale log2 e) to
+    // meta, [group][32] scales and offsets; per-channel ones to st, [channel].
+    // Returns what the scores of reconstructed keys take.
+    __device__ __forceinline__ float key_scales(const Loads& r, int live, float* meta, float* st) const
+    {
+        float sv[4], zv[4];
+        const float mid = coding<KB>(kaff).mid;
+        widen(r.ks, r.kz, kaff, mid, live, KH, sv, zv);
+        if constexpr (KH) {
+            const float f = range_scale(sv, zv, mid, nkc);
+            if (lane < nkc)
+                put_chunk(st, sv, zv, f);
+            return p.sm_log2 * (1.0f / f);
+        } else {
+            if (part == 0 && lane < nkc)
+                put_chunk(meta, sv, zv, p.sm_log2);
+            return 0.0f;
         }
     }
 
-    // This wave's part of the image of a block of fp16 rows: token i is row
-    // (first + i) % ring of kr, vr [.][D], the first `live` exist.
+    // The value scales of a coded block to st, [group][32]; returns the power of
+    // two that they were multiplied with.
+    __device__ __forceinline__ float value_scales(const Loads& r, int live, float* st) const
+    {
+        float sv[4], zv[4];
+        const float mid = coding<VB>(vaff).mid;
+        widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
+        const float f = range_scale(sv, zv, mid, nvc);
+        if (lane < nvc)
+            put_chunk(st, sv, zv, f);
+        return f;
+    }
+
+    // Eight reconstructed elements of the codes' operand a, hi + lo; s: their
+    // scales (natural order), offsets D further.
+    static __device__ __forceinline__ void reconstruct(const half8& a, const float* s, half8* hi, half8* lo)
+    {
+        const float4 s0 = *(const float4*)s, s1 = *(const float4*)(s + 4);
+        const float4 z0 = *(const float4*)(s + D), z1 = *(const float4*)(s + D + 4);
+        const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+        const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            x[j] = fmaf((float)a[j], sn[perm4(j)], zn[perm4(j)]);
+        split_nearest(x, hi, lo);
+    }
+
+    // Key piece i: the codes (lo untouched), or the reconstructed keys.
+    __device__ __forceinline__ void key_piece(const Loads& r, int i, const float* st, half8* hi, half8* lo) const
+    {
+        const half8 a = centred<KB>(r.k, i, coding<KB>(kaff).centre);
+        if constexpr (KH)
+            reconstruct(a, st + 32 * kblock(i) + 8 * (lane >> 4), hi, lo);
+        else
+            *hi = a;
+    }
+
+    // Value piece i (channels 16 (NV part + i) + lane % 16).
+    __device__ __forceinline__ void value_piece(const Loads& r, int i, const float* st, half8* hi, half8* lo) const
+    {
+        const int g = 16 * (NV * part + i) >> (31 - __builtin_clz(p.v_group));
+        reconstruct(centred<VB>(r.v, i, coding<VB>(vaff).centre), st + 32 * g + 8 * (lane >> 4), hi, lo);
+    }
+
+    // This wave's part of the image of a coded block whose first `live` tokens
+    // exist.  img: the image; meta: its scales; st: this wave's stage.
+    __device__ __forceinline__ void coded_image(const Loads& r, int live, uint8_t* img, float* meta, float* st) const
+    {
+        const float ksm = key_scales(r, live, meta, st);
+        lds_order();
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            half8 hi, lo;
+            key_piece(r, i, st, &hi, &lo);
+            uint8_t* at = img + 1024 * (half(i) * NKB + kblock(i)) + 16 * lane;
+            *(half8*)at = hi;
+            if constexpr (KH)
+                *(half8*)(at + 64 * D) = lo;
+        }
+        lds_order();
+        const float vf = value_scales(r, live, st);
+        lds_order();
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            half8 hi, lo;
+            value_piece(r, i, st, &hi, &lo);
+            uint8_t* at = img + key_bytes(D, KH) + 1024 * (NV * part + i) + 16 * lane;
+            *(half8*)at = hi;
+            *(half8*)(at + 64 * D) = lo;
+        }
+        if (part == 0 && lane == 0) {
+            meta[2 * D] = vf;
+            meta[2 * D + 1] = ksm;
+        }
+    }
+
+    // ---- Blocks of fp16 rows: token i is row (first + i) % ring of kr, vr [.][D],
+    // the first `live` exist.  (Dead tokens read a live row and are cleared: no
+    // load waits for a branch.)
+    __device__ __forceinline__ int key_token(int i) const { return 8 * ((lane & 15) >> 2) + 4 * half(i) + (lane & 3); }
+
+    __device__ __forceinline__ u32x4 load_key_row(const uint16_t* kr, int first, int ring, int live, int i) const
+    {
+        const int t = min(key_token(i), live - 1);
+        return *(const u32x4*)(kr + (uint32_t)((first + t) % ring * D + 32 * kblock(i) + 8 * (lane >> 4)));
+    }
+
+    __device__ __forceinline__ half8 key_row_piece(const u32x4& w, int live, int i) const
+    {
+        const bool on = key_token(i) < live;
+        u32x4 a;  // dword j: channels j and j + 4
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = w[j >> 1], y = w[2 + (j >> 1)];
+            a[j] = !on ? 0u : j & 1 ? (x >> 16) | (y & 0xFFFF0000u) : (x & 0xFFFFu) | (y << 16);
+        }
+        return __builtin_bit_cast(half8, a);
+    }
+
+    // Element offsets of this lane's eight tokens (operand order) in vr.
+    __device__ __forceinline__ void value_rows(int first, int ring, int live, uint32_t* row) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            row[j] = (uint32_t)((first + min(8 * (lane >> 4) + perm4(j), live - 1)) % ring * D + (lane & 15));
+    }
+
+    __device__ __forceinline__ half8 value_row_piece(const uint16_t* vr, const uint32_t* row, int live, int i) const
+    {
+        uint16_t h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            h[j] = vr[row[j] + 16 * (NV * part + i)];
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = 8 * (lane >> 4) + j < live ? h[2 * j] : 0u;
+            w[j] |= 8 * (lane >> 4) + j + 4 < live ? (uint32_t)h[2 * j + 1] << 16 : 0u;
+        }
+        return __builtin_bit_cast(half8, w);
+    }
+
+    // The scales of fp16 rows: ones (times the softmax scale for code operands).
+    __device__ __forceinline__ void row_scales(float* meta) const
+    {
+        if (part != 0)
+            return;
+        if (!KH && lane < nkc) {
+            const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f}, none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            put_chunk(meta, one, none, p.sm_log2);
+        }
+        if (lane == 0) {
+            meta[2 * D] = 1.0f;
+            meta[2 * D + 1] = p.sm_log2;
+        }
+    }
+
     __device__ __forceinline__ void rows_image(const uint16_t* kr, const uint16_t* vr, int first, int ring, int live,
                                                uint8_t* img, float* meta) const
     {
-        const int qg = lane >> 4, hh = lane & 15;
         const half8 zero = {};
-        // (dead tokens read a live row and are cleared: no load waits for a branch)
-        u32x4 kw[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = min(8 * (hh >> 2) + 4 * half(i) + (hh & 3), live - 1);
-            kw[i] = *(const u32x4*)(kr + (uint32_t)((first + t) % ring * D + 32 * kblock(i) + 8 * qg));
-        }
-        uint32_t row[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            row[j] = (first + min(8 * qg + perm4(j), live - 1)) % ring * D + 64 * part + hh;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool on = 8 * (hh >> 2) + 4 * half(i) + (hh & 3) < live;
-            u32x4 a;  // dword j: channels j and j + 4
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t x = kw[i][j >> 1], y = kw[i][2 + (j >> 1)];
-                a[j] = !on ? 0u : j & 1 ? (x >> 16) | (y & 0xFFFF0000u) : (x & 0xFFFFu) | (y << 16);
-            }
+        for (int i = 0; i < NK; ++i) {
             uint8_t* at = img + 1024 * (half(i) * NKB + kblock(i)) + 16 * lane;
-            *(u32x4*)at = a;
+            *(half8*)at = key_row_piece(load_key_row(kr, first, ring, live, i), live, i);
             if constexpr (KH)
                 *(half8*)(at + 64 * D) = zero;
         }
-        __builtin_amdgcn_sched_barrier(0);
+        uint32_t row[8];
+        value_rows(first, ring, live, row);
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            uint16_t h[2][8];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    h[u][j] = vr[row[j] + 16 * (i + u)];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                u32x4 w;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    w[j] = 8 * qg + j < live ? h[u][2 * j] : 0u;
-                    w[j] |= 8 * qg + j + 4 < live ? (uint32_t)h[u][2 * j + 1] << 16 : 0u;
-                }
-                uint8_t* at = img + key_bytes(D, KH) + 1024 * (4 * part + i + u) + 16 * lane;
-                *(u32x4*)at = w;
-                *(half8*)(at + 64 * D) = zero;
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < NV; ++i) {
+            uint8_t* at = img + key_bytes(D, KH) + 1024 * (NV * part + i) + 16 * lane;
+            *(half8*)at = value_row_piece(vr, row, live, i);
+            *(half8*)(at + 64 * D) = zero;
         }
-        if (part == 0) {
-            if (!KH && lane < nkc) {
-                const float f = p.sm_log2;
-                *(float4*)(meta + 4 * lane) = float4{f, f, f, f};
-                *(float4*)(meta + D + 4 * lane) = float4{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-            if (lane == 0) {
-                meta[2 * D] = 1.0f;
-                meta[2 * D + 1] = p.sm_log2;
-            }
-        }
+        row_scales(meta);
     }
 };
 
 // ------------------------------------------------------------ rows
 
+template <bool ORDER>
+__device__ __forceinline__ void piece_end()
+{
+    if constexpr (ORDER)
+        __builtin_amdgcn_sched_barrier(0);
+}
+
 // A wave's state: NT tiles of 16 query rows (columns of the MFMAs).  KG: key
 // group size / 32 (0: reconstructed keys, hi + lo).  ROT: rotated queries, hi + lo.
-template <int D, int KG, bool ROT>
+template <int D, int KG, bool ROT, int CT>
 struct Rows {
-    static constexpr int CT = tiles(D), NKB = D / 32, NMB = D / 16;
+    static constexpr int NKB = D / 32, NMB = D / 16;
     static constexpr bool KH = KG == 0;
     static constexpr int KS = KH ? NKB : KG, NG = NKB / KS, NZ = (NG + 3) / 4;
     half8 q[CT][NKB], ql[ROT ? CT : 1][ROT ? NKB : 1];
@@ -622,15 +692,18 @@ struct Rows {
         }
     }
 
-    // One image: tokens t0 .. t0 + 31 (tail indices; with `off` = the sink's size
-    // for sink blocks), the first `live` of which exist.
-    template <int NT>
-    __device__ __forceinline__ void consume(const uint8_t* img, const float* meta, int t0, int off, int live, int lane)
+    // One block: tokens t0 .. t0 + 31 (tail indices; with `off` = the sink's size
+    // for sink blocks), the first `live` of which exist.  key(e, kb, hi, lo) and
+    // value(mb, hi, lo) give its operands, meta its key scales; f is the values'
+    // power of two, ksm what the scores of reconstructed keys take.  LO: the
+    // operands have lo halves.  ORDER: one operand at a time (converted ones
+    // would otherwise all be made ahead of their products, in registers that
+    // there are not).
+    template <int NT, bool LO, bool ORDER, class Key, class Value>
+    __device__ __forceinline__ void block(Key key, Value value, const float* meta, float f, float ksm, int t0, int off,
+                                          int live, int lane)
     {
         const int qg = lane >> 4, hh = lane & 15;
-        const uint8_t* fb = img + 16 * lane;
-        const auto frag = [&](int at) { return *(const half8*)(fb + at); };
-        const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
         // ---- scores: l[c][4 e + i] is token 8 qg + 4 e + i
         float l[NT][8];
 #pragma unroll
@@ -659,7 +732,8 @@ struct Rows {
 #pragma unroll
                 for (int u = 0; u < KS; ++u) {
                     const int kb = g * KS + u;
-                    const half8 a = frag(1024 * (e * NKB + kb));
+                    half8 a, b;
+                    key(e, kb, &a, &b);
 #pragma unroll
                     for (int c = 0; c < NT; ++c)
                         acc[c] = mfma16(a, q[c][kb], acc[c]);
@@ -668,18 +742,17 @@ struct Rows {
                         for (int c = 0; c < NT; ++c)
                             acc[c] = mfma16(a, ql[c][kb], acc[c]);
                     }
-                    if constexpr (KH) {
-                        const half8 b = frag(64 * D + 1024 * (e * NKB + kb));
+                    if constexpr (KH && LO) {
 #pragma unroll
                         for (int c = 0; c < NT; ++c)
                             acc[c] = mfma16(b, q[c][kb], acc[c]);
                     }
+                    piece_end<ORDER>();
                 }
                 if constexpr (KH) {
-                    const float sm = meta[2 * D + 1];
 #pragma unroll
                     for (int c = 0; c < NT; ++c)
-                        S[c] = acc[c] * sm;
+                        S[c] = acc[c] * ksm;
                 } else {
                     const floatx4 s4 = *(const floatx4*)(meta + 32 * g + 8 * qg + 4 * e);
 #pragma unroll
@@ -754,18 +827,25 @@ struct Rows {
         // ---- values
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb) {
-            const half8 a = frag(key_bytes(D, KH) + 1024 * mb), b = frag(key_bytes(D, KH) + 64 * D + 1024 * mb);
+            half8 a, b;
+            value(mb, &a, &b);
 #pragma unroll
             for (int c = 0; c < NT; ++c)
                 oacc[c][mb] = mfma16(a, ph[c], oacc[c][mb]);
 #pragma unroll
             for (int c = 0; c < NT; ++c)
                 oacc[c][mb] = mfma16(a, pl[c], oacc[c][mb]);
+            if constexpr (LO) {
 #pragma unroll
-            for (int c = 0; c < NT; ++c)
-                oacc[c][mb] = mfma16(b, ph[c], oacc[c][mb]);
+                for (int c = 0; c < NT; ++c)
+                    oacc[c][mb] = mfma16(b, ph[c], oacc[c][mb]);
+            }
+            piece_end<ORDER>();
         }
     }
+
+    // The partial of tile c, unscaled: m, l and this lane's channels 16 mb + 4 qg .. + 3 of row lane % 16.
+    __device__ __forceinline__ float inverse() const { return vf == 0.0f ? 0.0f : 1.0f / vf; }
 };
 
 // ------------------------------------------------------------ work items
@@ -776,15 +856,13 @@ struct Item {
     int seq0;            // first batch sequence of the rows
     int r0, rows;        // first row of the item, rows of the unit
     int split, part;     // range of blocks, and its place among a row's partials
-    int v0, v1;          // blocks v0 .. v1 - 1 (sink blocks first, then the tail's)
     int lim, causal;     // limit of row 0, and whether a row of chunk token c sees c more
 };
 
-__device__ __forceinline__ Item find_item(const SharedParams& p)
+// Item x of a kernel that takes `per` rows per item.
+__device__ __forceinline__ Item find_item(const SharedParams& p, int x, int per)
 {
     Item it;
-    int x = blockIdx.x;
-    const int per = p.tile_rows;
     if (x < p.items0) {
         // prefix: ranges of a tile apart, tiles of a unit next to each other
         const AttnParams& a = p.seg[0];
@@ -827,116 +905,204 @@ __device__ __forceinline__ Item find_item(const SharedParams& p)
     return it;
 }
 
-// Row of O [B][C][H_q][D] (and of Q, and of the partials) of a unit's row r.
+// Row R of O [B][C][H_q][D] (and of Q, and of the partials) of a unit's row r.
 __device__ __forceinline__ size_t global_row(const SharedParams& p, const Item& it, int G, int r)
 {
     const int t = r / G;
     return ((size_t)it.seq0 * p.C + t) * p.H_q + (size_t)it.j * G + (r - t * G);
 }
 
+// The blocks of an item that some of its `left` rows see, in the order sink
+// blocks, coded blocks, window blocks.
+struct Blocks {
+    int v0, v1;  // v0 .. v1 - 1
+    int nsb;     // sink blocks come first; block v is tail block v - nsb after them
+    int ncb;     // coded blocks of the tail
+
+    __device__ __forceinline__ Blocks(const SharedParams& sp, const AttnParams& p, const Item& it, int left)
+    {
+        nsb = (p.n_sink + 31) >> 5;
+        ncb = (p.nq + 31) >> 5;
+        const int top = it.lim + (it.causal ? (it.r0 + left - 1) / p.G : 0);  // the most that a row sees
+        const int nv = min(nsb, (top + p.sink + 31) >> 5) + (top > 0 ? (top + 31) >> 5 : 0);
+        v0 = min(nv, it.split * sp.bps[it.seg]);
+        v1 = min(nv, v0 + sp.bps[it.seg]);
+    }
+
+    __device__ __forceinline__ bool coded(int v) const { return v >= nsb && v - nsb < ncb; }
+    // the coded block nearest to block v of this item
+    __device__ __forceinline__ int nearest(int v) const { return min(max(min(v, v1 - 1) - nsb, 0), ncb - 1); }
+};
+
+// Where fp16 block v's rows are.
+struct RowBlock {
+    const uint16_t *k, *v;
+    int first, ring, live;
+
+    __device__ __forceinline__ RowBlock(const AttnParams& p, int unit, const Blocks& b, int blk, int D)
+    {
+        const bool sink = blk < b.nsb;
+        first = 32 * (sink ? blk : blk - b.nsb);
+        ring = sink ? p.sink : p.ring;
+        live = (sink ? p.n_sink : p.n) - first;
+        const size_t at = (size_t)unit * ring * D;
+        k = (sink ? p.kq : p.kr) + at;
+        v = (sink ? p.vq : p.vr) + at;
+    }
+};
+
+// Block v's first token, what is added to the rows' limits, and its live tokens.
+struct Span {
+    int t0, off, live;
+
+    __device__ __forceinline__ Span(const AttnParams& p, const Blocks& b, int v)
+    {
+        const bool sink = v < b.nsb;
+        t0 = 32 * (sink ? v : v - b.nsb);
+        off = sink ? p.sink : 0;
+        live = (sink ? p.n_sink : p.n) - t0;
+    }
+};
+
+// One row's partial, merged over waves first, first + step, .. of lo [waves][16][D] and
+// lml [waves][16][2] (row r of each), four channels from d.
+template <int D>
+__device__ __forceinline__ void merge_row(const SharedParams& sp, const float* lo, const float* lml, int first, int step,
+                                          int waves, int r, int d, size_t at)
+{
+    float M = kNegInf, L = 0.0f;
+    for (int w = first; w < waves; w += step)
+        M = fmaxf(M, lml[2 * (w * 16 + r)]);
+    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (M != kNegInf) {
+        for (int w = first; w < waves; w += step) {
+            const float2 ml = *(const float2*)(lml + 2 * (w * 16 + r));
+            const float sc = __builtin_amdgcn_exp2f(ml.x - M);
+            acc += *(const floatx4*)(lo + ((size_t)w * 16 + r) * D + d) * sc;
+            L += sc * ml.y;
+        }
+    }
+    *(floatx4*)(sp.part_o + at * D + d) = acc;
+    if (d == 0)
+        *(float2*)(sp.part_ml + 2 * at) = make_float2(M, L);
+}
+
 template <int D, int KG, int KB, int VB, bool M16, bool ROT>
-__global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedParams sp)
+__global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
 {
     constexpr bool KH = KG == 0;
-    constexpr int CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16;
+    constexpr int CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16, NKB = D / 32;
     constexpr int BI = image_bytes(D, KH), BM = meta_bytes(D);
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const Item it = find_item(sp);
+    const Item it = find_item(sp, blockIdx.x, item_rows(D));
     const AttnParams& p = sp.seg[it.seg];
     const int G = p.G, left = min(it.rows - it.r0, item_rows(D));
+    const Blocks bl(sp, p, it, left);
 
-    // ---- this wave's rows and images: R row waves (at least what the images leave)
+    // ---- this wave's part of the images: block v0 + turn NI + own
+    typedef Builder<D, KH, KB, VB, M16, PB> Build;
+    const Build B(p, it.unit, wave % PB, lane);
+    const int own = wave / PB;
+    // (the nearest coded block's loads, fp16 blocks are read when they are
+    // built: without branches, so that nothing waits for them early)
+    const auto prefetch = [&](int v) {
+        typename Build::Loads r;
+        if (bl.ncb > 0)
+            B.load(r, bl.nearest(v));
+        return r;
+    };
+    typename Build::Loads raw = prefetch(bl.v0 + own);
+
+    // ---- this wave's rows and its images of a turn
     const int nt16 = (left + 15) >> 4;
     int R = kWaves / NI;
     while (R * CT < nt16)
         R *= 2;
-    const int rw = wave & (R - 1), bw = wave / R, BW = kWaves / R;
+    const int BW = kWaves / R, rw = wave / BW, bw = wave - rw * BW;
     const int nt = nt16 > rw ? (nt16 - rw + R - 1) / R : 0;  // tiles rw, rw + R, ..
-    Rows<D, KG, ROT> T;
-    T.init();
+    Rows<D, KG, ROT, CT> T;
     T.lim0 = it.lim + (it.causal ? (it.r0 + 16 * rw) / G : 0);
     {
         const int last = min(left, 16 * (rw + R * (nt - 1)) + 16) - 1;
         T.lim1 = nt > 0 ? it.lim + (it.causal ? (it.r0 + last) / G : 0) : -(1 << 30);
     }
-
-    // ---- the blocks that some row sees: sink blocks, then the tail's
-    const int nsb = (p.n_sink + 31) >> 5;
-    const int top = it.lim + (it.causal ? (it.r0 + left - 1) / G : 0);  // the most that a row sees
-    const int nv = min(nsb, (top + p.sink + 31) >> 5) + (top > 0 ? (top + 31) >> 5 : 0);
-    const int v0 = min(nv, it.split * sp.bps[it.seg]), v1 = min(nv, v0 + sp.bps[it.seg]);
-    const Builder<D, KH, KB, VB, M16> B(p, it.unit, wave % PB, lane);
-    const int own = wave / PB;  // the image of a phase that this wave builds
-    // Block v's loads, or of the nearest coded block (fp16 blocks are read when
-    // they are built): without branches, so that nothing waits for them early.
-    const int ncb = (p.nq + 31) >> 5;
-    const auto prefetch = [&](int v) {
-        Raw<KB, VB, M16> r;
-        if (ncb > 0)
-            B.load(r, min(max(min(v, v1 - 1) - nsb, 0), ncb - 1));
-        return r;
-    };
-    Raw<KB, VB, M16> raw = prefetch(v0 + own);
-
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int r = 16 * (rw + R * c) + hh, rc = min(r, left - 1);
+        const int rc = min(16 * (rw + R * c) + hh, left - 1);
         T.lim[c] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
         T.load_query(c, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
     }
 
-    uint8_t* metas = lds + NI * BI;
-    float* st = (float*)(metas + NI * BM + kStage * wave);
+    T.init();
+    uint8_t* metas = lds + 2 * NI * BI;
+    float* st = (float*)(metas + 2 * NI * BM + stage_bytes(D) * wave);
+    const auto build = [&](int v, int buf) __attribute__((always_inline)) {  // the turn that starts at block v
+        const int mine = v + own;
+        if (mine < bl.v1) {
+            uint8_t* img = lds + (buf * NI + own) * BI;
+            float* meta = (float*)(metas + (buf * NI + own) * BM);
+            if (bl.coded(mine)) {
+                B.coded_image(raw, min(32, p.nq - 32 * (mine - bl.nsb)), img, meta, st);
+            } else {
+                const RowBlock rb(p, it.unit, bl, mine, D);
+                B.rows_image(rb.k, rb.v, rb.first, rb.ring, rb.live, img, meta);
+            }
+        }
+        raw = prefetch(mine + NI);
+    };
     // (two loops, so that the registers of a wave's tiles have one place in each)
     const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
         constexpr int NT = decltype(tiles_now)::value;
-        for (int v = v0; v < v1; v += NI) {
-            // ---- build
-            const int mine = v + own;
-            if (mine < v1) {
-                uint8_t* img = lds + own * BI;
-                float* meta = (float*)(metas + own * BM);
-                const int tb = mine - nsb;
-                if (tb >= 0 && 32 * tb < p.nq) {
-                    B.coded_image(raw, min(32, p.nq - 32 * tb), img, meta, st);
-                } else {
-                    const bool sink = tb < 0;
-                    const int first = sink ? 32 * mine : 32 * tb, rows = sink ? p.sink : p.ring;
-                    const size_t at = (size_t)it.unit * rows * D;
-                    B.rows_image((sink ? p.kq : p.kr) + at, (sink ? p.vq : p.vr) + at, first, rows,
-                                 (sink ? p.n_sink : p.n) - first, img, meta);
-                }
-            }
-            raw = prefetch(mine + NI);
-            sync_lds();
-            // ---- consume
-            for (int i = bw; i < NI && v + i < v1; i += BW) {
-                const int tb = v + i - nsb;
-                const bool sink = tb < 0;
-                const int t0 = sink ? 32 * (v + i) : 32 * tb, off = sink ? p.sink : 0;
-                if (t0 >= T.lim1 + off)
+        const auto consume = [&](int v, int buf) __attribute__((always_inline)) {
+            for (int i = bw; i < NI && v + i < bl.v1; i += BW) {
+                const Span s(p, bl, v + i);
+                if (s.t0 >= T.lim1 + s.off)
                     continue;
-                const int live = sink ? p.n_sink - t0 : p.n - t0;
-                const uint8_t* img = lds + i * BI;
-                const float* meta = (const float*)(metas + i * BM);
-                T.template consume<NT>(img, meta, t0, off, live, lane);
+                const uint8_t* fb = lds + (buf * NI + i) * BI + 16 * lane;
+                const float* meta = (const float*)(metas + (buf * NI + i) * BM);
+                const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
+                const float ksm = KH ? meta[2 * D + 1] : 0.0f;
+                T.template block<NT, true, false>(
+                    [&](int e, int kb, half8* hi, half8* lo) {
+                        *hi = *(const half8*)(fb + 1024 * (e * NKB + kb));
+                        if constexpr (KH)
+                            *lo = *(const half8*)(fb + 64 * D + 1024 * (e * NKB + kb));
+                    },
+                    [&](int mb, half8* hi, half8* lo) {
+                        *hi = *(const half8*)(fb + key_bytes(D, KH) + 1024 * mb);
+                        *lo = *(const half8*)(fb + key_bytes(D, KH) + 64 * D + 1024 * mb);
+                    },
+                    meta, f, ksm, s.t0, s.off, s.live, lane);
             }
+        };
+        const bool late = wave >= kWaves / 2;
+        int buf = 0;
+        for (int v = bl.v0; v < bl.v1; v += NI, buf ^= 1) {
+            if (!late)
+                build(v + NI, buf ^ 1);
+            consume(v, buf);
+            if (late)
+                build(v + NI, buf ^ 1);
             sync_lds();
         }
     };
+    build(bl.v0, 0);
+    sync_lds();
     if (CT == 1 || nt <= 1)
         walk(std::integral_constant<int, 1>{});
     else
         walk(std::integral_constant<int, CT>{});
 
     // ---- partials: of each wave when its rows are its own, else merged in LDS
-    const float inv = T.vf == 0.0f ? 0.0f : 1.0f / T.vf;
+    const float inv = T.inverse();
     float* lo = (float*)lds;              // [waves][16][D]
     float* lml = lo + kWaves * 16 * D;    // [waves][16][2]
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
+        if (R * c >= nt16)
+            break;
         const float l = sum_rows(T.lsum[c]);
         const int r = 16 * (rw + R * c) + hh;
         if (BW == 1) {
@@ -959,60 +1125,158 @@ __global__ __launch_bounds__(kThreads, 2) void shared_kernel(SharedParams sp)
             *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
         sync_lds();
         for (int idx = threadIdx.x; idx < 16 * R * (D / 4); idx += kThreads) {
-            const int row = idx / (D / 4), d = 4 * (idx % (D / 4)), w0 = row >> 4, rr = 16 * (w0 + R * c) + (row & 15);
-            if (rr >= left)
-                continue;
-            float M = kNegInf;
-            for (int w = w0; w < kWaves; w += R)
-                M = fmaxf(M, lml[2 * (w * 16 + (row & 15))]);
-            floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-            float L = 0.0f;
-            if (M != kNegInf) {
-                for (int w = w0; w < kWaves; w += R) {
-                    const float2 ml = *(const float2*)(lml + 2 * (w * 16 + (row & 15)));
-                    const float sc = __builtin_amdgcn_exp2f(ml.x - M);
-                    acc += *(const floatx4*)(lo + ((size_t)w * 16 + (row & 15)) * D + d) * sc;
-                    L += sc * ml.y;
-                }
-            }
-            const size_t at = (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + rr);
-            *(floatx4*)(sp.part_o + at * D + d) = acc;
-            if (d == 0)
-                *(float2*)(sp.part_ml + 2 * at) = make_float2(M, L);
+            const int row = idx / (D / 4), d = 4 * (idx % (D / 4)), w = row >> 4, rr = 16 * (w + R * c) + (row & 15);
+            if (rr < left)
+                merge_row<D>(sp, lo, lml, w * BW, 1, w * BW + BW, row & 15, d,
+                             (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + rr));
         }
     }
 }
 
-template <int D, int KG, int KB, int VB, bool M16, bool ROT>
-hipError_t launch_instance(const SharedParams& p, int items, hipStream_t stream)
+// Waves per SIMD that the registers are held to.
+__host__ __device__ constexpr int direct_waves(int D)
 {
-    launch_kernel(shared_kernel<D, KG, KB, VB, M16, ROT>, dim3(items), dim3(kThreads), (size_t)lds_bytes(D, KG == 0),
-                  stream, p);
+    return D == 64 ? 3 : 2;
+}
+
+template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+__global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
+{
+    constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves;
+    constexpr bool kAhead = D < 256;  // (two blocks' loads do not fit the registers of the widest heads)
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const Item it = find_item(sp, blockIdx.x + sp.direct0, kDirectRows);
+    const AttnParams& p = sp.seg[it.seg];
+    const int G = p.G, left = min(it.rows - it.r0, kDirectRows);
+    const Blocks bl(sp, p, it, left);
+
+    typedef Builder<D, KG == 0, KB, VB, M16, 1> Build;
+    const Build B(p, it.unit, 0, lane);
+    const auto prefetch = [&](int v) {
+        typename Build::Loads r;
+        if (bl.ncb > 0)
+            B.load(r, bl.nearest(v));
+        return r;
+    };
+    typename Build::Loads raw = prefetch(bl.v0 + wave);
+    Rows<D, KG, ROT, 1> T;
+    T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
+    {
+        const int rc = min(hh, left - 1);
+        T.lim[0] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
+        T.load_query(0, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
+    }
+    T.init();
+    float* meta = (float*)(lds + wave * direct_region(D, p.ring || p.sink));
+    float* st = meta + meta_bytes(D) / 4;
+    for (int v = bl.v0 + wave; v < bl.v1; v += W) {
+        const Span s(p, bl, v);
+        lds_order();
+        if (bl.coded(v)) {
+            const typename Build::Loads now = raw;
+            if constexpr (kAhead)
+                raw = prefetch(v + W);
+            const int live = min(32, p.nq - s.t0);
+            const float ksm = B.key_scales(now, live, meta, meta), f = B.value_scales(now, live, st);
+            lds_order();
+            T.template block<1, true, true>(
+                [&](int e, int kb, half8* hi, half8* lo) { B.key_piece(now, e * NKB + kb, meta, hi, lo); },
+                [&](int mb, half8* hi, half8* lo) { B.value_piece(now, mb, st, hi, lo); }, meta, f, ksm, s.t0, s.off,
+                s.live, lane);
+            if constexpr (!kAhead)
+                raw = prefetch(v + W);
+        } else {
+            const RowBlock rb(p, it.unit, bl, v, D);
+            // all loads first (at D = 256 the keys' after the values')
+            constexpr int NV = D / 16;
+            u32x4 kw[2 * NKB], vw[NV];
+            const auto load_keys = [&] {
+#pragma unroll
+                for (int i = 0; i < 2 * NKB; ++i)
+                    kw[i] = B.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
+            };
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int idx = lane + 64 * i, r = idx / (D / 8), c8 = 8 * (idx % (D / 8));
+                vw[i] = *(const u32x4*)(rb.v + (uint32_t)((rb.first + min(r, rb.live - 1)) % rb.ring * D + c8));
+            }
+            if constexpr (D < 256)
+                load_keys();
+            B.row_scales(meta);
+            uint16_t* vt = (uint16_t*)st;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int idx = lane + 64 * i, r = idx / (D / 8), c8 = 8 * (idx % (D / 8));
+                const int e = r & 7, pos = (r & ~7) + (e < 4 ? 2 * e : 2 * (e - 4) + 1);  // operand slot of token r
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    vt[(c8 + j) * kVtPitch + pos] = r < rb.live ? (uint16_t)(vw[i][j >> 1] >> (16 * (j & 1))) : (uint16_t)0;
+            }
+            if constexpr (D == 256)
+                load_keys();
+            lds_order();
+            T.template block<1, false, true>(
+                [&](int e, int kb, half8* hi, half8*) { *hi = B.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); },
+                [&](int mb, half8* hi, half8*) { *hi = *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, meta,
+                1.0f, p.sm_log2, s.t0, s.off, s.live, lane);
+            raw = prefetch(v + W);
+        }
+    }
+
+    // ---- the waves' partials merged
+    const float inv = T.inverse(), l = sum_rows(T.lsum[0]);
+    float* lo = (float*)lds;
+    float* lml = lo + W * 16 * D;
+    __syncthreads();
+    if (hh < left) {
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+            *(floatx4*)(lo + ((size_t)wave * 16 + hh) * D + 16 * mb + 4 * qg) = T.oacc[0][mb] * inv;
+        if (qg == 0)
+            *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[0], l);
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < left * (D / 4); idx += kDirectThreads) {
+        const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
+        merge_row<D>(sp, lo, lml, 0, 1, W, r, d, (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + r));
+    }
+}
+
+// Items [0, image_items) by the image kernel, then direct_items by the direct one.
+template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
+{
+    if (p.image_items > 0)
+        launch_kernel(image_kernel<D, KG, KB, VB, M16, ROT>, dim3(p.image_items), dim3(kThreads),
+                      (size_t)image_lds(D, KG == 0), stream, p);
+    if (p.direct_items > 0)
+        launch_kernel(direct_kernel<D, KG, KB, VB, M16, ROT>, dim3(p.direct_items), dim3(kDirectThreads),
+                      (size_t)direct_lds(D, p.seg[0].ring > 0 || p.seg[0].sink > 0), stream, p);
     return hipGetLastError();
 }
 
 template <int D, int KG, bool M16, bool ROT>
-hipError_t launch_widths(const SharedParams& p, int items, hipStream_t stream)
+hipError_t launch_widths(const SharedParams& p, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
     if (a.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
-        return launch_instance<D, KG, 8, 8, M16, ROT>(p, items, stream);
+        return launch_instance<D, KG, 8, 8, M16, ROT>(p, stream);
     if (a.k_bits == 4)
-        return a.v_bits == 4 ? launch_instance<D, KG, 4, 4, M16, ROT>(p, items, stream)
-                             : launch_instance<D, KG, 4, 2, M16, ROT>(p, items, stream);
-    return a.v_bits == 4 ? launch_instance<D, KG, 2, 4, M16, ROT>(p, items, stream)
-                         : launch_instance<D, KG, 2, 2, M16, ROT>(p, items, stream);
+        return a.v_bits == 4 ? launch_instance<D, KG, 4, 4, M16, ROT>(p, stream)
+                             : launch_instance<D, KG, 4, 2, M16, ROT>(p, stream);
+    return a.v_bits == 4 ? launch_instance<D, KG, 2, 4, M16, ROT>(p, stream)
+                         : launch_instance<D, KG, 2, 2, M16, ROT>(p, stream);
 }
 
 // The kernels of one head size and key grouping.
 template <int D, int KG>
-hipError_t launch_family(const SharedParams& p, int items, hipStream_t stream)
+hipError_t launch_family(const SharedParams& p, hipStream_t stream)
 {
     if (p.rotate)
-        return p.seg[0].meta16 ? launch_widths<D, KG, true, true>(p, items, stream)
-                               : launch_widths<D, KG, false, true>(p, items, stream);
-    return p.seg[0].meta16 ? launch_widths<D, KG, true, false>(p, items, stream)
-                           : launch_widths<D, KG, false, false>(p, items, stream);
+        return p.seg[0].meta16 ? launch_widths<D, KG, true, true>(p, stream) : launch_widths<D, KG, false, true>(p, stream);
+    return p.seg[0].meta16 ? launch_widths<D, KG, true, false>(p, stream) : launch_widths<D, KG, false, false>(p, stream);
 }
 
 }  // namespace shr

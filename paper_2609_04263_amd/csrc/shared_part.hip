@@ -12,9 +12,9 @@
 
 namespace kvq {
 
-hipError_t KVQ_CAT(launch_shared, KVQ_PART_D, KVQ_PART_KG)(const SharedParams& p, int items, hipStream_t stream)
+hipError_t KVQ_CAT(launch_shared, KVQ_PART_D, KVQ_PART_KG)(const SharedParams& p, hipStream_t stream)
 {
-    return shr::launch_family<KVQ_PART_D, KVQ_PART_KG>(p, items, stream);
+    return shr::launch_family<KVQ_PART_D, KVQ_PART_KG>(p, stream);
 }
 
 }  // namespace kvq
