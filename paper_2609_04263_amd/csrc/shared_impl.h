@@ -761,6 +761,7 @@ struct Rows {
                         for (int i = 0; i < 4; ++i)
                             S[c][i] = fmaf(s4[i], acc[c][i], S[c][i]);
                 }
+                piece_end<(NG >= 4)>();  // (the sums of many groups side by side spill)
             }
 #pragma unroll
             for (int c = 0; c < NT; ++c)
@@ -987,7 +988,9 @@ __device__ __forceinline__ void merge_row(const SharedParams& sp, const float* l
         *(float2*)(sp.part_ml + 2 * at) = make_float2(M, L);
 }
 
-template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+// ROWS: the format has fp16 tokens (their conversion in the loop costs the other
+// formats registers that the loop spills).
+template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
 {
     constexpr bool KH = KG == 0;
@@ -1009,7 +1012,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     // built: without branches, so that nothing waits for them early)
     const auto prefetch = [&](int v) {
         typename Build::Loads r;
-        if (bl.ncb > 0)
+        if (!ROWS || bl.ncb > 0)
             B.load(r, bl.nearest(v));
         return r;
     };
@@ -1043,7 +1046,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
         if (mine < bl.v1) {
             uint8_t* img = lds + (buf * NI + own) * BI;
             float* meta = (float*)(metas + (buf * NI + own) * BM);
-            if (bl.coded(mine)) {
+            if (!ROWS || bl.coded(mine)) {
                 B.coded_image(raw, min(32, p.nq - 32 * (mine - bl.nsb)), img, meta, st);
             } else {
                 const RowBlock rb(p, it.unit, bl, mine, D);
@@ -1248,12 +1251,16 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
 template <int D, int KG, int KB, int VB, bool M16, bool ROT>
 hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
 {
-    if (p.image_items > 0)
-        launch_kernel(image_kernel<D, KG, KB, VB, M16, ROT>, dim3(p.image_items), dim3(kThreads),
-                      (size_t)image_lds(D, KG == 0), stream, p);
+    const bool rows = p.seg[0].ring > 0 || p.seg[0].sink > 0;
+    if (p.image_items > 0) {
+        // (per-channel keys come with a window)
+        constexpr bool kWindow = KG == 0;
+        launch_kernel(rows ? image_kernel<D, KG, KB, VB, M16, ROT, true> : image_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
+                      dim3(p.image_items), dim3(kThreads), (size_t)image_lds(D, KG == 0), stream, p);
+    }
     if (p.direct_items > 0)
         launch_kernel(direct_kernel<D, KG, KB, VB, M16, ROT>, dim3(p.direct_items), dim3(kDirectThreads),
-                      (size_t)direct_lds(D, p.seg[0].ring > 0 || p.seg[0].sink > 0), stream, p);
+                      (size_t)direct_lds(D, rows), stream, p);
     return hipGetLastError();
 }
 
