@@ -15,13 +15,13 @@
 //
 //   image_kernel   more than 16 rows per unit.  Eight waves, two per SIMD; up to
 //                  128 tiles(D) rows.  In turns, the waves convert the next
-//                  kImages blocks into images in LDS (kParts waves per block)
-//                  and multiply their own rows with the present ones (two
-//                  buffers, one barrier per turn; the two waves of a SIMD take
-//                  the halves of a turn in opposite order, so that one's
-//                  matrix products run beside the other's conversions).  With
-//                  R row waves a wave has up to tiles(D) tiles of 16 rows and
-//                  every kWaves / R-th image.
+//                  images(D) blocks into images in LDS (parts(D) waves per
+//                  block), then multiply their own rows with them.  With R row
+//                  waves a wave has up to tiles(D) tiles of 16 rows and every
+//                  kWaves / R-th image.  (Two buffers with one barrier per turn
+//                  leave room for half the images, and every wave that takes
+//                  part in a block repeats the work on its scales: 3 to 15%
+//                  slower, in either order of the halves.)
 //   direct_kernel  at most 16 rows per unit (a suffix's queries, few samples):
 //                  four waves, each with blocks of its own, converts codes
 //                  into operands in registers.
@@ -77,11 +77,11 @@ __host__ __device__ constexpr int item_rows(int D)
     return 16 * tiles(D) * kWaves;
 }
 
-// Images of a turn (LDS holds two turns'), and waves that build one: two key
-// and two value pieces per lane.
+// Images of a turn, and waves that build one: four key and four value pieces
+// per lane.
 __host__ __device__ constexpr int images(int D)
 {
-    return 256 / D;
+    return 512 / D;
 }
 
 __host__ __device__ constexpr int parts(int D)
@@ -89,7 +89,7 @@ __host__ __device__ constexpr int parts(int D)
     return kWaves / images(D);
 }
 
-// LDS: two buffers of images, per image its scales and offsets ([group][32]
+// LDS: the images, per image its scales and offsets ([group][32]
 // each) and two scalars, then per wave room to pass a block's scales and
 // offsets between lanes.  The merge of the waves reuses it from the start.
 __host__ __device__ constexpr int key_bytes(int D, bool hilo)
@@ -114,7 +114,7 @@ __host__ __device__ constexpr int stage_bytes(int D)
 
 __host__ __device__ constexpr int image_lds(int D, bool hilo)
 {
-    const int walk = 2 * images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * stage_bytes(D);
+    const int walk = images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * stage_bytes(D);
     const int merge = kWaves * 16 * (D + 2) * 4;
     return walk > merge ? walk : merge;
 }
@@ -408,7 +408,7 @@ struct Builder {
                 put_chunk(st, sv, zv, f);
             return p.sm_log2 * (1.0f / f);
         } else {
-            if (part == 0 && lane < nkc)
+            if (lane < nkc)
                 put_chunk(meta, sv, zv, p.sm_log2);
             return 0.0f;
         }
@@ -463,7 +463,7 @@ struct Builder {
     // exist.  img: the image; meta: its scales; st: this wave's stage.
     __device__ __forceinline__ void coded_image(const Loads& r, int live, uint8_t* img, float* meta, float* st) const
     {
-        const float ksm = key_scales(r, live, meta, st);
+        const float ksm = KH || part == 0 ? key_scales(r, live, meta, st) : 0.0f;
         lds_order();
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
@@ -1039,13 +1039,13 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     }
 
     T.init();
-    uint8_t* metas = lds + 2 * NI * BI;
-    float* st = (float*)(metas + 2 * NI * BM + stage_bytes(D) * wave);
-    const auto build = [&](int v, int buf) __attribute__((always_inline)) {  // the turn that starts at block v
+    uint8_t* metas = lds + NI * BI;
+    float* st = (float*)(metas + NI * BM + stage_bytes(D) * wave);
+    const auto build = [&](int v) __attribute__((always_inline)) {  // the turn that starts at block v
         const int mine = v + own;
         if (mine < bl.v1) {
-            uint8_t* img = lds + (buf * NI + own) * BI;
-            float* meta = (float*)(metas + (buf * NI + own) * BM);
+            uint8_t* img = lds + own * BI;
+            float* meta = (float*)(metas + own * BM);
             if (!ROWS || bl.coded(mine)) {
                 B.coded_image(raw, min(32, p.nq - 32 * (mine - bl.nsb)), img, meta, st);
             } else {
@@ -1058,13 +1058,13 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     // (two loops, so that the registers of a wave's tiles have one place in each)
     const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
         constexpr int NT = decltype(tiles_now)::value;
-        const auto consume = [&](int v, int buf) __attribute__((always_inline)) {
+        const auto consume = [&](int v) __attribute__((always_inline)) {
             for (int i = bw; i < NI && v + i < bl.v1; i += BW) {
                 const Span s(p, bl, v + i);
                 if (s.t0 >= T.lim1 + s.off)
                     continue;
-                const uint8_t* fb = lds + (buf * NI + i) * BI + 16 * lane;
-                const float* meta = (const float*)(metas + (buf * NI + i) * BM);
+                const uint8_t* fb = lds + i * BI + 16 * lane;
+                const float* meta = (const float*)(metas + i * BM);
                 const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
                 const float ksm = KH ? meta[2 * D + 1] : 0.0f;
                 T.template block<NT, true, false>(
@@ -1080,19 +1080,13 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
                     meta, f, ksm, s.t0, s.off, s.live, lane);
             }
         };
-        const bool late = wave >= kWaves / 2;
-        int buf = 0;
-        for (int v = bl.v0; v < bl.v1; v += NI, buf ^= 1) {
-            if (!late)
-                build(v + NI, buf ^ 1);
-            consume(v, buf);
-            if (late)
-                build(v + NI, buf ^ 1);
+        for (int v = bl.v0; v < bl.v1; v += NI) {
+            build(v);
+            sync_lds();
+            consume(v);
             sync_lds();
         }
     };
-    build(bl.v0, 0);
-    sync_lds();
     if (CT == 1 || nt <= 1)
         walk(std::integral_constant<int, 1>{});
     else
