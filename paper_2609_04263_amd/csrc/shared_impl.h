@@ -692,20 +692,18 @@ struct Rows {
         }
     }
 
-    // One block: tokens t0 .. t0 + 31 (tail indices; with `off` = the sink's size
-    // for sink blocks), the first `live` of which exist.  key(e, kb, hi, lo) and
-    // value(mb, hi, lo) give its operands, meta its key scales; f is the values'
-    // power of two, ksm what the scores of reconstructed keys take.  LO: the
-    // operands have lo halves.  ORDER: one operand at a time (converted ones
-    // would otherwise all be made ahead of their products, in registers that
-    // there are not).
-    template <int NT, bool LO, bool ORDER, class Key, class Value>
-    __device__ __forceinline__ void block(Key key, Value value, const float* meta, float f, float ksm, int t0, int off,
-                                          int live, int lane)
+    // ---- A block takes four steps: scores (matrix products), settle (masks,
+    // running maxima), probabilities (vector operations), values (matrix
+    // products).  ORDER: one operand at a time (converted ones would otherwise
+    // all be made ahead of their products, in registers that there are not).
+
+    // l[c][4 e + i]: the score of token 8 qg + 4 e + i, in log2 units.  key(e, kb,
+    // hi, lo) gives the operands (LO: they have lo halves), meta the key
+    // scales, ksm what the scores of reconstructed keys take.
+    template <int NT, bool LO, bool ORDER, class Key>
+    __device__ __forceinline__ void scores(Key key, const float* meta, float ksm, int lane, float (*l)[8])
     {
         const int qg = lane >> 4, hh = lane & 15;
-        // ---- scores: l[c][4 e + i] is token 8 qg + 4 e + i
-        float l[NT][8];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             floatx4 S[NT];
@@ -761,7 +759,6 @@ struct Rows {
                         for (int i = 0; i < 4; ++i)
                             S[c][i] = fmaf(s4[i], acc[c][i], S[c][i]);
                 }
-                piece_end<(NG >= 4)>();  // (the sums of many groups side by side spill)
             }
 #pragma unroll
             for (int c = 0; c < NT; ++c)
@@ -769,6 +766,17 @@ struct Rows {
                 for (int i = 0; i < 4; ++i)
                     l[c][4 * e + i] = S[c][i];
         }
+    }
+
+    // Masks, the running maxima, and the values' power of two f (accumulators
+    // follow the largest values); shift and back are for probabilities().  The block is tokens t0
+    // .. t0 + 31 (tail indices; with `off` = the sink's size for sink blocks),
+    // the first `live` of which exist.
+    template <int NT>
+    __device__ __forceinline__ void settle(float (*l)[8], float f, int t0, int off, int live, int lane, float* shift,
+                                           float* back)
+    {
+        const int qg = lane >> 4;
         if (live < 32 || t0 + 32 > lim0 + off) {
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
@@ -778,8 +786,8 @@ struct Rows {
                     l[c][k] = 8 * qg + k < valid ? l[c][k] : kNegInf;
             }
         }
-        // ---- the values' power of two: accumulators follow the largest values
-        float bias = kPBits, back = 1.0f;
+        float bias = kPBits;
+        *back = 1.0f;
         if (f != vf) {
             const int d = (int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23);  // log2(f / vf)
             const float r = __uint_as_float((uint32_t)min(max(127 + d, 0), 254) << 23);
@@ -795,11 +803,9 @@ struct Rows {
             } else {
                 // smaller values: their probabilities make up for it
                 bias = kPBits - (float)d;
-                back = r;
+                *back = r;
             }
         }
-        // ---- softmax, and the probabilities' operands
-        half8 ph[NT], pl[NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             float bm = fmaxf(fmaxf(fmaxf(l[c][0], l[c][1]), fmaxf(l[c][2], l[c][3])),
@@ -815,17 +821,29 @@ struct Rows {
                     oacc[c][mb] *= alpha;
             }
             // (a column that has seen no token keeps m = -inf and gets zeros)
-            const float shift = bias - (m[c] == kNegInf ? 0.0f : m[c]);
+            shift[c] = bias - (m[c] == kNegInf ? 0.0f : m[c]);
+        }
+    }
+
+    template <int NT>
+    __device__ __forceinline__ void probabilities(const float (*l)[8], const float* shift, float back, half8* ph, half8* pl)
+    {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
             float pv[8], ps = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                pv[j] = __builtin_amdgcn_exp2f(l[c][perm4(j)] + shift);
+                pv[j] = __builtin_amdgcn_exp2f(l[c][perm4(j)] + shift[c]);
                 ps += pv[j];
             }
             lsum[c] = fmaf(ps, back, lsum[c]);
             split_nearest(pv, &ph[c], &pl[c]);
         }
-        // ---- values
+    }
+
+    template <int NT, bool LO, bool ORDER, class Value>
+    __device__ __forceinline__ void values(Value value, const half8* ph, const half8* pl)
+    {
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb) {
             half8 a, b;
@@ -843,6 +861,122 @@ struct Rows {
             }
             piece_end<ORDER>();
         }
+    }
+
+    // ---- The matrix products of an image in LDS.  Its fragments are read in the
+    // order of use, kAhead of them ahead of their products, through one ring
+    // of registers: keys, then values, then the keys of the next image.  (Left
+    // to itself the compiler reads each fragment right before its products,
+    // whose wait for LDS is longer than the products.)
+    static constexpr int kAhead = 4, NKF = 2 * NKB * (KH ? 2 : 1), NF = NKF + 2 * NMB;
+    static_assert(NKF % kAhead == 0 && NF % kAhead == 0, "a fragment's slot does not depend on the image");
+
+    // fragment k at fb (the image + 16 lane): (half, 32 channels, hi / lo) of the keys, (16 channels, hi / lo) of the values
+    static __device__ __forceinline__ half8 fragment(const uint8_t* fb, int k)
+    {
+        const int at = k >= NKF ? key_bytes(D, KH) + 1024 * ((k - NKF) >> 1) + 64 * D * ((k - NKF) & 1)
+                       : KH     ? 1024 * (k >> 1) + 64 * D * (k & 1)
+                                : 1024 * k;
+        return *(const half8*)(fb + at);
+    }
+
+    // The scores of the image at fb; the ring holds its first fragments.
+    template <int NT>
+    __device__ __forceinline__ void image_scores(half8* ring, const uint8_t* fb, const float* meta, int lane, float (*l)[8])
+    {
+        const int qg = lane >> 4, hh = lane & 15;
+        constexpr int PER = KH ? 2 : 1, GF = KS * PER;  // fragments of a key piece, and of a group
+        const float ksm = KH ? meta[2 * D + 1] : 0.0f;
+        floatx4 S[NT], acc[NT], s4;
+#pragma unroll
+        for (int k = 0; k < NKF; ++k) {
+            const int e = k / (NKF / 2), kk = k % (NKF / 2), g = kk / GF, kb = kk / PER;
+            if (kk == 0) {
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (!KH) {
+                    // offsets of four groups at once: row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
+                    const int tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
+#pragma unroll
+                    for (int j = 0; j < NZ; ++j) {
+                        const float z = meta[D + 32 * min(4 * j + qg, NG - 1) + tok];  // (times a zero sum past the last group)
+#pragma unroll
+                        for (int c = 0; c < NT; ++c)
+                            S[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z, qz[c][j], S[c], 0, 0, 0);
+                    }
+                }
+            }
+            if (kk % GF == 0) {
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    acc[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (!KH)
+                    s4 = *(const floatx4*)(meta + 32 * g + 8 * qg + 4 * e);
+            }
+            const half8 a = ring[k % kAhead];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                acc[c] = mfma16(a, q[c][kb], acc[c]);
+            if constexpr (ROT) {
+                if (!KH || k % 2 == 0) {  // (all but lo x lo)
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+                        acc[c] = mfma16(a, ql[c][kb], acc[c]);
+                }
+            }
+            ring[k % kAhead] = fragment(fb, k + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+            if (kk % GF == GF - 1) {
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        S[c][i] = KH ? acc[c][i] * ksm : fmaf(s4[i], acc[c][i], S[c][i]);
+            }
+            if (kk == NKF / 2 - 1) {
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        l[c][4 * e + i] = S[c][i];
+            }
+        }
+    }
+
+    // The value products of the image at fb; the ring goes on with the image at `next`.
+    template <int NT>
+    __device__ __forceinline__ void image_values(half8* ring, const uint8_t* fb, const uint8_t* next, const half8* ph,
+                                                 const half8* pl)
+    {
+#pragma unroll
+        for (int k = NKF; k < NF; ++k) {
+            const int mb = (k - NKF) >> 1;
+            const half8 a = ring[k % kAhead];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                oacc[c][mb] = mfma16(a, ph[c], oacc[c][mb]);
+            if ((k - NKF) % 2 == 0) {
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    oacc[c][mb] = mfma16(a, pl[c], oacc[c][mb]);
+            }
+            ring[k % kAhead] = k + kAhead < NF ? fragment(fb, k + kAhead) : fragment(next, k + kAhead - NF);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // All four steps of one block of converted operands.
+    template <bool LO, class Key, class Value>
+    __device__ __forceinline__ void block(Key key, Value value, const float* meta, float f, float ksm, int t0, int off,
+                                          int live, int lane)
+    {
+        float l[CT][8], shift[CT], back;
+        half8 ph[CT], pl[CT];
+        scores<CT, LO, true>(key, meta, ksm, lane, l);
+        settle<CT>(l, f, t0, off, live, lane, shift, &back);
+        probabilities<CT>(l, shift, back, ph, pl);
+        values<CT, LO, true>(value, ph, pl);
     }
 
     // The partial of tile c, unscaled: m, l and this lane's channels 16 mb + 4 qg .. + 3 of row lane % 16.
@@ -1059,25 +1193,37 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
         constexpr int NT = decltype(tiles_now)::value;
         const auto consume = [&](int v) __attribute__((always_inline)) {
-            for (int i = bw; i < NI && v + i < bl.v1; i += BW) {
-                const Span s(p, bl, v + i);
-                if (s.t0 >= T.lim1 + s.off)
-                    continue;
-                const uint8_t* fb = lds + i * BI + 16 * lane;
+            // images bw, bw + BW, .. that some of this wave's rows see
+            const int n = min(NI, bl.v1 - v);
+            const auto seen = [&](int i) {  // the first of them from i on
+                while (i < n) {
+                    const Span s(p, bl, v + i);
+                    if (s.t0 < T.lim1 + s.off)
+                        break;
+                    i += BW;
+                }
+                return i;
+            };
+            int i = seen(bw);
+            if (i >= n)
+                return;
+            half8 ring[T.kAhead];
+#pragma unroll
+            for (int k = 0; k < T.kAhead; ++k)
+                ring[k] = T.fragment(lds + i * BI + 16 * lane, k);
+            while (i < n) {
+                const int j = seen(i + BW);
+                const uint8_t *fb = lds + i * BI + 16 * lane, *next = j < n ? lds + j * BI + 16 * lane : fb;
                 const float* meta = (const float*)(metas + i * BM);
+                const Span s(p, bl, v + i);
                 const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
-                const float ksm = KH ? meta[2 * D + 1] : 0.0f;
-                T.template block<NT, true, false>(
-                    [&](int e, int kb, half8* hi, half8* lo) {
-                        *hi = *(const half8*)(fb + 1024 * (e * NKB + kb));
-                        if constexpr (KH)
-                            *lo = *(const half8*)(fb + 64 * D + 1024 * (e * NKB + kb));
-                    },
-                    [&](int mb, half8* hi, half8* lo) {
-                        *hi = *(const half8*)(fb + key_bytes(D, KH) + 1024 * mb);
-                        *lo = *(const half8*)(fb + key_bytes(D, KH) + 64 * D + 1024 * mb);
-                    },
-                    meta, f, ksm, s.t0, s.off, s.live, lane);
+                float l[NT][8], shift[NT], back;
+                half8 ph[NT], pl[NT];
+                T.template image_scores<NT>(ring, fb, meta, lane, l);
+                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
+                T.template probabilities<NT>(l, shift, back, ph, pl);
+                T.template image_values<NT>(ring, fb, next, ph, pl);
+                i = j;
             }
         };
         for (int v = bl.v0; v < bl.v1; v += NI) {
@@ -1178,7 +1324,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
             const int live = min(32, p.nq - s.t0);
             const float ksm = B.key_scales(now, live, meta, meta), f = B.value_scales(now, live, st);
             lds_order();
-            T.template block<1, true, true>(
+            T.template block<true>(
                 [&](int e, int kb, half8* hi, half8* lo) { B.key_piece(now, e * NKB + kb, meta, hi, lo); },
                 [&](int mb, half8* hi, half8* lo) { B.value_piece(now, mb, st, hi, lo); }, meta, f, ksm, s.t0, s.off,
                 s.live, lane);
@@ -1214,7 +1360,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
             if constexpr (D == 256)
                 load_keys();
             lds_order();
-            T.template block<1, false, true>(
+            T.template block<false>(
                 [&](int e, int kb, half8* hi, half8*) { *hi = B.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); },
                 [&](int mb, half8* hi, half8*) { *hi = *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, meta,
                 1.0f, p.sm_log2, s.t0, s.off, s.live, lane);
