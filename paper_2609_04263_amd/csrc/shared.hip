@@ -22,17 +22,41 @@ int ceil_div(int a, int b)
     return (a + b - 1) / b;
 }
 
-// How a segment's rows are taken: `rows` the most that one of its units has.
+// How a segment's rows are taken.
 struct Kind {
     bool direct;
     int per, step, round;  // rows per item, blocks that a range is a multiple of, items of a round
 };
 
-Kind kind_of(int D, int rows)
+Kind direct_kind()
 {
-    if (rows <= shr::kDirectRows)
-        return {true, shr::kDirectRows, shr::kDirectWaves, kDirectRound};
-    return {false, shr::item_rows(D), shr::images(D), kImageRound};
+    return {true, shr::kDirectRows, shr::kDirectWaves, kDirectRound};
+}
+
+Kind image_kind(int D, int rows)
+{
+    const int per = shr::item_rows(D), n16 = ceil_div(rows < per ? rows : per, 16);
+    return {false, per, shr::kWaves / shr::row_waves(D, n16), kImageRound};
+}
+
+// `rows` the most that a unit of the segment has, `units` of `blocks` blocks.
+// The direct kernel converts the codes once per 16 rows, the image kernel once
+// per 128 or 256, but begins with all waves converting and ends with the merge of
+// a wave's partials, which a range of a few images does not repay.  Two tiles
+// of 16 rows are always faster direct, three and four when the image kernel's
+// ranges would be two turns or less.  Direct / image, 8192 tokens, us:
+//                    32 rows               64 rows
+//                    1 prefix  8 prefixes  1 prefix (ranges of)  8 prefixes
+//     D = 64         19 / 25   30 / 35     20 / 26 (4 blocks)    49 / 42 (32 blocks)
+//     D = 128        26 / 30   52 / 52     33 / 43 (8 blocks)
+//     D = 256        49 / 46   98 / 98     72 / 65 (8 blocks)
+Kind kind_of(int D, int rows, long long units, int blocks)
+{
+    const Kind k = image_kind(D, rows);
+    return rows <= 2 * shr::kDirectRows ||
+                   (rows <= 4 * shr::kDirectRows && units * blocks <= 2ll * shr::images(D) * k.round)
+               ? direct_kind()
+               : k;
 }
 
 // Ranges that a segment of `tiles` tiles is cut into, at most.
@@ -129,14 +153,23 @@ void launch_join(const SharedParams& p, hipStream_t stream)
 
 // Each segment is cut into ranges for one round of its kernel's workgroups, a
 // range a multiple of the blocks that a workgroup takes at a time.  When both
-// segments go to one kernel the prefix' items, the longer ones, start first.
+// segments go to one kernel the prefix' items, the longer ones, start first,
+// and the suffix is cut for what they leave of their round: its later items
+// begin where others end, and more of them only add their fixed cost (200 tokens
+// after 2048, D = 64: 64 us with one range of a suffix, 76 with two).  If they
+// leave nothing the suffix is a round of its own (512 tokens after 8192,
+// D = 256: 389 us with one range of a suffix, 377 with two).
 void shared_plan(SharedParams* p, int D, int B)
 {
     const AttnParams &a = p->seg[0], &b = p->seg[1];
     int most = 0;
     for (int g = 0; g < p->P; ++g)
         most = p->first[g + 1] - p->first[g] > most ? p->first[g + 1] - p->first[g] : most;
-    const Kind kind[2] = {kind_of(D, most * p->C * a.G), kind_of(D, p->C * a.G)};
+    const auto blocks = [](const AttnParams& s) { return ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32); };
+    const int nb[2] = {blocks(a), blocks(b)};
+    // (a unit of the suffix never has more rows than its group's of the prefix: no direct prefix beside an image suffix)
+    const Kind k0 = kind_of(D, most * p->C * a.G, (long long)a.H * p->P, nb[0]);
+    const Kind kind[2] = {k0, k0.direct ? k0 : kind_of(D, p->C * a.G, (long long)a.H * B, nb[1])};
     p->tiles0 = 0;
     for (int g = 0; g < p->P; ++g) {
         p->tile0[g] = p->tiles0;
@@ -145,15 +178,15 @@ void shared_plan(SharedParams* p, int D, int B)
     p->tile0[p->P] = p->tiles0;
     const int tiles[2] = {p->tiles0, B * a.H * ceil_div(p->C * a.G, kind[1].per)};
     for (int k = 0; k < 2; ++k) {
-        const AttnParams& s = k ? b : a;
-        const int blocks = ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32), step = kind[k].step;
-        const int want = shared_splits(tiles[k], kind[k].round);
-        p->bps[k] = blocks > 0 ? ceil_div(ceil_div(blocks, want), step) * step : step;
-        p->S[k] = ceil_div(blocks, p->bps[k]);
+        int round = kind[k].round;
+        if (k && kind[1].direct == kind[0].direct && tiles[0] * p->S[0] < round)
+            round -= tiles[0] * p->S[0];
+        const int want = shared_splits(tiles[k], round), step = kind[k].step;
+        p->bps[k] = nb[k] > 0 ? ceil_div(ceil_div(nb[k], want), step) * step : step;
+        p->S[k] = ceil_div(nb[k], p->bps[k]);
     }
     p->items0 = tiles[0] * p->S[0];
     const int items1 = tiles[1] * p->S[1];
-    // (a suffix never has more rows per unit than the prefix of its group)
     p->image_items = (kind[0].direct ? 0 : p->items0) + (kind[1].direct ? 0 : items1);
     p->direct0 = p->image_items;
     p->direct_items = p->items0 + items1 - p->image_items;
@@ -163,11 +196,12 @@ int shared_split_bound(int B, int H, int D, int C, int G)
 {
     // The groups' tiles are never fewer than one group's of all rows; with fewer
     // rows per group either kernel may take them.
+    const auto splits = [&](long long units, int rows, const Kind& k) {
+        return shared_splits(units * ceil_div(rows, k.per), k.round);
+    };
     const auto most = [&](long long units, int rows) {
-        const Kind k = kind_of(D, rows);
-        const int one = shared_splits(units * ceil_div(rows, k.per), k.round);
-        const int direct = shared_splits(units * ceil_div(rows, shr::kDirectRows), kDirectRound);
-        return one > direct ? one : direct;
+        const int image = splits(units, rows, image_kind(D, rows)), direct = splits(units, rows, direct_kind());
+        return image > direct ? image : direct;
     };
     return most(H, B * C * G) + most((long long)B * H, C * G);
 }

@@ -13,7 +13,7 @@
 // So the codes of a prefix are read once per tile of its group's rows instead
 // of once per sequence.  Two kernels:
 //
-//   image_kernel   more than 16 rows per unit.  Eight waves, two per SIMD; up to
+//   image_kernel   units of many rows (more than 32, or 64).  Eight waves, two per SIMD; up to
 //                  128 tiles(D) rows.  In turns, the waves convert the next
 //                  images(D) blocks into images in LDS (parts(D) waves per
 //                  block), then multiply their own rows with them.  With R row
@@ -22,8 +22,8 @@
 //                  leave room for half the images, and every wave that takes
 //                  part in a block repeats the work on its scales: 3 to 15%
 //                  slower, in either order of the halves.)
-//   direct_kernel  at most 16 rows per unit (a suffix's queries, few samples):
-//                  four waves, each with blocks of its own, converts codes
+//   direct_kernel  units of few rows (a suffix's queries, few samples), 16 at a
+//                  time: four waves, each with blocks of its own, convert codes
 //                  into operands in registers.
 //
 // An image (or a converted block) holds operand fragments of
@@ -112,11 +112,27 @@ __host__ __device__ constexpr int stage_bytes(int D)
     return 8 * D;
 }
 
+// Floats per row of the waves' partials in LDS (16 rows next to each other are
+// written at once: a pitch of D would be one bank for all of them).
+__host__ __device__ constexpr int merge_pitch(int D)
+{
+    return D + 4;
+}
+
 __host__ __device__ constexpr int image_lds(int D, bool hilo)
 {
     const int walk = images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * stage_bytes(D);
-    const int merge = kWaves * 16 * (D + 2) * 4;
+    const int merge = kWaves * 16 * (merge_pitch(D) + 2) * 4;
     return walk > merge ? walk : merge;
+}
+
+// Waves that share an item's rows, of n16 tiles; kWaves / it take turns at the images.
+__host__ __device__ constexpr int row_waves(int D, int n16)
+{
+    int R = kWaves / images(D);
+    while (R * tiles(D) < n16)
+        R *= 2;
+    return R;
 }
 
 // ---- direct_kernel
@@ -133,7 +149,7 @@ __host__ __device__ constexpr int direct_region(int D, bool fp16)
 
 __host__ __device__ constexpr int direct_lds(int D, bool fp16)
 {
-    const int walk = kDirectWaves * direct_region(D, fp16), merge = kDirectWaves * 16 * (D + 2) * 4;
+    const int walk = kDirectWaves * direct_region(D, fp16), merge = kDirectWaves * 16 * (merge_pitch(D) + 2) * 4;
     return walk > merge ? walk : merge;
 }
 
@@ -1099,21 +1115,21 @@ struct Span {
     }
 };
 
-// One row's partial, merged over waves first, first + step, .. of lo [waves][16][D] and
-// lml [waves][16][2] (row r of each), four channels from d.
+// One row's partial, merged over waves first, first + 1, .. of lo [waves][16][merge_pitch]
+// and lml [waves][16][2] (row r of each), four channels from d.
 template <int D>
-__device__ __forceinline__ void merge_row(const SharedParams& sp, const float* lo, const float* lml, int first, int step,
+__device__ __forceinline__ void merge_row(const SharedParams& sp, const float* lo, const float* lml, int first,
                                           int waves, int r, int d, size_t at)
 {
     float M = kNegInf, L = 0.0f;
-    for (int w = first; w < waves; w += step)
+    for (int w = first; w < waves; ++w)
         M = fmaxf(M, lml[2 * (w * 16 + r)]);
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     if (M != kNegInf) {
-        for (int w = first; w < waves; w += step) {
+        for (int w = first; w < waves; ++w) {
             const float2 ml = *(const float2*)(lml + 2 * (w * 16 + r));
             const float sc = __builtin_amdgcn_exp2f(ml.x - M);
-            acc += *(const floatx4*)(lo + ((size_t)w * 16 + r) * D + d) * sc;
+            acc += *(const floatx4*)(lo + (w * 16 + r) * merge_pitch(D) + d) * sc;
             L += sc * ml.y;
         }
     }
@@ -1154,9 +1170,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
 
     // ---- this wave's rows and its images of a turn
     const int nt16 = (left + 15) >> 4;
-    int R = kWaves / NI;
-    while (R * CT < nt16)
-        R *= 2;
+    const int R = row_waves(D, nt16);
     const int BW = kWaves / R, rw = wave / BW, bw = wave - rw * BW;
     const int nt = nt16 > rw ? (nt16 - rw + R - 1) / R : 0;  // tiles rw, rw + R, ..
     Rows<D, KG, ROT, CT> T;
@@ -1240,8 +1254,8 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
 
     // ---- partials: of each wave when its rows are its own, else merged in LDS
     const float inv = T.inverse();
-    float* lo = (float*)lds;              // [waves][16][D]
-    float* lml = lo + kWaves * 16 * D;    // [waves][16][2]
+    float* lo = (float*)lds;                          // [waves][16][pitch]
+    float* lml = lo + kWaves * 16 * merge_pitch(D);   // [waves][16][2]
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         if (R * c >= nt16)
@@ -1263,14 +1277,14 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
             sync_lds();
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb)
-            *(floatx4*)(lo + ((size_t)wave * 16 + hh) * D + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
+            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
         if (qg == 0)
             *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
         sync_lds();
         for (int idx = threadIdx.x; idx < 16 * R * (D / 4); idx += kThreads) {
             const int row = idx / (D / 4), d = 4 * (idx % (D / 4)), w = row >> 4, rr = 16 * (w + R * c) + (row & 15);
             if (rr < left)
-                merge_row<D>(sp, lo, lml, w * BW, 1, w * BW + BW, row & 15, d,
+                merge_row<D>(sp, lo, lml, w * BW, w * BW + BW, row & 15, d,
                              (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + rr));
         }
     }
@@ -1332,31 +1346,36 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                 raw = prefetch(v + W);
         } else {
             const RowBlock rb(p, it.unit, bl, v, D);
-            // all loads first (at D = 256 the keys' after the values')
-            constexpr int NV = D / 16;
-            u32x4 kw[2 * NKB], vw[NV];
+            // All loads first (at D = 256 the keys' after the values').  Values are
+            // transposed through LDS: a lane has 8 channels of tokens t and t + 4,
+            // neighbours in the operand, 16 such pairs and 4 lanes of channels at a
+            // time: two lanes per bank.
+            constexpr int NV = D / 32;
+            u32x4 kw[2 * NKB], vw[NV][2];
             const auto load_keys = [&] {
 #pragma unroll
                 for (int i = 0; i < 2 * NKB; ++i)
                     kw[i] = B.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
             };
+            const int pair = lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (lane & 3);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int idx = lane + 64 * i, r = idx / (D / 8), c8 = 8 * (idx % (D / 8));
-                vw[i] = *(const u32x4*)(rb.v + (uint32_t)((rb.first + min(r, rb.live - 1)) % rb.ring * D + c8));
+            for (int h = 0; h < 2; ++h) {
+                const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    vw[i][h] = *(const u32x4*)(row + 32 * i);
             }
             if constexpr (D < 256)
                 load_keys();
             B.row_scales(meta);
             uint16_t* vt = (uint16_t*)st;
+            const uint32_t keep = (t0 < rb.live ? 0xFFFFu : 0u) | (t0 + 4 < rb.live ? 0xFFFF0000u : 0u);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int idx = lane + 64 * i, r = idx / (D / 8), c8 = 8 * (idx % (D / 8));
-                const int e = r & 7, pos = (r & ~7) + (e < 4 ? 2 * e : 2 * (e - 4) + 1);  // operand slot of token r
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    vt[(c8 + j) * kVtPitch + pos] = r < rb.live ? (uint16_t)(vw[i][j >> 1] >> (16 * (j & 1))) : (uint16_t)0;
-            }
+                    *(uint32_t*)(vt + (32 * i + c8 + j) * kVtPitch + 2 * pair) =
+                        __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
             if constexpr (D == 256)
                 load_keys();
             lds_order();
@@ -1371,19 +1390,19 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     // ---- the waves' partials merged
     const float inv = T.inverse(), l = sum_rows(T.lsum[0]);
     float* lo = (float*)lds;
-    float* lml = lo + W * 16 * D;
+    float* lml = lo + W * 16 * merge_pitch(D);
     __syncthreads();
     if (hh < left) {
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb)
-            *(floatx4*)(lo + ((size_t)wave * 16 + hh) * D + 16 * mb + 4 * qg) = T.oacc[0][mb] * inv;
+            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[0][mb] * inv;
         if (qg == 0)
             *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[0], l);
     }
     __syncthreads();
     for (int idx = threadIdx.x; idx < left * (D / 4); idx += kDirectThreads) {
         const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
-        merge_row<D>(sp, lo, lml, 0, 1, W, r, d, (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + r));
+        merge_row<D>(sp, lo, lml, 0, W, r, d, (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + r));
     }
 }
 
