@@ -411,15 +411,15 @@ struct Builder {
     }
 
     // The key scales of a coded block: per-token groups (times sm_scale log2 e) to
-    // meta, [group][32] scales and offsets; per-channel ones to st, [channel].
-    // Returns what the scores of reconstructed keys take.
-    __device__ __forceinline__ float key_scales(const Loads& r, int live, float* meta, float* st) const
+    // meta, [group][32] scales and offsets; per-channel ones (times a power of two
+    // and pre) to st, [channel].  Returns what the scores of the latter take.
+    __device__ __forceinline__ float key_scales(const Loads& r, int live, float* meta, float* st, float pre = 1.0f) const
     {
         float sv[4], zv[4];
         const float mid = coding<KB>(kaff).mid;
         widen(r.ks, r.kz, kaff, mid, live, KH, sv, zv);
         if constexpr (KH) {
-            const float f = range_scale(sv, zv, mid, nkc);
+            const float f = range_scale(sv, zv, mid, nkc) * pre;
             if (lane < nkc)
                 put_chunk(st, sv, zv, f);
             return p.sm_log2 * (1.0f / f);
@@ -431,13 +431,13 @@ struct Builder {
     }
 
     // The value scales of a coded block to st, [group][32]; returns the power of
-    // two that they were multiplied with.
-    __device__ __forceinline__ float value_scales(const Loads& r, int live, float* st) const
+    // two (pre included) that they were multiplied with.
+    __device__ __forceinline__ float value_scales(const Loads& r, int live, float* st, float pre = 1.0f) const
     {
         float sv[4], zv[4];
         const float mid = coding<VB>(vaff).mid;
         widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
-        const float f = range_scale(sv, zv, mid, nvc);
+        const float f = range_scale(sv, zv, mid, nvc) * pre;
         if (lane < nvc)
             put_chunk(st, sv, zv, f);
         return f;
@@ -458,10 +458,20 @@ struct Builder {
         split_nearest(x, hi, lo);
     }
 
+    __device__ __forceinline__ half8 key_codes(const Loads& r, int i) const
+    {
+        return centred<KB>(r.k, i, coding<KB>(kaff).centre);
+    }
+
+    __device__ __forceinline__ half8 value_codes(const Loads& r, int i) const
+    {
+        return centred<VB>(r.v, i, coding<VB>(vaff).centre);
+    }
+
     // Key piece i: the codes (lo untouched), or the reconstructed keys.
     __device__ __forceinline__ void key_piece(const Loads& r, int i, const float* st, half8* hi, half8* lo) const
     {
-        const half8 a = centred<KB>(r.k, i, coding<KB>(kaff).centre);
+        const half8 a = key_codes(r, i);
         if constexpr (KH)
             reconstruct(a, st + 32 * kblock(i) + 8 * (lane >> 4), hi, lo);
         else
@@ -472,7 +482,7 @@ struct Builder {
     __device__ __forceinline__ void value_piece(const Loads& r, int i, const float* st, half8* hi, half8* lo) const
     {
         const int g = 16 * (NV * part + i) >> (31 - __builtin_clz(p.v_group));
-        reconstruct(centred<VB>(r.v, i, coding<VB>(vaff).centre), st + 32 * g + 8 * (lane >> 4), hi, lo);
+        reconstruct(value_codes(r, i), st + 32 * g + 8 * (lane >> 4), hi, lo);
     }
 
     // This wave's part of the image of a coded block whose first `live` tokens
@@ -593,16 +603,18 @@ struct Builder {
 
 // ------------------------------------------------------------ rows
 
-template <bool ORDER>
-__device__ __forceinline__ void piece_end()
+// A power of two <= 1 by which scales in range_scale's range are at most one
+// (mid scale <= 2^12): the row side's operand x scale is no larger than x then.
+template <int BITS>
+__device__ __forceinline__ float to_one()
 {
-    if constexpr (ORDER)
-        __builtin_amdgcn_sched_barrier(0);
+    return (BITS == 8 ? 128.0f : BITS == 4 ? 8.0f : 2.0f) / 4096.0f;
 }
 
 // A wave's state: NT tiles of 16 query rows (columns of the MFMAs).  KG: key
-// group size / 32 (0: reconstructed keys, hi + lo).  ROT: rotated queries, hi + lo.
-template <int D, int KG, bool ROT, int CT>
+// group size / 32 (0: per-channel scales).  ROT: rotated queries, hi + lo.
+// DIRECT: direct_kernel's, which takes value offsets apart.
+template <int D, int KG, bool ROT, int CT, bool DIRECT>
 struct Rows {
     static constexpr int NKB = D / 32, NMB = D / 16;
     static constexpr bool KH = KG == 0;
@@ -610,6 +622,7 @@ struct Rows {
     half8 q[CT][NKB], ql[ROT ? CT : 1][ROT ? NKB : 1];
     float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg
     floatx4 oacc[CT][NMB];
+    float zacc[DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
     float m[CT], lsum[CT];   // running max (log2 units), lane partial sum (times 2^kPBits)
     float vf;                // power of two that the accumulated values carry (uniform)
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
@@ -699,6 +712,9 @@ struct Rows {
     {
         vf = 0.0f;
 #pragma unroll
+        for (float& z : zacc)
+            z = 0.0f;
+#pragma unroll
         for (int c = 0; c < CT; ++c) {
             m[c] = kNegInf;
             lsum[c] = 0.0f;
@@ -710,77 +726,14 @@ struct Rows {
 
     // ---- A block takes four steps: scores (matrix products), settle (masks,
     // running maxima), probabilities (vector operations), values (matrix
-    // products).  ORDER: one operand at a time (converted ones would otherwise
-    // all be made ahead of their products, in registers that there are not).
+    // products).
 
-    // l[c][4 e + i]: the score of token 8 qg + 4 e + i, in log2 units.  key(e, kb,
-    // hi, lo) gives the operands (LO: they have lo halves), meta the key
-    // scales, ksm what the scores of reconstructed keys take.
-    template <int NT, bool LO, bool ORDER, class Key>
-    __device__ __forceinline__ void scores(Key key, const float* meta, float ksm, int lane, float (*l)[8])
+    __device__ __forceinline__ void scale_offsets(float by)
     {
-        const int qg = lane >> 4, hh = lane & 15;
+        if constexpr (DIRECT) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            floatx4 S[NT];
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-                S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            if constexpr (!KH) {
-                // offsets of four groups at once: row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
-                const int tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
-#pragma unroll
-                for (int j = 0; j < NZ; ++j) {
-                    const float z = meta[D + 32 * min(4 * j + qg, NG - 1) + tok];  // (times a zero sum past the last group)
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-                        S[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z, qz[c][j], S[c], 0, 0, 0);
-                }
-            }
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                floatx4 acc[NT];
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-                    acc[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int u = 0; u < KS; ++u) {
-                    const int kb = g * KS + u;
-                    half8 a, b;
-                    key(e, kb, &a, &b);
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-                        acc[c] = mfma16(a, q[c][kb], acc[c]);
-                    if constexpr (ROT) {
-#pragma unroll
-                        for (int c = 0; c < NT; ++c)
-                            acc[c] = mfma16(a, ql[c][kb], acc[c]);
-                    }
-                    if constexpr (KH && LO) {
-#pragma unroll
-                        for (int c = 0; c < NT; ++c)
-                            acc[c] = mfma16(b, q[c][kb], acc[c]);
-                    }
-                    piece_end<ORDER>();
-                }
-                if constexpr (KH) {
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-                        S[c] = acc[c] * ksm;
-                } else {
-                    const floatx4 s4 = *(const floatx4*)(meta + 32 * g + 8 * qg + 4 * e);
-#pragma unroll
-                    for (int c = 0; c < NT; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            S[c][i] = fmaf(s4[i], acc[c][i], S[c][i]);
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    l[c][4 * e + i] = S[c][i];
+            for (float& z : zacc)
+                z *= by;
         }
     }
 
@@ -814,6 +767,7 @@ struct Rows {
 #pragma unroll
                         for (int mb = 0; mb < NMB; ++mb)
                             oacc[c][mb] *= r;
+                    scale_offsets(r);
                 }
                 vf = f;
             } else {
@@ -835,10 +789,23 @@ struct Rows {
 #pragma unroll
                 for (int mb = 0; mb < NMB; ++mb)
                     oacc[c][mb] *= alpha;
+                scale_offsets(alpha);
             }
             // (a column that has seen no token keeps m = -inf and gets zeros)
             shift[c] = bias - (m[c] == kNegInf ? 0.0f : m[c]);
         }
+    }
+
+    // The probabilities of tile c in operand order, summed.
+    __device__ __forceinline__ void exponentials(int c, const float* l, float shift, float back, float* pv)
+    {
+        float ps = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            pv[j] = __builtin_amdgcn_exp2f(l[perm4(j)] + shift);
+            ps += pv[j];
+        }
+        lsum[c] = fmaf(ps, back, lsum[c]);
     }
 
     template <int NT>
@@ -846,36 +813,9 @@ struct Rows {
     {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-            float pv[8], ps = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                pv[j] = __builtin_amdgcn_exp2f(l[c][perm4(j)] + shift[c]);
-                ps += pv[j];
-            }
-            lsum[c] = fmaf(ps, back, lsum[c]);
+            float pv[8];
+            exponentials(c, l[c], shift[c], back, pv);
             split_nearest(pv, &ph[c], &pl[c]);
-        }
-    }
-
-    template <int NT, bool LO, bool ORDER, class Value>
-    __device__ __forceinline__ void values(Value value, const half8* ph, const half8* pl)
-    {
-#pragma unroll
-        for (int mb = 0; mb < NMB; ++mb) {
-            half8 a, b;
-            value(mb, &a, &b);
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-                oacc[c][mb] = mfma16(a, ph[c], oacc[c][mb]);
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-                oacc[c][mb] = mfma16(a, pl[c], oacc[c][mb]);
-            if constexpr (LO) {
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-                    oacc[c][mb] = mfma16(b, ph[c], oacc[c][mb]);
-            }
-            piece_end<ORDER>();
         }
     }
 
@@ -982,17 +922,148 @@ struct Rows {
         }
     }
 
-    // All four steps of one block of converted operands.
-    template <bool LO, class Key, class Value>
-    __device__ __forceinline__ void block(Key key, Value value, const float* meta, float f, float ksm, int t0, int off,
-                                          int live, int lane)
+    // ---- One block of codes or fp16 rows in registers, of a wave with one tile.
+    // The pieces are made one at a time (left to itself the compiler makes
+    // them all ahead of their products, in registers that there are not).
+
+    // l[4 e + i]: the score of token 8 qg + 4 e + i, in log2 units, from key(e, kb)
+    // and meta's scales.
+    template <class Key>
+    __device__ __forceinline__ void group_scores(Key key, const float* meta, int lane, float* l)
     {
-        float l[CT][8], shift[CT], back;
-        half8 ph[CT], pl[CT];
-        scores<CT, LO, true>(key, meta, ksm, lane, l);
-        settle<CT>(l, f, t0, off, live, lane, shift, &back);
-        probabilities<CT>(l, shift, back, ph, pl);
-        values<CT, LO, true>(value, ph, pl);
+        const int qg = lane >> 4, hh = lane & 15;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            floatx4 S = {0.0f, 0.0f, 0.0f, 0.0f};
+            // offsets of four groups at once: row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
+            const int tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
+#pragma unroll
+            for (int j = 0; j < NZ; ++j)  // (times a zero sum past the last group)
+                S = __builtin_amdgcn_mfma_f32_16x16x4f32(meta[D + 32 * min(4 * j + qg, NG - 1) + tok], qz[0][j], S, 0, 0, 0);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int kb = g * KS; kb < (g + 1) * KS; ++kb) {
+                    const half8 a = key(e, kb);
+                    acc = mfma16(a, q[0][kb], acc);
+                    if constexpr (ROT)
+                        acc = mfma16(a, ql[0][kb], acc);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const floatx4 s4 = *(const floatx4*)(meta + 32 * g + 8 * qg + 4 * e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    S[i] = fmaf(s4[i], acc[i], S[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                l[4 * e + i] = S[i];
+        }
+    }
+
+    // The same with per-channel scales (CODED: scales s at st, offsets z D further):
+    // sum_d q_d (s_d c_d + z_d) = (q s) . c + q . z.
+    template <bool CODED, class Key>
+    __device__ __forceinline__ void channel_scores(Key key, const float* st, float ksm, int lane, float* l)
+    {
+        const int qg = lane >> 4;
+        floatx4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        float z = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+            half8 hi = q[0][kb], lo = ql[0][ROT ? kb : 0];
+            if constexpr (CODED) {
+                const float* at = st + 32 * kb + 8 * qg;
+                const float4 s0 = *(const float4*)at, s1 = *(const float4*)(at + 4);
+                const float4 z0 = *(const float4*)(at + D), z1 = *(const float4*)(at + D + 4);
+                const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+                const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float qf = (float)hi[j] + (ROT ? (float)lo[j] : 0.0f);
+                    x[j] = qf * sn[perm4(j)];
+                    z = fmaf(qf, zn[perm4(j)], z);
+                }
+                split_nearest(x, &hi, &lo);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const half8 a = key(e, kb);
+                acc[e] = mfma16(a, hi, acc[e]);
+                if constexpr (CODED || ROT)
+                    acc[e] = mfma16(a, lo, acc[e]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (CODED)
+            z = sum_rows(z);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                l[4 * e + i] = (acc[e][i] + z) * ksm;
+    }
+
+    // Values of codes(mb), scales s at st (offsets z D further) of `group` channels:
+    // sum_t p_t (s_t c_t + z_t) = (p s) . c + p . z.
+    template <class Codes>
+    __device__ __forceinline__ void group_values(Codes codes, const float* st, int group, bool affine, const float* pv,
+                                                 int lane)
+    {
+        half8 hi, lo;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb) {
+            if (mb % 2 == 0 && (16 * mb & (group - 1)) == 0) {
+                const float* at = st + 32 * (16 * mb >> (31 - __builtin_clz(group))) + 8 * (lane >> 4);
+                const float4 s0 = *(const float4*)at, s1 = *(const float4*)(at + 4);
+                const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = pv[j] * sn[perm4(j)];
+                split_nearest(x, &hi, &lo);
+                if (affine) {
+                    const float4 z0 = *(const float4*)(at + D), z1 = *(const float4*)(at + D + 4);
+                    const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        zacc[mb / 2] = fmaf(pv[j], zn[perm4(j)], zacc[mb / 2]);
+                }
+            }
+            const half8 a = codes(mb);
+            oacc[0][mb] = mfma16(a, hi, oacc[0][mb]);
+            oacc[0][mb] = mfma16(a, lo, oacc[0][mb]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // Values that are operands as they are.
+    template <class Value>
+    __device__ __forceinline__ void row_values(Value value, const float* pv)
+    {
+        half8 hi, lo;
+        split_nearest(pv, &hi, &lo);
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb) {
+            const half8 a = value(mb);
+            oacc[0][mb] = mfma16(a, hi, oacc[0][mb]);
+            oacc[0][mb] = mfma16(a, lo, oacc[0][mb]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // The value offsets join their channels.
+    __device__ __forceinline__ void add_offsets(int group)
+    {
+        float z = 0.0f;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb) {
+            if (mb % 2 == 0 && (16 * mb & (group - 1)) == 0)
+                z = sum_rows(zacc[mb / 2]);
+            oacc[0][mb] += z;
+        }
     }
 
     // The partial of tile c, unscaled: m, l and this lane's channels 16 mb + 4 qg .. + 3 of row lane % 16.
@@ -1138,13 +1209,13 @@ __device__ __forceinline__ void merge_row(const SharedParams& sp, const float* l
         *(float2*)(sp.part_ml + 2 * at) = make_float2(M, L);
 }
 
-// ROWS: the format has fp16 tokens (their conversion in the loop costs the other
-// formats registers that the loop spills).
+// ROWS (of both kernels): the format has fp16 tokens (their conversion in the
+// loop costs the other formats registers that the loop spills).
 template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
 {
     constexpr bool KH = KG == 0;
-    constexpr int CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16, NKB = D / 32;
+    constexpr int CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16;
     constexpr int BI = image_bytes(D, KH), BM = meta_bytes(D);
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
@@ -1173,7 +1244,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     const int R = row_waves(D, nt16);
     const int BW = kWaves / R, rw = wave / BW, bw = wave - rw * BW;
     const int nt = nt16 > rw ? (nt16 - rw + R - 1) / R : 0;  // tiles rw, rw + R, ..
-    Rows<D, KG, ROT, CT> T;
+    Rows<D, KG, ROT, CT, false> T;
     T.lim0 = it.lim + (it.causal ? (it.r0 + 16 * rw) / G : 0);
     {
         const int last = min(left, 16 * (rw + R * (nt - 1)) + 16) - 1;
@@ -1296,7 +1367,7 @@ __host__ __device__ constexpr int direct_waves(int D)
     return D == 64 ? 3 : 2;
 }
 
-template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
 {
     constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves;
@@ -1313,12 +1384,12 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     const Build B(p, it.unit, 0, lane);
     const auto prefetch = [&](int v) {
         typename Build::Loads r;
-        if (bl.ncb > 0)
+        if (!ROWS || bl.ncb > 0)
             B.load(r, bl.nearest(v));
         return r;
     };
     typename Build::Loads raw = prefetch(bl.v0 + wave);
-    Rows<D, KG, ROT, 1> T;
+    Rows<D, KG, ROT, 1, true> T;
     T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
     {
         const int rc = min(hh, left - 1);
@@ -1330,62 +1401,76 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     float* st = meta + meta_bytes(D) / 4;
     for (int v = bl.v0 + wave; v < bl.v1; v += W) {
         const Span s(p, bl, v);
+        float l[1][8], pv[8], shift, back;
         lds_order();
-        if (bl.coded(v)) {
+        if (!ROWS || bl.coded(v)) {
             const typename Build::Loads now = raw;
             if constexpr (kAhead)
                 raw = prefetch(v + W);
             const int live = min(32, p.nq - s.t0);
-            const float ksm = B.key_scales(now, live, meta, meta), f = B.value_scales(now, live, st);
+            const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
+            const float f = B.value_scales(now, live, st, to_one<VB>());
             lds_order();
-            T.template block<true>(
-                [&](int e, int kb, half8* hi, half8* lo) { B.key_piece(now, e * NKB + kb, meta, hi, lo); },
-                [&](int mb, half8* hi, half8* lo) { B.value_piece(now, mb, st, hi, lo); }, meta, f, ksm, s.t0, s.off,
-                s.live, lane);
+            const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
+            if constexpr (KG == 0)
+                T.template channel_scores<true>(key, meta, ksm, lane, l[0]);
+            else
+                T.group_scores(key, meta, lane, l[0]);
+            T.template settle<1>(l, f, s.t0, s.off, s.live, lane, &shift, &back);
+            T.exponentials(0, l[0], shift, back, pv);
+            T.group_values([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
             if constexpr (!kAhead)
                 raw = prefetch(v + W);
         } else {
             const RowBlock rb(p, it.unit, bl, v, D);
-            // All loads first (at D = 256 the keys' after the values').  Values are
-            // transposed through LDS: a lane has 8 channels of tokens t and t + 4,
-            // neighbours in the operand, 16 such pairs and 4 lanes of channels at a
-            // time: two lanes per bank.
-            constexpr int NV = D / 32;
-            u32x4 kw[2 * NKB], vw[NV][2];
-            const auto load_keys = [&] {
-#pragma unroll
-                for (int i = 0; i < 2 * NKB; ++i)
-                    kw[i] = B.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
-            };
-            const int pair = lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (lane & 3);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    vw[i][h] = *(const u32x4*)(row + 32 * i);
-            }
-            if constexpr (D < 256)
-                load_keys();
-            B.row_scales(meta);
+            Build A = B;  // (the addresses below are made here, not kept in registers over the loop)
+            asm volatile("" : "+v"(A.lane));
+            // Values are transposed through LDS, 128 channels at a time: a lane has 8
+            // channels of tokens t and t + 4, neighbours in the operand, 16 such
+            // pairs and 4 lanes of channels at a time: two lanes per bank.
+            constexpr int NV = (D < 128 ? D : 128) / 32;
+            u32x4 kw[2 * NKB];
             uint16_t* vt = (uint16_t*)st;
+            const int pair = A.lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (A.lane & 3);
             const uint32_t keep = (t0 < rb.live ? 0xFFFFu : 0u) | (t0 + 4 < rb.live ? 0xFFFF0000u : 0u);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int u = 0; u < D / 32; u += NV) {
+                u32x4 vw[NV][2];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *(uint32_t*)(vt + (32 * i + c8 + j) * kVtPitch + 2 * pair) =
-                        __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
-            if constexpr (D == 256)
-                load_keys();
+                for (int h = 0; h < 2; ++h) {
+                    const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        vw[i][h] = *(const u32x4*)(row + 32 * (u + i));
+                }
+                if (u + NV >= D / 32) {
+#pragma unroll
+                    for (int i = 0; i < 2 * NKB; ++i)
+                        kw[i] = A.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
+                }
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *(uint32_t*)(vt + (32 * (u + i) + c8 + j) * kVtPitch + 2 * pair) =
+                            __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            A.row_scales(meta);
             lds_order();
-            T.template block<false>(
-                [&](int e, int kb, half8* hi, half8*) { *hi = B.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); },
-                [&](int mb, half8* hi, half8*) { *hi = *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, meta,
-                1.0f, p.sm_log2, s.t0, s.off, s.live, lane);
+            const auto key = [&](int e, int kb) { return A.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); };
+            if constexpr (KG == 0)
+                T.template channel_scores<false>(key, nullptr, p.sm_log2, lane, l[0]);
+            else
+                T.group_scores(key, meta, lane, l[0]);
+            T.template settle<1>(l, 1.0f, s.t0, s.off, s.live, lane, &shift, &back);
+            T.exponentials(0, l[0], shift, back, pv);
+            T.row_values([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
             raw = prefetch(v + W);
         }
     }
+
+    T.add_offsets(p.v_group);
 
     // ---- the waves' partials merged
     const float inv = T.inverse(), l = sum_rows(T.lsum[0]);
@@ -1411,14 +1496,12 @@ template <int D, int KG, int KB, int VB, bool M16, bool ROT>
 hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
 {
     const bool rows = p.seg[0].ring > 0 || p.seg[0].sink > 0;
-    if (p.image_items > 0) {
-        // (per-channel keys come with a window)
-        constexpr bool kWindow = KG == 0;
+    constexpr bool kWindow = KG == 0;  // (per-channel keys come with a window)
+    if (p.image_items > 0)
         launch_kernel(rows ? image_kernel<D, KG, KB, VB, M16, ROT, true> : image_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
                       dim3(p.image_items), dim3(kThreads), (size_t)image_lds(D, KG == 0), stream, p);
-    }
     if (p.direct_items > 0)
-        launch_kernel(direct_kernel<D, KG, KB, VB, M16, ROT>, dim3(p.direct_items), dim3(kDirectThreads),
+        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true> : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow>, dim3(p.direct_items), dim3(kDirectThreads),
                       (size_t)direct_lds(D, rows), stream, p);
     return hipGetLastError();
 }
