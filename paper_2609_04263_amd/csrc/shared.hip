@@ -68,73 +68,84 @@ int shared_splits(long long tiles, int round)
 // Joins the partials of a row: D / 4 threads, four output channels each, take
 // every J-th partial, J of them side by side,
 //     O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s,
-// then their sums meet in LDS and a rotating format's rows are rotated back
-// there (the normalized transform is its own inverse).  Bound by the read of the
-// partials, which needs many loads in flight: with one thread per four channels
-// walking all of 33 partials, 2048 rows at D = 128 took 17 us.
-constexpr int kJoinThreads = 256;
+// with a running M over batches of kJoinBatch; then their sums meet in LDS and a
+// rotating format's rows are rotated back over the threads' registers (the
+// normalized transform is its own inverse).  Bound by the latency of its loads:
+// of 33 partials, 2048 rows at D = 128 take 10 us, 17 when one thread per
+// four channels walks them and 12 when M is found in a pass before.
+constexpr int kJoinThreads = 256, kJoinBatch = 4;
 
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p, int J)
 {
     constexpr int TR = D / 4, SLOTS = kJoinThreads / TR;  // threads of a row, rows J = 1 would take
     __shared__ __attribute__((aligned(16))) float x[SLOTS * D];
-    __shared__ float xl[SLOTS];
+    __shared__ float2 xml[SLOTS];
     const int slot = threadIdx.x / TR, d = 4 * (threadIdx.x % TR);
     const int R = SLOTS / J, rl = slot % R, j = slot / R;
     const size_t row = (size_t)blockIdx.x * R + rl;
+    const size_t at = row < p.rows ? row : p.rows - 1;
     const int S = p.S[0] + p.S[1];
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    float L = 0.0f;
-    if (row < p.rows) {
-        const float* ml = p.part_ml + 2 * row;
-        float M = -INFINITY;
-#pragma unroll 4
-        for (int s = 0; s < S; ++s)
-            M = fmaxf(M, ml[2 * (size_t)s * p.rows]);
-#pragma unroll 4
-        for (int s = j; s < S; s += J) {
-            const float2 v = *(const float2*)(ml + 2 * (size_t)s * p.rows);
-            const floatx4 o = *(const floatx4*)(p.part_o + ((size_t)s * p.rows + row) * D + d);
-            const float w = v.x == -INFINITY ? 0.0f : fast_exp2(v.x - M);
-            acc += o * w;
-            L += v.y * w;
+    float M = -INFINITY, L = 0.0f;
+    const auto raise = [&](float m) {  // M to at least m
+        if (m > M) {
+            const float w = fast_exp2(M - m);
+            acc *= w;
+            L *= w;
+            M = m;
+        }
+    };
+    for (int s0 = j; s0 < S; s0 += kJoinBatch * J) {
+        float2 ml[kJoinBatch];
+        floatx4 o[kJoinBatch];
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) {
+            const size_t i = (size_t)min(s0 + k * J, S - 1) * p.rows + at;
+            ml[k] = *(const float2*)(p.part_ml + 2 * i);
+            o[k] = *(const floatx4*)(p.part_o + i * D + d);
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) {
+            ml[k].x = s0 + k * J < S ? ml[k].x : -INFINITY;
+            m = fmaxf(m, ml[k].x);
+        }
+        raise(m);
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) {
+            const float w = ml[k].x == -INFINITY ? 0.0f : fast_exp2(ml[k].x - M);
+            acc += o[k] * w;
+            L += ml[k].y * w;
         }
     }
     if (J > 1) {
         *(floatx4*)(x + slot * D + d) = acc;
         if (d == 0)
-            xl[slot] = L;
+            xml[slot] = make_float2(M, L);
         __syncthreads();
-        if (slot < R) {
-            for (int k = 1; k < J; ++k) {
-                acc += *(const floatx4*)(x + (slot + k * R) * D + d);
-                L += xl[slot + k * R];
-            }
+        for (int k = 1; k < J && slot < R; ++k) {
+            const float2 ml = xml[slot + k * R];
+            raise(ml.x);
+            const float w = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - M);
+            acc += *(const floatx4*)(x + (slot + k * R) * D + d) * w;
+            L += ml.y * w;
         }
     }
     acc *= 1.0f / L;  // every row sees a token
-    if (!p.rotate) {
-        if (slot < R && row < p.rows)
-            *(floatx4*)(p.out + row * D + d) = acc;
-        return;
-    }
-    if (J > 1)
-        __syncthreads();
-    if (slot < R)
-        *(floatx4*)(x + slot * D + d) = acc;
-    __syncthreads();
-    for (int h = 1; h < D; h <<= 1) {
-        for (int i = threadIdx.x; i < R * (D / 2); i += kJoinThreads) {
-            const int r = i / (D / 2), k = i % (D / 2), jj = r * D + (k / h) * 2 * h + (k % h);
-            const float a = x[jj], c = x[jj + h];
-            x[jj] = a + c;
-            x[jj + h] = a - c;
-        }
-        __syncthreads();
+    if (p.rotate) {
+        const float a = acc[0] + acc[1], b = acc[0] - acc[1], c = acc[2] + acc[3], e = acc[2] - acc[3];
+        acc = floatx4{a + c, b + e, a - c, b - e} * p.rot_c;
+#pragma unroll
+        for (int h = 1; h < TR; h <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float y = __shfl_xor(acc[i], h);
+                acc[i] = threadIdx.x & h ? y - acc[i] : acc[i] + y;
+            }
     }
     if (slot < R && row < p.rows)
-        *(floatx4*)(p.out + row * D + d) = *(const floatx4*)(x + slot * D + d) * p.rot_c;
+        *(floatx4*)(p.out + row * D + d) = acc;
 }
 
 template <int D>
