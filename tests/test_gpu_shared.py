@@ -1,17 +1,16 @@
 """Attention over a shared prefix and own suffixes against 64-bit attention
 over the oracle's reconstruction of both caches.
 
-Bound.  All products of the kernels are exact (binary16 operands, hi + lo
-where a value has more bits) and sums are binary32, so a score's error is
-about sqrt(steps) 2^-25 of the largest partial sum.  A score sums D / 32
-products of 32 channels and up to D / 32 scaled groups (at most 16 steps at D
-= 256), and the coded operands carry a bias that inflates the partial sums up
-to eight times |q| |k| sm, which with four outlier channels of 20 is about
-sm sqrt(D) sqrt(1 + 4 * 400 / D) <= 5 natural units: an error of 4 * 2^-25 * 40
-= 5e-6.  Outputs are averages of values weighted by e^score, so that is their
-relative error too, and the value sums, biased alike, add as much again.
-2^-14 = 6e-5 of the norm leaves a factor of six; without the lo half of an
-operand the error would be 2^-12.  A larger softmax scale scales it.
+Bound.  The matrix products are exact (binary16 operands, hi + lo where a value
+has more bits: 22 of them) and sums are binary32.  A score sums D / 32 products
+of 32 channels and up to D / 32 scaled groups, at most 16 steps at D = 256, each
+off by 2^-24 of a partial sum of at most |q| |k| sm, which with four outlier
+channels of 20 is about sm sqrt(D) sqrt(1 + 4 * 400 / D) <= 5 natural units, and
+the codes' centre up to eight times that.  Taken as random that is 4 * 2^-25 * 40 =
+5e-6, and an output, an average of values weighted by e^score, is off by as much
+relatively; its own sums add as much again.  2^-14 = 6e-5 of the norm leaves a
+factor of six; without the lo half of an operand the error would be 2^-12.  A
+larger softmax scale scales it.
 """
 import numpy as np
 import pytest
@@ -139,6 +138,19 @@ def test_decode(name, n_p, n_s):
 
 
 @pytest.mark.parametrize("name", list(CASES))
+def test_decode_of_many_samples(name):
+    # groups of 36 and 124 rows: the prefix is converted once for all of them
+    run(name, [0, 9, 40], 1500, 70, seed=3)
+
+
+@pytest.mark.parametrize("n_p", [100, 4500])
+@pytest.mark.parametrize("G,count", [(2, 16), (3, 11), (2, 32), (5, 13)])
+def test_rows_between_the_kernels(G, count, n_p):
+    # 32, 33, 64 and 65 rows of eight units, of a few blocks and of many
+    run("gqa12b", [0, count, 2 * count], n_p, 40, G=G, H=4, seed=4)
+
+
+@pytest.mark.parametrize("name", list(CASES))
 @pytest.mark.parametrize("C,n_s", [(5, 5), (5, 165), (37, 70), (130, 131)])
 def test_chunk(name, C, n_s):
     run(name, [0, 1, 3], 290, n_s, C=C, seed=C + n_s)
@@ -239,6 +251,38 @@ def test_the_largest_scores_on_one_side(name, span):
     Q = synth.to_bf16_bits(synth.bf16_bits_to_f32(Q) * np.float32(0.25) + u)
     # (partial sums of these scores reach 8 (40 + 5) units: nine times the bound's)
     close(call(*caches, [0, B], Q, D ** -0.5), reference(*caches, [0, B], Q, D ** -0.5), 9.0)
+
+
+@pytest.mark.parametrize("first", [[0, 3], [0, 33]])
+@pytest.mark.parametrize("name", [n for n in CASES if n in ("tiny_b1", "tiny_b16", "kivi", "gqa12b", "hadamard", "sink64")
+                                  or CASES[n][0]["k_bits"] == 8])
+def test_values_of_all_magnitudes(name, first):
+    """Runs of tokens whose values are tiny, large, all equal and zero: blocks whose scales are far apart."""
+    fmt, D = CASES[name]
+    caches = []
+    for n, U, nm in ((777, 1, "p"), (301, first[-1], "s")):
+        K, V = synth.kv_tokens(45, U, n, 2, D, name=nm)
+        f = synth.bf16_bits_to_f32(V) * np.repeat(np.float32([1, 1e-6, 300, 0, 1e-3, 1e-20]), 37)[
+            np.arange(n) % 222][None, :, None, None]
+        f[:, 100:140] = 3.0
+        caches.append(Pair(fmt, U, 2, D, n).append(K, synth.to_bf16_bits(f.astype(np.float32))))
+    Q = synth.queries(46, first[-1], 8, D).reshape(first[-1], 1, 8, D)
+    close(call(*caches, first, Q, D ** -0.5), reference(*caches, first, Q, D ** -0.5))
+
+
+@pytest.mark.parametrize("first", [[0, 3], [0, 33]])
+@pytest.mark.parametrize("name", ["tiny_b16", "kivi", "hadamard"])
+def test_values_of_zero(name, first):
+    fmt, D = CASES[name]
+    caches = []
+    for n, U in ((300, 1), (200, first[-1])):
+        K, V = synth.kv_tokens(47, U, n, 2, D)
+        caches.append(Pair(fmt, U, 2, D, n).append(K, np.zeros_like(V)))
+    Q = synth.queries(48, first[-1], 8, D).reshape(first[-1], 1, 8, D)
+    # An affine token of zeros has the least scale, 1e-8, and is 1e-8 (c - mid) + 1e-8 mid with c = 0 and mid
+    # <= 7.5.  Both terms are taken with a weight rounded to 22 bits and summed in binary32 (some 2^-24 of a
+    # partial sum per step): they cancel to 2^-20 of one of them.
+    assert (call(*caches, first, Q, D ** -0.5).abs() <= 2.0 ** -20 * 7.5e-8).all()
 
 
 def test_same_bits_every_time_and_after_a_larger_call():
