@@ -36,7 +36,7 @@ Kind direct_kind()
 Kind image_kind(int D, int rows)
 {
     const int per = shr::item_rows(D), n16 = ceil_div(rows < per ? rows : per, 16);
-    return {false, per, shr::kWaves / shr::row_waves(D, n16), kImageRound};
+    return {false, per, shr::waves(D) / shr::row_waves(D, n16), kImageRound};
 }
 
 // `rows` the most that a unit of the segment has, `units` of `blocks` blocks.

@@ -18,7 +18,7 @@
 //                  images(D) blocks into images in LDS (parts(D) waves per
 //                  block), then multiply their own rows with them.  With R row
 //                  waves a wave has up to tiles(D) tiles of 16 rows and every
-//                  kWaves / R-th image.  (Two buffers with one barrier per turn
+//                  waves(D) / R-th image.  (Two buffers with one barrier per turn
 //                  leave room for half the images, and every wave that takes
 //                  part in a block repeats the work on its scales: 3 to 15%
 //                  slower, in either order of the halves.)
@@ -31,8 +31,8 @@
 // KiB fragment is one 16-byte piece per lane):
 //   keys    per-token groups: the codes, centred (c - (2^b - 1) / 2, or c -
 //           2^(b-1) when symmetric), exact in fp16, with scales and offsets s, z'
-//           beside them: S = sum_g s_g (A_g . q_g) + z'_g sum q_g, the offsets
-//           by one fp32 MFMA of four groups.  Per-channel groups: the
+//           beside them: S = sum_g s_g (A_g . q_g) + z'_g sum q_g.  Per-channel
+//           groups: the
 //           reconstructed key times a power of two, as fp16 hi + lo (22 bits);
 //   values  the reconstructed value times a power of two, hi + lo.
 // The product of the values with the probabilities (hi + lo as well) is three
@@ -63,18 +63,22 @@ constexpr float kPBits = 10.0f;  // probabilities are kept times 2^kPBits, so th
 constexpr float kNegInf = -__builtin_inff();
 
 // ---- image_kernel
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+// Waves of a workgroup, the only one on its CU.
+__host__ __device__ constexpr int waves(int D)
+{
+    return D == 64 ? 16 : 8;
+}
 
 // 16-row tiles per wave: 32 rows' accumulators and queries fit 256 registers
 // up to D = 128.
 __host__ __device__ constexpr int tiles(int D)
 {
-    return D == 256 ? 1 : 2;
+    return D == 128 ? 2 : 1;
 }
 
 __host__ __device__ constexpr int item_rows(int D)
 {
-    return 16 * tiles(D) * kWaves;
+    return 16 * tiles(D) * waves(D);
 }
 
 // Images of a turn, and waves that build one: four key and four value pieces
@@ -86,7 +90,7 @@ __host__ __device__ constexpr int images(int D)
 
 __host__ __device__ constexpr int parts(int D)
 {
-    return kWaves / images(D);
+    return waves(D) / images(D);
 }
 
 // LDS: the images, per image its scales and offsets ([group][32]
@@ -121,15 +125,15 @@ __host__ __device__ constexpr int merge_pitch(int D)
 
 __host__ __device__ constexpr int image_lds(int D, bool hilo)
 {
-    const int walk = images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + kWaves * stage_bytes(D);
-    const int merge = kWaves * 16 * (merge_pitch(D) + 2) * 4;
+    const int walk = images(D) * (image_bytes(D, hilo) + meta_bytes(D)) + waves(D) * stage_bytes(D);
+    const int merge = waves(D) * 16 * (merge_pitch(D) + 2) * 4;
     return walk > merge ? walk : merge;
 }
 
-// Waves that share an item's rows, of n16 tiles; kWaves / it take turns at the images.
+// Waves that share an item's rows, of n16 tiles; waves(D) / it take turns at the images.
 __host__ __device__ constexpr int row_waves(int D, int n16)
 {
-    int R = kWaves / images(D);
+    int R = waves(D) / images(D);
     while (R * tiles(D) < n16)
         R *= 2;
     return R;
@@ -286,19 +290,21 @@ __device__ __forceinline__ half8 centred(const uint32_t* w, int k, uint32_t cent
 }
 
 // The loads of one wave's part of a coded block: NK key pieces and NV value
-// pieces per lane, and chunk `lane` (four numbers) of the block's key and of
-// its value scales and offsets.
-template <int KB, int VB, int NK, int NV>
+// pieces per lane, and of the block's key and value scales and offsets (at most
+// D of each) D / 64 numbers in NW words.
+template <int KB, int VB, int NK, int NV, int NW>
 struct Raw {
     uint32_t k[NK * KB / 4], v[NV * VB / 4];
-    u32x4 ks, kz, vs, vz;
+    uint32_t ks[NW], kz[NW], vs[NW], vz[NW];
 };
 
-// N bytes (4 to 128, aligned to N or 16) from global memory, streaming.
+// N bytes (2 to 128, aligned to N or 16) from global memory, streaming.
 template <int N>
 __device__ __forceinline__ void load_bytes(const uint8_t* at, uint32_t* w)
 {
-    if constexpr (N == 4) {
+    if constexpr (N == 2) {
+        w[0] = __builtin_nontemporal_load((const uint16_t*)at);
+    } else if constexpr (N == 4) {
         w[0] = __builtin_nontemporal_load((const uint32_t*)at);
     } else if constexpr (N == 8) {
         const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
@@ -319,12 +325,13 @@ __device__ __forceinline__ void load_bytes(const uint8_t* at, uint32_t* w)
 template <int D, bool KH, int KB, int VB, bool M16, int PB>
 struct Builder {
     static constexpr int NKB = D / 32, NMB = D / 16, NK = 2 * NKB / PB, NV = NMB / PB;
-    typedef Raw<KB, VB, NK, NV> Loads;
+    static constexpr int NM = D / 64, ESZ = M16 ? 2 : 4;  // numbers of a lane, and their bytes
+    typedef Raw<KB, VB, NK, NV, (NM * ESZ + 3) / 4> Loads;
     const AttnParams& p;
     int unit, part, lane;
-    int nkc, nvc;      // chunks of a block's key and value scales
+    int nk, nv;        // key and value scales of a block
     bool kaff, vaff;
-    const uint8_t *k, *v, *ks, *vs;  // this lane's pieces and chunks of block 0
+    const uint8_t *k, *v, *ks, *vs;  // this lane's pieces and numbers of block 0
     long dkz, dvz;                   // offsets - scales (0 when symmetric: the scales once more)
 
     // key piece i of the lane: half block and 32-channel block
@@ -335,33 +342,21 @@ struct Builder {
         : p(p_), unit(unit_), part(part_), lane(lane_)
     {
         const size_t ub0 = (size_t)unit * (p.T >> 5);
-        constexpr int ESZ = M16 ? 2 : 4;
-        nkc = KH ? D / 4 : 8 * (D / p.k_group);
-        nvc = 8 * (D / p.v_group);
+        nk = KH ? D : 32 * (D / p.k_group);
+        nv = 32 * (D / p.v_group);
         kaff = p.k_mode == KVQ_AFFINE;
         vaff = p.v_mode == KVQ_AFFINE;
         k = (const uint8_t*)p.kc + ((ub0 * 2 + half(0)) * 64 + lane) * (NKB * KB) + kblock(0) * KB;
         v = (const uint8_t*)p.vc + (ub0 * 64 + lane) * (NMB * VB) + NV * part * VB;
-        ks = (const uint8_t*)p.ks + (ub0 * nkc + min(lane, nkc - 1)) * (4 * ESZ);
-        vs = (const uint8_t*)p.vs + (ub0 * nvc + min(lane, nvc - 1)) * (4 * ESZ);
+        ks = (const uint8_t*)p.ks + (ub0 * nk + min(NM * lane, nk - NM)) * ESZ;
+        vs = (const uint8_t*)p.vs + (ub0 * nv + min(NM * lane, nv - NM)) * ESZ;
         dkz = kaff ? (const uint8_t*)p.kz - (const uint8_t*)p.ks : 0;
         dvz = vaff ? (const uint8_t*)p.vz - (const uint8_t*)p.vs : 0;
-    }
-
-    __device__ __forceinline__ u32x4 load_chunk(const uint8_t* at) const
-    {
-        if constexpr (M16) {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2*)at);
-            return u32x4{x.x, x.y, 0u, 0u};
-        } else {
-            return __builtin_nontemporal_load((const u32x4*)at);
-        }
     }
 
     // Every lane issues the same loads whatever the block.
     __device__ __forceinline__ void load(Loads& r, int blk) const
     {
-        constexpr int ESZ = M16 ? 2 : 4;
         const uint8_t* kb = k + (size_t)blk * (2 * 64 * NKB * KB);
         if constexpr (PB == 1) {
             load_bytes<NKB * KB>(kb, r.k);
@@ -370,33 +365,38 @@ struct Builder {
             load_bytes<NK * KB>(kb, r.k);
         }
         load_bytes<NV * VB>(v + (size_t)blk * (64 * NMB * VB), r.v);
-        const uint8_t *a = ks + (size_t)blk * (nkc * 4 * ESZ), *b = vs + (size_t)blk * (nvc * 4 * ESZ);
-        r.ks = load_chunk(a);
-        r.kz = load_chunk(a + dkz);
-        r.vs = load_chunk(b);
-        r.vz = load_chunk(b + dvz);
+        const uint8_t *a = ks + (size_t)blk * (nk * ESZ), *b = vs + (size_t)blk * (nv * ESZ);
+        load_bytes<NM * ESZ>(a, r.ks);
+        load_bytes<NM * ESZ>(a + dkz, r.kz);
+        load_bytes<NM * ESZ>(b, r.vs);
+        load_bytes<NM * ESZ>(b + dvz, r.vz);
     }
 
-    // The numbers of a chunk pair: scale, and offset of the centred code.
-    // Dead slots (a chunk is four tokens of a group, unless `whole`) give zeros.
-    __device__ __forceinline__ void widen(const u32x4& s, const u32x4& z, bool aff, float mid, int live, bool whole,
+    // This lane's scales, and offsets of the centred codes.  Dead tokens (number i
+    // is token i % 32 of a group, unless `whole`) give zeros.
+    __device__ __forceinline__ void widen(const uint32_t* s, const uint32_t* z, bool aff, float mid, int live, bool whole,
                                           float* sv, float* zv) const
     {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < NM; ++e) {
             sv[e] = M16 ? f16_bits_to_f32((uint16_t)(s[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(s[e]);
             zv[e] = M16 ? f16_bits_to_f32((uint16_t)(z[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(z[e]);
-            const bool on = whole || 4 * (lane & 7) + e < live;
+            const bool on = whole || ((NM * lane + e) & 31) < live;
             sv[e] = on ? sv[e] : 0.0f;
             zv[e] = on && aff ? fmaf(mid, sv[e], zv[e]) : 0.0f;
         }
     }
 
-    // A chunk pair times f to st (scales) and st + D (offsets).
-    __device__ __forceinline__ void put_chunk(float* st, const float* sv, const float* zv, float f) const
+    // This lane's numbers (of n) times f to st (scales) and st + D (offsets).
+    __device__ __forceinline__ void put(float* st, const float* sv, const float* zv, float f, int n) const
     {
-        *(float4*)(st + 4 * lane) = float4{sv[0] * f, sv[1] * f, sv[2] * f, sv[3] * f};
-        *(float4*)(st + D + 4 * lane) = float4{zv[0] * f, zv[1] * f, zv[2] * f, zv[3] * f};
+        if (NM * lane < n) {
+#pragma unroll
+            for (int e = 0; e < NM; ++e) {
+                st[NM * lane + e] = sv[e] * f;
+                st[D + NM * lane + e] = zv[e] * f;
+            }
+        }
     }
 
     // A power of two that brings the block's largest magnitude |offset| + mid
@@ -405,9 +405,9 @@ struct Builder {
     {
         float top = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < NM; ++e)
             top = fmaxf(top, fmaf(mid, sv[e], fabsf(zv[e])));
-        return scale_to_range(wave_max(lane < n ? top : 0.0f));
+        return scale_to_range(wave_max(NM * lane < n ? top : 0.0f));
     }
 
     // The key scales of a coded block: per-token groups (times sm_scale log2 e) to
@@ -415,17 +415,15 @@ struct Builder {
     // and pre) to st, [channel].  Returns what the scores of the latter take.
     __device__ __forceinline__ float key_scales(const Loads& r, int live, float* meta, float* st, float pre = 1.0f) const
     {
-        float sv[4], zv[4];
+        float sv[NM], zv[NM];
         const float mid = coding<KB>(kaff).mid;
         widen(r.ks, r.kz, kaff, mid, live, KH, sv, zv);
         if constexpr (KH) {
-            const float f = range_scale(sv, zv, mid, nkc) * pre;
-            if (lane < nkc)
-                put_chunk(st, sv, zv, f);
+            const float f = range_scale(sv, zv, mid, nk) * pre;
+            put(st, sv, zv, f, nk);
             return p.sm_log2 * (1.0f / f);
         } else {
-            if (lane < nkc)
-                put_chunk(meta, sv, zv, p.sm_log2);
+            put(meta, sv, zv, p.sm_log2, nk);
             return 0.0f;
         }
     }
@@ -434,12 +432,11 @@ struct Builder {
     // two (pre included) that they were multiplied with.
     __device__ __forceinline__ float value_scales(const Loads& r, int live, float* st, float pre = 1.0f) const
     {
-        float sv[4], zv[4];
+        float sv[NM], zv[NM];
         const float mid = coding<VB>(vaff).mid;
         widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
-        const float f = range_scale(sv, zv, mid, nvc) * pre;
-        if (lane < nvc)
-            put_chunk(st, sv, zv, f);
+        const float f = range_scale(sv, zv, mid, nv) * pre;
+        put(st, sv, zv, f, nv);
         return f;
     }
 
@@ -568,9 +565,12 @@ struct Builder {
     {
         if (part != 0)
             return;
-        if (!KH && lane < nkc) {
-            const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f}, none[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            put_chunk(meta, one, none, p.sm_log2);
+        if constexpr (!KH) {
+            if (NM * lane < nk) {
+#pragma unroll
+                for (int e = 0; e < NM; ++e)
+                    meta[NM * lane + e] = p.sm_log2;
+            }
         }
         if (lane == 0) {
             meta[2 * D] = 1.0f;
@@ -618,9 +618,13 @@ template <int D, int KG, bool ROT, int CT, bool DIRECT>
 struct Rows {
     static constexpr int NKB = D / 32, NMB = D / 16;
     static constexpr bool KH = KG == 0;
-    static constexpr int KS = KH ? NKB : KG, NG = NKB / KS, NZ = (NG + 3) / 4;
+    static constexpr int KS = KH ? NKB : KG, NG = NKB / KS;
+    // Offsets of up to two groups are added by vector operations (eight per group
+    // and tile, 32 cycles), of more by an fp32 MFMA per four (two of 32 cycles).
+    static constexpr bool ZM = NG > 2;
+    static constexpr int NZ = ZM ? (NG + 3) / 4 : NG;
     half8 q[CT][NKB], ql[ROT ? CT : 1][ROT ? NKB : 1];
-    float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg
+    float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg (ZM), or over group j
     floatx4 oacc[CT][NMB];
     float zacc[DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
     float m[CT], lsum[CT];   // running max (log2 units), lane partial sum (times 2^kPBits)
@@ -699,9 +703,9 @@ struct Rows {
         if constexpr (!KH) {
 #pragma unroll
             for (int j = 0; j < NZ; ++j)
-                qz[c][j] = 0.0f;
+                qz[c][j] = ZM ? 0.0f : sum_rows(sum[j]);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
+            for (int g = 0; ZM && g < NG; ++g) {
                 const float s = sum_rows(sum[g]);
                 qz[c][g / 4] = qg == g % 4 ? s : qz[c][g / 4];
             }
@@ -836,9 +840,36 @@ struct Rows {
         return *(const half8*)(fb + at);
     }
 
+    // S += offset x sum of the group's query, of half e: all groups, and one group.
+    template <int NT>
+    __device__ __forceinline__ void add_offset_products(floatx4* S, const float* meta, int e, int lane)
+    {
+        // row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
+        const int qg = lane >> 4, hh = lane & 15, tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
+#pragma unroll
+        for (int j = 0; j < NZ; ++j) {
+            const float z = meta[D + 32 * min(4 * j + qg, NG - 1) + tok];  // (times a zero sum past the last group)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                S[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z, qz[c][j], S[c], 0, 0, 0);
+        }
+    }
+
+    template <int NT>
+    __device__ __forceinline__ void add_group_offset(floatx4* S, const float* meta, int g, int e, int lane)
+    {
+        const floatx4 z = *(const floatx4*)(meta + D + 32 * g + 8 * (lane >> 4) + 4 * e);
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                S[c][i] = fmaf(z[i], qz[c][g], S[c][i]);
+    }
+
     // The scores of the image at fb; the ring holds its first fragments.
     template <int NT>
-    __device__ __forceinline__ void image_scores(half8* ring, const uint8_t* fb, const float* meta, int lane, float (*l)[8])
+    __device__ __forceinline__ void image_scores(half8* ring, const uint8_t* fb, const float* meta, bool affine, int lane,
+                                                 float (*l)[8])
     {
         const int qg = lane >> 4, hh = lane & 15;
         constexpr int PER = KH ? 2 : 1, GF = KS * PER;  // fragments of a key piece, and of a group
@@ -851,16 +882,9 @@ struct Rows {
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
                     S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (!KH) {
-                    // offsets of four groups at once: row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
-                    const int tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
-#pragma unroll
-                    for (int j = 0; j < NZ; ++j) {
-                        const float z = meta[D + 32 * min(4 * j + qg, NG - 1) + tok];  // (times a zero sum past the last group)
-#pragma unroll
-                        for (int c = 0; c < NT; ++c)
-                            S[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z, qz[c][j], S[c], 0, 0, 0);
-                    }
+                if constexpr (!KH && ZM) {
+                    if (affine)
+                        add_offset_products<NT>(S, meta, e, lane);
                 }
             }
             if (kk % GF == 0) {
@@ -889,6 +913,10 @@ struct Rows {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         S[c][i] = KH ? acc[c][i] * ksm : fmaf(s4[i], acc[c][i], S[c][i]);
+                if constexpr (!KH && !ZM) {
+                    if (affine)
+                        add_group_offset<NT>(S, meta, g, e, lane);
+                }
             }
             if (kk == NKF / 2 - 1) {
 #pragma unroll
@@ -929,17 +957,16 @@ struct Rows {
     // l[4 e + i]: the score of token 8 qg + 4 e + i, in log2 units, from key(e, kb)
     // and meta's scales.
     template <class Key>
-    __device__ __forceinline__ void group_scores(Key key, const float* meta, int lane, float* l)
+    __device__ __forceinline__ void group_scores(Key key, const float* meta, bool affine, int lane, float* l)
     {
-        const int qg = lane >> 4, hh = lane & 15;
+        const int qg = lane >> 4;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             floatx4 S = {0.0f, 0.0f, 0.0f, 0.0f};
-            // offsets of four groups at once: row hh of the half is token 8 (hh / 4) + 4 e + hh % 4
-            const int tok = 8 * (hh >> 2) + 4 * e + (hh & 3);
-#pragma unroll
-            for (int j = 0; j < NZ; ++j)  // (times a zero sum past the last group)
-                S = __builtin_amdgcn_mfma_f32_16x16x4f32(meta[D + 32 * min(4 * j + qg, NG - 1) + tok], qz[0][j], S, 0, 0, 0);
+            if constexpr (ZM) {
+                if (affine)
+                    add_offset_products<1>(&S, meta, e, lane);
+            }
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -955,6 +982,10 @@ struct Rows {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     S[i] = fmaf(s4[i], acc[i], S[i]);
+                if constexpr (!ZM) {
+                    if (affine)
+                        add_group_offset<1>(&S, meta, g, e, lane);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -1212,10 +1243,10 @@ __device__ __forceinline__ void merge_row(const SharedParams& sp, const float* l
 // ROWS (of both kernels): the format has fp16 tokens (their conversion in the
 // loop costs the other formats registers that the loop spills).
 template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
-__global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
+__global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(SharedParams sp)
 {
     constexpr bool KH = KG == 0;
-    constexpr int CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16;
+    constexpr int W = waves(D), CT = tiles(D), NI = images(D), PB = parts(D), NMB = D / 16;
     constexpr int BI = image_bytes(D, KH), BM = meta_bytes(D);
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
@@ -1242,7 +1273,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     // ---- this wave's rows and its images of a turn
     const int nt16 = (left + 15) >> 4;
     const int R = row_waves(D, nt16);
-    const int BW = kWaves / R, rw = wave / BW, bw = wave - rw * BW;
+    const int BW = W / R, rw = wave / BW, bw = wave - rw * BW;
     const int nt = nt16 > rw ? (nt16 - rw + R - 1) / R : 0;  // tiles rw, rw + R, ..
     Rows<D, KG, ROT, CT, false> T;
     T.lim0 = it.lim + (it.causal ? (it.r0 + 16 * rw) / G : 0);
@@ -1301,10 +1332,11 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
                 const uint8_t *fb = lds + i * BI + 16 * lane, *next = j < n ? lds + j * BI + 16 * lane : fb;
                 const float* meta = (const float*)(metas + i * BM);
                 const Span s(p, bl, v + i);
+                const bool affine = B.kaff && (!ROWS || bl.coded(v + i));  // (fp16 rows have no offsets)
                 const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
                 float l[NT][8], shift[NT], back;
                 half8 ph[NT], pl[NT];
-                T.template image_scores<NT>(ring, fb, meta, lane, l);
+                T.template image_scores<NT>(ring, fb, meta, affine, lane, l);
                 T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
                 T.template probabilities<NT>(l, shift, back, ph, pl);
                 T.template image_values<NT>(ring, fb, next, ph, pl);
@@ -1326,7 +1358,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
     // ---- partials: of each wave when its rows are its own, else merged in LDS
     const float inv = T.inverse();
     float* lo = (float*)lds;                          // [waves][16][pitch]
-    float* lml = lo + kWaves * 16 * merge_pitch(D);   // [waves][16][2]
+    float* lml = lo + W * 16 * merge_pitch(D);   // [waves][16][2]
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         if (R * c >= nt16)
@@ -1352,7 +1384,7 @@ __global__ __launch_bounds__(kThreads, 2) void image_kernel(SharedParams sp)
         if (qg == 0)
             *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
         sync_lds();
-        for (int idx = threadIdx.x; idx < 16 * R * (D / 4); idx += kThreads) {
+        for (int idx = threadIdx.x; idx < 16 * R * (D / 4); idx += 64 * W) {
             const int row = idx / (D / 4), d = 4 * (idx % (D / 4)), w = row >> 4, rr = 16 * (w + R * c) + (row & 15);
             if (rr < left)
                 merge_row<D>(sp, lo, lml, w * BW, w * BW + BW, row & 15, d,
@@ -1415,7 +1447,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
             if constexpr (KG == 0)
                 T.template channel_scores<true>(key, meta, ksm, lane, l[0]);
             else
-                T.group_scores(key, meta, lane, l[0]);
+                T.group_scores(key, meta, B.kaff, lane, l[0]);
             T.template settle<1>(l, f, s.t0, s.off, s.live, lane, &shift, &back);
             T.exponentials(0, l[0], shift, back, pv);
             T.group_values([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
@@ -1462,7 +1494,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
             if constexpr (KG == 0)
                 T.template channel_scores<false>(key, nullptr, p.sm_log2, lane, l[0]);
             else
-                T.group_scores(key, meta, lane, l[0]);
+                T.group_scores(key, meta, false, lane, l[0]);
             T.template settle<1>(l, 1.0f, s.t0, s.off, s.live, lane, &shift, &back);
             T.exponentials(0, l[0], shift, back, pv);
             T.row_values([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
@@ -1499,7 +1531,7 @@ hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
     constexpr bool kWindow = KG == 0;  // (per-channel keys come with a window)
     if (p.image_items > 0)
         launch_kernel(rows ? image_kernel<D, KG, KB, VB, M16, ROT, true> : image_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
-                      dim3(p.image_items), dim3(kThreads), (size_t)image_lds(D, KG == 0), stream, p);
+                      dim3(p.image_items), dim3(64 * waves(D)), (size_t)image_lds(D, KG == 0), stream, p);
     if (p.direct_items > 0)
         launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true> : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow>, dim3(p.direct_items), dim3(kDirectThreads),
                       (size_t)direct_lds(D, rows), stream, p);
