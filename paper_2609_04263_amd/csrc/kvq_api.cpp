@@ -1028,7 +1028,7 @@ kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* 
 // those tokens have to be in the suffix.
 static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
                               int C, int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, bool self,
-                              void* stream)
+                              void* stream, int kernels = 0)
 {
     const kvq_status st = shared_caches(prefix, suffix, C, H_q);
     if (st != KVQ_OK)
@@ -1061,7 +1061,7 @@ static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, 
     p.rot_c = rotation_constant(suffix->D);
     for (int g = 0; g <= P; ++g)
         p.first[g] = first ? first[g] : B / P * g;
-    kvq::shared_plan(&p, suffix->D, B);
+    kvq::shared_plan(&p, suffix->D, B, kernels);
     return kvq::launch_shared(p, suffix->D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
@@ -1076,6 +1076,13 @@ kvq_status kvq_prefill_attn_shared(const kvq_cache* prefix, const kvq_cache* suf
                                    size_t ws_bytes, void* stream)
 {
     return shared_attn(prefix, suffix, first, Q, C, H_q, sm_scale, O, workspace, ws_bytes, true, stream);
+}
+
+kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                    int C, int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, int self,
+                                    void* stream, int kernels)
+{
+    return shared_attn(prefix, suffix, first, Q, C, H_q, sm_scale, O, workspace, ws_bytes, self != 0, stream, kernels);
 }
 
 // Block images per (b, h) unit that a chunked prefill reconstructs: the sink

@@ -251,7 +251,7 @@ struct SharedParams {
     int tile0[kSharedPrefixes + 1];  // first tile of each group
 };
 // Fills S, bps, tiles0, items0, tile0 and the kernels' items from the rest.
-void shared_plan(SharedParams* p, int D, int B);
+void shared_plan(SharedParams* p, int D, int B, int kernels);
 // Upper bound of S0 + S1 for any lengths and groups.
 int shared_split_bound(int B, int H, int D, int C, int G);
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream);
@@ -265,5 +265,11 @@ extern "C" int kvq_internal_project_tile(int M, int N);
 // destination -1), at most 3 B_dst + 2 kGatherBatch of them; returns their number.
 extern "C" int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src, int in_place, int32_t* pairs,
                                        int* ordered);
+// A call over a shared prefix as its two entry points make it (`self`: the
+// queries are the suffixes' newest tokens), by the direct (1) or the image (2)
+// kernel alone.
+extern "C" kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
+                                               const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
+                                               size_t ws_bytes, int self, void* stream, int kernels);
 extern "C" int kvq_internal_prefill_ranges(const kvq_cache* cache, int C, int H_q);
 extern "C" int kvq_internal_prefill_tile_rows(const kvq_cache* cache, int C, int H_q);

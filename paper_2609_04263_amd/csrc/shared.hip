@@ -39,24 +39,21 @@ Kind image_kind(int D, int rows)
     return {false, per, shr::waves(D) / shr::row_waves(D, n16), kImageRound};
 }
 
-// `rows` the most that a unit of the segment has, `units` of `blocks` blocks.
-// The direct kernel converts the codes once per 16 rows, the image kernel once
-// per 128 or 256, but begins with all waves converting and ends with the merge of
-// a wave's partials, which a range of a few images does not repay.  Two tiles
-// of 16 rows are always faster direct, three and four when the image kernel's
-// ranges would be two turns or less.  Direct / image, 8192 tokens, us:
-//                    32 rows               64 rows
-//                    1 prefix  8 prefixes  1 prefix (ranges of)  8 prefixes
-//     D = 64         19 / 25   30 / 35     20 / 26 (4 blocks)    49 / 42 (32 blocks)
-//     D = 128        26 / 30   52 / 52     33 / 43 (8 blocks)
-//     D = 256        49 / 46   98 / 98     72 / 65 (8 blocks)
-Kind kind_of(int D, int rows, long long units, int blocks)
+// Whether the direct kernel takes everything: `rows` the most that a unit of the
+// prefix has, `work` the 32-token blocks of all 16-row tiles of both segments.
+// The direct kernel converts a block's codes for every tile, the image kernel once
+// per 128 or 256 rows, which costs it half as much per tile and block (D = 256:
+// two thirds); but a call has to pay its launch beside the direct one's, the
+// conversion before its first product, the merge of a wave's partials and the
+// join of more of them: 16 to 25 us.  Direct / image, us, at `work` in 1024s:
+//     D = 64    64 rows  15 / 21 (4)   33 / 36 (32)   256 rows  15 / 29 (8)   21 / 32 (16)
+//     D = 128   64 rows  23 / 32 (8)   94 / 91 (64)   256 rows  33 / 50 (16)  51 / 59 (32)
+//     D = 256   64 rows  43 / 48 (8)  205 / 181 (64)  256 rows  54 / 58 (8)   73 / 68 (16)
+// Units of two tiles would leave most of an image kernel's waves idle: 32 rows of
+// 8192 tokens, 8 prefixes, 21 / 30, 52 / 70 and 110 / 141 us.
+bool all_direct(int D, int rows, long long work)
 {
-    const Kind k = image_kind(D, rows);
-    return rows <= 2 * shr::kDirectRows ||
-                   (rows <= 4 * shr::kDirectRows && units * blocks <= 2ll * shr::images(D) * k.round)
-               ? direct_kind()
-               : k;
+    return rows <= 2 * shr::kDirectRows || work <= (D == 256 ? 12 : 40) * 1024;
 }
 
 // Ranges that a segment of `tiles` tiles is cut into, at most.
@@ -169,18 +166,23 @@ void launch_join(const SharedParams& p, hipStream_t stream)
 // begin where others end, and more of them only add their fixed cost (200 tokens
 // after 2048, D = 64: 64 us with one range of a suffix, 76 with two).  If they
 // leave nothing the suffix is a round of its own (512 tokens after 8192,
-// D = 256: 389 us with one range of a suffix, 377 with two).
-void shared_plan(SharedParams* p, int D, int B)
+// D = 256: 389 us with one range of a suffix, 377 with two).  `kernels`: 0 by
+// the rule above, 1 and 2 the direct and the image kernel only.
+void shared_plan(SharedParams* p, int D, int B, int kernels)
 {
     const AttnParams &a = p->seg[0], &b = p->seg[1];
-    int most = 0;
-    for (int g = 0; g < p->P; ++g)
-        most = p->first[g + 1] - p->first[g] > most ? p->first[g + 1] - p->first[g] : most;
     const auto blocks = [](const AttnParams& s) { return ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32); };
-    const int nb[2] = {blocks(a), blocks(b)};
-    // (a unit of the suffix never has more rows than its group's of the prefix: no direct prefix beside an image suffix)
-    const Kind k0 = kind_of(D, most * p->C * a.G, (long long)a.H * p->P, nb[0]);
-    const Kind kind[2] = {k0, k0.direct ? k0 : kind_of(D, p->C * a.G, (long long)a.H * B, nb[1])};
+    const int nb[2] = {blocks(a), blocks(b)}, own = p->C * a.G;
+    int most = 0;
+    long long work = (long long)B * a.H * ceil_div(own, shr::kDirectRows) * nb[1];
+    for (int g = 0; g < p->P; ++g) {
+        const int rows = (p->first[g + 1] - p->first[g]) * own;
+        most = rows > most ? rows : most;
+        work += (long long)a.H * ceil_div(rows, shr::kDirectRows) * nb[0];
+    }
+    const bool direct = kernels ? kernels == 1 : all_direct(D, most, work);
+    const Kind kind[2] = {direct ? direct_kind() : image_kind(D, most),
+                          direct || (!kernels && own <= 2 * shr::kDirectRows) ? direct_kind() : image_kind(D, own)};
     p->tiles0 = 0;
     for (int g = 0; g < p->P; ++g) {
         p->tile0[g] = p->tiles0;

@@ -12,6 +12,8 @@ relatively; its own sums add as much again.  2^-14 = 6e-5 of the norm leaves a
 factor of six; without the lo half of an operand the error would be 2^-12.  A
 larger softmax scale scales it.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -84,7 +86,18 @@ def reference(prefix, suffix, first, Q, sm):
 GUARD = 64
 
 
-def call(prefix, suffix, first, Q, sm, chunk=None, ws=None, **kw):
+def call_kernel(prefix, suffix, first, Q, H_q, C, sm, O, ws, chunk, kernels):
+    """The same call by one of the two kernels alone (1: direct, 2: image)."""
+    from paper_2609_04263_amd import kvq
+    f = kvq._lib.kvq_internal_shared_attn
+    V, I = ctypes.c_void_p, ctypes.c_int
+    f.argtypes = [V, V, V, V, I, I, ctypes.c_float, V, V, ctypes.c_size_t, I, V, I]
+    arr = None if first is None else (ctypes.c_int32 * len(first))(*first)
+    assert f(prefix.handle, suffix.handle, arr, Q.data_ptr(), C, H_q, sm, O.data_ptr(), ws.data_ptr(), ws.numel(),
+             int(chunk), torch.cuda.current_stream().cuda_stream, kernels) == 0
+
+
+def call(prefix, suffix, first, Q, sm, chunk=None, ws=None, kernels=0, **kw):
     """The output of a shared call, with the floats around it checked."""
     B, C, H_q, D = Q.shape
     s, p = suffix.gpu, prefix.gpu
@@ -96,7 +109,9 @@ def call(prefix, suffix, first, Q, sm, chunk=None, ws=None, **kw):
     dq = dev_bf16(Q)
     if chunk is None:
         chunk = C > 1
-    if chunk:
+    if kernels:
+        call_kernel(p, s, first, dq, H_q, C, sm, O, ws, chunk, kernels)
+    elif chunk:
         s.prefill_attn_shared(p, dq, C, H_q, sm, O, ws, first=first, **kw)
     else:
         s.decode_attn_shared(p, dq, H_q, sm, O, ws, first=first, **kw)
@@ -126,8 +141,10 @@ def run(name, first, n_p, n_s, G=4, H=2, C=1, seed=0, sm=None, chunk=None):
     sm0 = D ** -0.5
     sm = sm0 if sm is None else sm
     got = call(prefix, suffix, first, Q, sm, chunk)
-    close(got, reference(prefix, suffix, first, Q, sm), max(1.0, sm / sm0),
-          f"{name} first={first} n={n_p}+{n_s} G={G} C={C}")
+    want = reference(prefix, suffix, first, Q, sm)
+    for k, o in ((0, got), (1, call(prefix, suffix, first, Q, sm, chunk, kernels=1)),
+                 (2, call(prefix, suffix, first, Q, sm, chunk, kernels=2))):
+        close(o, want, max(1.0, sm / sm0), f"{name} first={first} n={n_p}+{n_s} G={G} C={C} kernels={k}")
     return prefix, suffix, Q, got
 
 
@@ -139,15 +156,22 @@ def test_decode(name, n_p, n_s):
 
 @pytest.mark.parametrize("name", list(CASES))
 def test_decode_of_many_samples(name):
-    # groups of 36 and 124 rows: the prefix is converted once for all of them
+    # groups of 36 and 124 rows
     run(name, [0, 9, 40], 1500, 70, seed=3)
 
 
-@pytest.mark.parametrize("n_p", [100, 4500])
-@pytest.mark.parametrize("G,count", [(2, 16), (3, 11), (2, 32), (5, 13)])
-def test_rows_between_the_kernels(G, count, n_p):
-    # 32, 33, 64 and 65 rows of eight units, of a few blocks and of many
-    run("gqa12b", [0, count, 2 * count], n_p, 40, G=G, H=4, seed=4)
+@pytest.mark.parametrize("G,count", [(2, 16), (3, 11), (2, 32), (5, 13), (16, 8), (15, 9), (16, 16), (15, 18)])
+@pytest.mark.parametrize("name", ["tiny_b16", "gqa12b", "hadamard"])
+def test_rows_around_whole_tiles(name, G, count):
+    # one to sixteen tiles and a row more, of one wave, several and all of a workgroup
+    run(name, [0, count, 2 * count], 700, 40, G=G, H=1, seed=4)
+
+
+@pytest.mark.parametrize("C,n_s", [(40, 40), (3, 70)])
+def test_enough_work_for_the_image_kernel(C, n_s):
+    # 480 tiles of 54 blocks; the suffix has units of 640 rows, and of 48
+    first = [0, 4 * (120 // C)]
+    run("gqa12b", first, 1700, n_s, G=16, H=1, C=C, seed=5)
 
 
 @pytest.mark.parametrize("name", list(CASES))
@@ -250,7 +274,9 @@ def test_the_largest_scores_on_one_side(name, span):
     Q = synth.queries(42, B, 2 * H, D).reshape(B, 1, 2 * H, D)
     Q = synth.to_bf16_bits(synth.bf16_bits_to_f32(Q) * np.float32(0.25) + u)
     # (partial sums of these scores reach 8 (40 + 5) units: nine times the bound's)
-    close(call(*caches, [0, B], Q, D ** -0.5), reference(*caches, [0, B], Q, D ** -0.5), 9.0)
+    want = reference(*caches, [0, B], Q, D ** -0.5)
+    for k in range(3):
+        close(call(*caches, [0, B], Q, D ** -0.5, kernels=k), want, 9.0, f"kernels={k}")
 
 
 @pytest.mark.parametrize("first", [[0, 3], [0, 33]])
@@ -267,7 +293,9 @@ def test_values_of_all_magnitudes(name, first):
         f[:, 100:140] = 3.0
         caches.append(Pair(fmt, U, 2, D, n).append(K, synth.to_bf16_bits(f.astype(np.float32))))
     Q = synth.queries(46, first[-1], 8, D).reshape(first[-1], 1, 8, D)
-    close(call(*caches, first, Q, D ** -0.5), reference(*caches, first, Q, D ** -0.5))
+    want = reference(*caches, first, Q, D ** -0.5)
+    for k in range(3):
+        close(call(*caches, first, Q, D ** -0.5, kernels=k), want, what=f"kernels={k}")
 
 
 @pytest.mark.parametrize("first", [[0, 3], [0, 33]])
@@ -282,7 +310,8 @@ def test_values_of_zero(name, first):
     # An affine token of zeros has the least scale, 1e-8, and is 1e-8 (c - mid) + 1e-8 mid with c = 0 and mid
     # <= 7.5.  Both terms are taken with a weight rounded to 22 bits and summed in binary32 (some 2^-24 of a
     # partial sum per step): they cancel to 2^-20 of one of them.
-    assert (call(*caches, first, Q, D ** -0.5).abs() <= 2.0 ** -20 * 7.5e-8).all()
+    for k in range(3):
+        assert (call(*caches, first, Q, D ** -0.5, kernels=k).abs() <= 2.0 ** -20 * 7.5e-8).all(), k
 
 
 def test_same_bits_every_time_and_after_a_larger_call():
