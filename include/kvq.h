@@ -341,11 +341,12 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * A prefix and its suffix are attended as if they were one cache (sinks,
  * window and coded groups are those of the two caches as they are: a suffix
  * has sink tokens and a window of its own).  The codes of a prefix are read
- * once per 32 query rows of its group instead of once per sequence.  H_q as
- * for kvq_decode_attn (H_q / H_kv <= 16); products and their limits as there,
- * and the reconstructed keys of per-channel formats below 65504 in magnitude.
- * The sums run in an order that depends on the shapes and lengths alone, so a
- * call gives the same bits every time. */
+ * once per 16 query rows (sequence, query, head of a group) of its group, of
+ * calls of much work once per 128 (D = 256) or 256, instead of once per
+ * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16), and its limits.
+ * Products have 22 bits or more, sums are fp32 and run in an order that depends
+ * on the shapes, the groups and the lengths alone, so a call gives the same
+ * bits every time. */
 
 /* Workspace bytes for calls of up to C queries per sequence at any lengths and
  * groups of these caches (contents need no initialization; calls that share a

@@ -13,8 +13,8 @@ KVQ_FAMILY(256, 0) KVQ_FAMILY(256, 1) KVQ_FAMILY(256, 2) KVQ_FAMILY(256, 4) KVQ_
 
 namespace {
 
-// Work items of a round: one image_kernel workgroup per CU, eight wave pairs of
-// direct_kernel workgroups.
+// Work items of a round: one image_kernel workgroup per CU, two direct_kernel
+// workgroups (three or four: up to 20% slower).
 constexpr int kImageRound = 256, kDirectRound = 512;
 
 int ceil_div(int a, int b)

@@ -11,37 +11,48 @@
 // row's partials of both segments:
 //     M = max m,  O = sum 2^(m - M) o / sum 2^(m - M) l.
 // So the codes of a prefix are read once per tile of its group's rows instead
-// of once per sequence.  Two kernels:
+// of once per sequence.  Two kernels (shared.hip has the rule):
 //
-//   image_kernel   units of many rows (more than 32, or 64).  Eight waves, two per SIMD; up to
-//                  128 tiles(D) rows.  In turns, the waves convert the next
-//                  images(D) blocks into images in LDS (parts(D) waves per
-//                  block), then multiply their own rows with them.  With R row
-//                  waves a wave has up to tiles(D) tiles of 16 rows and every
-//                  waves(D) / R-th image.  (Two buffers with one barrier per turn
-//                  leave room for half the images, and every wave that takes
-//                  part in a block repeats the work on its scales: 3 to 15%
-//                  slower, in either order of the halves.)
-//   direct_kernel  units of few rows (a suffix's queries, few samples), 16 at a
-//                  time: four waves, each with blocks of its own, convert codes
-//                  into operands in registers.
+//   image_kernel   much work.  One workgroup per CU, of eight waves (sixteen at
+//                  D = 64) and up to 16 tiles(D) waves(D) rows.  In turns, the
+//                  waves convert the next images(D) blocks into images in LDS
+//                  (parts(D) waves per block), then multiply their own rows with
+//                  them.  With R row waves a wave has up to tiles(D) tiles of 16
+//                  rows and every waves(D) / R-th image.  (Two buffers with one
+//                  barrier per turn leave room for half the images, and every
+//                  wave that takes part in a block repeats the work on its
+//                  scales: 3 to 15% slower, in either order of the halves.)
+//   direct_kernel  little work, or few rows per unit (a suffix's queries, few
+//                  samples): 16 rows, four waves, each with blocks of its own,
+//                  whose codes become operands in registers.
 //
-// An image (or a converted block) holds operand fragments of
-// v_mfma_f32_16x16x32_f16 in the order in which the cache stores its codes (a 1
-// KiB fragment is one 16-byte piece per lane):
-//   keys    per-token groups: the codes, centred (c - (2^b - 1) / 2, or c -
-//           2^(b-1) when symmetric), exact in fp16, with scales and offsets s, z'
-//           beside them: S = sum_g s_g (A_g . q_g) + z'_g sum q_g.  Per-channel
-//           groups: the
-//           reconstructed key times a power of two, as fp16 hi + lo (22 bits);
-//   values  the reconstructed value times a power of two, hi + lo.
-// The product of the values with the probabilities (hi + lo as well) is three
-// MFMAs, all but the 2^-22 of lo x lo.  Values as codes with p s as the other
-// operand take two, but cost each tile 40 vector operations per value group,
-// and a bias in the codes costs precision where outputs are small beside the
-// values: 32768 tokens of flat attention were 4.7e-4 off with decode
-// attention's operands and 1e-6 with these.
+// Operands are in the order in which the cache stores its codes, that of
+// v_mfma_f32_16x16x32_f16 (a 1 KiB fragment is one 16-byte piece per lane).
+// Codes are centred (c - (2^b - 1) / 2, or c - 2^(b-1) when symmetric), exact in
+// fp16; s and z' are a group's scale and the offset of its centred codes:
+//   keys in per-token groups
+//           the codes: S = sum_g s_g (A_g . q_g) + z'_g sum q_g;
+//   keys with per-channel scales, values
+//           image_kernel: reconstructed, times a power of two, as fp16 hi + lo
+//           (22 bits); direct_kernel: the codes, and the other side takes the
+//           scales: (q s) . c + q . z', (p s) . c + p . z', q s and p s as hi + lo.
+// The product of reconstructed values with the probabilities (hi + lo as well) is
+// three MFMAs, all but the 2^-22 of lo x lo, that with codes two.  But the scaled
+// side costs a tile 24 vector operations (96 cycles) per value group and block
+// where an image shares the 50 of a reconstructed fragment among up to 16 tiles.
+// Direct, D = 256, groups of 64: 55 us with reconstructed values, 46 with codes.
+// (Codes that are not centred cost precision where outputs are small beside the
+// values: 32768 tokens of flat attention were 4.7e-4 off with decode attention's
+// operands and are 4e-7 with these.)
 // fp16 tokens (window, sink) are operands as they are, with a lo half of zero.
+//
+// What bounds them (MI355X): image_kernel, 64 sequences x 4 heads per KV head, 32768
+// rotated tokens at D = 128, 102 us: the matrix pipes 0.40 and the vector pipes 0.36 of
+// its waves' time, which add up instead of overlapping whatever the waves' order,
+// priority or number (sixteen waves at D = 128: 15% slower); without LDS reads 2% faster.
+// 850 TFLOP/s of executed products, where a large library product reaches 1160.
+// direct_kernel: vector operations of the conversions, and at small sizes the
+// latency of one block after another.
 //
 // Softmax: online per column in base 2, the running maximum raised only when a
 // block exceeds it by more than kTau; probabilities are at most 2^(kTau +
@@ -63,14 +74,15 @@ constexpr float kPBits = 10.0f;  // probabilities are kept times 2^kPBits, so th
 constexpr float kNegInf = -__builtin_inff();
 
 // ---- image_kernel
-// Waves of a workgroup, the only one on its CU.
+// Waves of a workgroup, the only one on its CU, and 16-row tiles of a wave.  The
+// accumulators and queries of 32 rows at D = 128 and of 16 at D = 256 fit the
+// 256 registers of two waves per SIMD; at D = 64 16 rows fit the 128 of four (200
+// tokens after 2048: 3% faster than 32 rows in two).
 __host__ __device__ constexpr int waves(int D)
 {
     return D == 64 ? 16 : 8;
 }
 
-// 16-row tiles per wave: 32 rows' accumulators and queries fit 256 registers
-// up to D = 128.
 __host__ __device__ constexpr int tiles(int D)
 {
     return D == 128 ? 2 : 1;
