@@ -16,6 +16,7 @@ namespace {
 // Work items of a round: one image_kernel workgroup per CU, two direct_kernel
 // workgroups (three or four: up to 20% slower).
 constexpr int kImageRound = 256, kDirectRound = 512;
+constexpr int kTile = 16;  // rows of an MFMA
 
 int ceil_div(int a, int b)
 {
@@ -28,9 +29,9 @@ struct Kind {
     int per, step, round;  // rows per item, blocks that a range is a multiple of, items of a round
 };
 
-Kind direct_kind()
+Kind direct_kind(int D, int bits, bool fp16)
 {
-    return {true, shr::kDirectRows, shr::kDirectWaves, kDirectRound};
+    return {true, kTile * shr::direct_tiles(D, bits, fp16), shr::kDirectWaves, kDirectRound};
 }
 
 Kind image_kind(int D, int rows)
@@ -53,7 +54,7 @@ Kind image_kind(int D, int rows)
 // 8192 tokens, 8 prefixes, 21 / 30, 52 / 70 and 110 / 141 us.
 bool all_direct(int D, int rows, long long work)
 {
-    return rows <= 2 * shr::kDirectRows || work <= (D == 256 ? 12 : 40) * 1024;
+    return rows <= 2 * kTile || work <= (D == 256 ? 12 : 40) * 1024;
 }
 
 // Ranges that a segment of `tiles` tiles is cut into, at most.
@@ -174,15 +175,16 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
     const auto blocks = [](const AttnParams& s) { return ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32); };
     const int nb[2] = {blocks(a), blocks(b)}, own = p->C * a.G;
     int most = 0;
-    long long work = (long long)B * a.H * ceil_div(own, shr::kDirectRows) * nb[1];
+    long long work = (long long)B * a.H * ceil_div(own, kTile) * nb[1];
     for (int g = 0; g < p->P; ++g) {
         const int rows = (p->first[g + 1] - p->first[g]) * own;
         most = rows > most ? rows : most;
-        work += (long long)a.H * ceil_div(rows, shr::kDirectRows) * nb[0];
+        work += (long long)a.H * ceil_div(rows, kTile) * nb[0];
     }
     const bool direct = kernels ? kernels == 1 : all_direct(D, most, work);
-    const Kind kind[2] = {direct ? direct_kind() : image_kind(D, most),
-                          direct || (!kernels && own <= 2 * shr::kDirectRows) ? direct_kind() : image_kind(D, own)};
+    const Kind few = direct_kind(D, a.k_bits, a.ring > 0 || a.sink > 0);
+    const Kind kind[2] = {direct ? few : image_kind(D, most),
+                          direct || (!kernels && own <= 2 * kTile) ? few : image_kind(D, own)};
     p->tiles0 = 0;
     for (int g = 0; g < p->P; ++g) {
         p->tile0[g] = p->tiles0;
@@ -207,13 +209,14 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
 
 int shared_split_bound(int B, int H, int D, int C, int G)
 {
-    // The groups' tiles are never fewer than one group's of all rows; with fewer
-    // rows per group either kernel may take them.
+    // The groups' tiles are never fewer than one group's of all rows, nor those
+    // of any format than of the one with the most rows per tile; either kernel may
+    // take them.
     const auto splits = [&](long long units, int rows, const Kind& k) {
         return shared_splits(units * ceil_div(rows, k.per), k.round);
     };
     const auto most = [&](long long units, int rows) {
-        const int image = splits(units, rows, image_kind(D, rows)), direct = splits(units, rows, direct_kind());
+        const int image = splits(units, rows, image_kind(D, rows)), direct = splits(units, rows, direct_kind(D, 2, false));
         return image > direct ? image : direct;
     };
     return most(H, B * C * G) + most((long long)B * H, C * G);

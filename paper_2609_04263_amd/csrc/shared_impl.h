@@ -152,7 +152,14 @@ __host__ __device__ constexpr int row_waves(int D, int n16)
 }
 
 // ---- direct_kernel
-constexpr int kDirectWaves = 4, kDirectThreads = 64 * kDirectWaves, kDirectRows = 16;
+constexpr int kDirectWaves = 4, kDirectThreads = 64 * kDirectWaves;
+
+// 16-row tiles of a wave, which shares a block's codes between them: as many as
+// fit the registers beside wide codes or the conversion of fp16 tokens.
+__host__ __device__ constexpr int direct_tiles(int D, int bits, bool fp16)
+{
+    return D == 256 || bits == 8 || fp16 ? 1 : 2;
+}
 
 // Per wave: a block's key scales, offsets and scalars, then its value scales and
 // offsets, or (fp16 tokens) its values transposed, [D][kVtPitch].
@@ -638,7 +645,7 @@ struct Rows {
     half8 q[CT][NKB], ql[ROT ? CT : 1][ROT ? NKB : 1];
     float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg (ZM), or over group j
     floatx4 oacc[CT][NMB];
-    float zacc[DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
+    float zacc[CT][DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
     float m[CT], lsum[CT];   // running max (log2 units), lane partial sum (times 2^kPBits)
     float vf;                // power of two that the accumulated values carry (uniform)
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
@@ -728,10 +735,10 @@ struct Rows {
     {
         vf = 0.0f;
 #pragma unroll
-        for (float& z : zacc)
-            z = 0.0f;
-#pragma unroll
         for (int c = 0; c < CT; ++c) {
+#pragma unroll
+            for (float& z : zacc[c])
+                z = 0.0f;
             m[c] = kNegInf;
             lsum[c] = 0.0f;
 #pragma unroll
@@ -744,11 +751,11 @@ struct Rows {
     // running maxima), probabilities (vector operations), values (matrix
     // products).
 
-    __device__ __forceinline__ void scale_offsets(float by)
+    __device__ __forceinline__ void scale_offsets(int c, float by)
     {
         if constexpr (DIRECT) {
 #pragma unroll
-            for (float& z : zacc)
+            for (float& z : zacc[c])
                 z *= by;
         }
     }
@@ -779,11 +786,12 @@ struct Rows {
             if (vf == 0.0f || d < 0) {
                 if (vf != 0.0f) {
 #pragma unroll
-                    for (int c = 0; c < CT; ++c)
+                    for (int c = 0; c < CT; ++c) {
 #pragma unroll
                         for (int mb = 0; mb < NMB; ++mb)
                             oacc[c][mb] *= r;
-                    scale_offsets(r);
+                        scale_offsets(c, r);
+                    }
                 }
                 vf = f;
             } else {
@@ -805,7 +813,7 @@ struct Rows {
 #pragma unroll
                 for (int mb = 0; mb < NMB; ++mb)
                     oacc[c][mb] *= alpha;
-                scale_offsets(alpha);
+                scale_offsets(c, alpha);
             }
             // (a column that has seen no token keeps m = -inf and gets zeros)
             shift[c] = bias - (m[c] == kNegInf ? 0.0f : m[c]);
@@ -962,150 +970,209 @@ struct Rows {
         }
     }
 
-    // ---- One block of codes or fp16 rows in registers, of a wave with one tile.
+    // ---- One block of codes or fp16 rows in registers, of a wave with NT tiles.
     // The pieces are made one at a time (left to itself the compiler makes
     // them all ahead of their products, in registers that there are not).
 
-    // l[4 e + i]: the score of token 8 qg + 4 e + i, in log2 units, from key(e, kb)
+    // l[c][4 e + i]: the score of token 8 qg + 4 e + i, in log2 units, from key(e, kb)
     // and meta's scales.
-    template <class Key>
-    __device__ __forceinline__ void group_scores(Key key, const float* meta, bool affine, int lane, float* l)
+    template <int NT, class Key>
+    __device__ __forceinline__ void group_scores(Key key, const float* meta, bool affine, int lane, float (*l)[8])
     {
         const int qg = lane >> 4;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            floatx4 S = {0.0f, 0.0f, 0.0f, 0.0f};
+            floatx4 S[NT];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (ZM) {
                 if (affine)
-                    add_offset_products<1>(&S, meta, e, lane);
+                    add_offset_products<NT>(S, meta, e, lane);
             }
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+                floatx4 acc[NT];
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    acc[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int kb = g * KS; kb < (g + 1) * KS; ++kb) {
                     const half8 a = key(e, kb);
-                    acc = mfma16(a, q[0][kb], acc);
-                    if constexpr (ROT)
-                        acc = mfma16(a, ql[0][kb], acc);
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+                        acc[c] = mfma16(a, q[c][kb], acc[c]);
+                    if constexpr (ROT) {
+#pragma unroll
+                        for (int c = 0; c < NT; ++c)
+                            acc[c] = mfma16(a, ql[c][kb], acc[c]);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 const floatx4 s4 = *(const floatx4*)(meta + 32 * g + 8 * qg + 4 * e);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    S[i] = fmaf(s4[i], acc[i], S[i]);
+                for (int c = 0; c < NT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        S[c][i] = fmaf(s4[i], acc[c][i], S[c][i]);
                 if constexpr (!ZM) {
                     if (affine)
-                        add_group_offset<1>(&S, meta, g, e, lane);
+                        add_group_offset<NT>(S, meta, g, e, lane);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                l[4 * e + i] = S[i];
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    l[c][4 * e + i] = S[c][i];
         }
+    }
+
+    // Eight scales and offsets (D further) at `at`, in operand order.
+    static __device__ __forceinline__ void load_scales(const float* at, float* sn)
+    {
+        const float4 a = *(const float4*)at, b = *(const float4*)(at + 4);
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            sn[j] = x[perm4(j)];
     }
 
     // The same with per-channel scales (CODED: scales s at st, offsets z D further):
     // sum_d q_d (s_d c_d + z_d) = (q s) . c + q . z.
-    template <bool CODED, class Key>
-    __device__ __forceinline__ void channel_scores(Key key, const float* st, float ksm, int lane, float* l)
+    template <int NT, bool CODED, class Key>
+    __device__ __forceinline__ void channel_scores(Key key, const float* st, float ksm, int lane, float (*l)[8])
     {
         const int qg = lane >> 4;
-        floatx4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-        float z = 0.0f;
+        floatx4 acc[NT][2];
+        float z[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            acc[c][0] = acc[c][1] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            z[c] = 0.0f;
+        }
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
-            half8 hi = q[0][kb], lo = ql[0][ROT ? kb : 0];
+            half8 hi[NT], lo[NT];
             if constexpr (CODED) {
-                const float* at = st + 32 * kb + 8 * qg;
-                const float4 s0 = *(const float4*)at, s1 = *(const float4*)(at + 4);
-                const float4 z0 = *(const float4*)(at + D), z1 = *(const float4*)(at + D + 4);
-                const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-                const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
-                float x[8];
+                float sn[8], zn[8];
+                load_scales(st + 32 * kb + 8 * qg, sn);
+                load_scales(st + D + 32 * kb + 8 * qg, zn);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float qf = (float)hi[j] + (ROT ? (float)lo[j] : 0.0f);
-                    x[j] = qf * sn[perm4(j)];
-                    z = fmaf(qf, zn[perm4(j)], z);
+                for (int c = 0; c < NT; ++c) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float qf = (float)q[c][kb][j] + (ROT ? (float)ql[c][ROT ? kb : 0][j] : 0.0f);
+                        x[j] = qf * sn[j];
+                        z[c] = fmaf(qf, zn[j], z[c]);
+                    }
+                    split_nearest(x, &hi[c], &lo[c]);
                 }
-                split_nearest(x, &hi, &lo);
+            } else {
+#pragma unroll
+                for (int c = 0; c < NT; ++c) {
+                    hi[c] = q[c][kb];
+                    if constexpr (ROT)
+                        lo[c] = ql[c][kb];
+                }
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const half8 a = key(e, kb);
-                acc[e] = mfma16(a, hi, acc[e]);
-                if constexpr (CODED || ROT)
-                    acc[e] = mfma16(a, lo, acc[e]);
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    acc[c][e] = mfma16(a, hi[c], acc[c][e]);
+                if constexpr (CODED || ROT) {
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+                        acc[c][e] = mfma16(a, lo[c], acc[c][e]);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (CODED)
-            z = sum_rows(z);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int c = 0; c < NT; ++c) {
+            const float zs = CODED ? sum_rows(z[c]) : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                l[4 * e + i] = (acc[e][i] + z) * ksm;
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    l[c][4 * e + i] = (acc[c][e][i] + zs) * ksm;
+        }
     }
 
     // Values of codes(mb), scales s at st (offsets z D further) of `group` channels:
     // sum_t p_t (s_t c_t + z_t) = (p s) . c + p . z.
-    template <class Codes>
-    __device__ __forceinline__ void group_values(Codes codes, const float* st, int group, bool affine, const float* pv,
-                                                 int lane)
+    template <int NT, class Codes>
+    __device__ __forceinline__ void group_values(Codes codes, const float* st, int group, bool affine,
+                                                 const float (*pv)[8], int lane)
     {
-        half8 hi, lo;
+        half8 hi[NT], lo[NT];
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb) {
             if (mb % 2 == 0 && (16 * mb & (group - 1)) == 0) {
                 const float* at = st + 32 * (16 * mb >> (31 - __builtin_clz(group))) + 8 * (lane >> 4);
-                const float4 s0 = *(const float4*)at, s1 = *(const float4*)(at + 4);
-                const float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-                float x[8];
+                float sn[8];
+                load_scales(at, sn);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = pv[j] * sn[perm4(j)];
-                split_nearest(x, &hi, &lo);
-                if (affine) {
-                    const float4 z0 = *(const float4*)(at + D), z1 = *(const float4*)(at + D + 4);
-                    const float zn[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+                for (int c = 0; c < NT; ++c) {
+                    float x[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        zacc[mb / 2] = fmaf(pv[j], zn[perm4(j)], zacc[mb / 2]);
+                        x[j] = pv[c][j] * sn[j];
+                    split_nearest(x, &hi[c], &lo[c]);
+                }
+                if (affine) {
+                    load_scales(at + D, sn);
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            zacc[c][mb / 2] = fmaf(pv[c][j], sn[j], zacc[c][mb / 2]);
                 }
             }
-            const half8 a = codes(mb);
-            oacc[0][mb] = mfma16(a, hi, oacc[0][mb]);
-            oacc[0][mb] = mfma16(a, lo, oacc[0][mb]);
-            __builtin_amdgcn_sched_barrier(0);
+            value_products<NT>(codes(mb), mb, hi, lo);
         }
     }
 
-    // Values that are operands as they are.
-    template <class Value>
-    __device__ __forceinline__ void row_values(Value value, const float* pv)
+    template <int NT>
+    __device__ __forceinline__ void value_products(const half8& a, int mb, const half8* hi, const half8* lo)
     {
-        half8 hi, lo;
-        split_nearest(pv, &hi, &lo);
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb) {
-            const half8 a = value(mb);
-            oacc[0][mb] = mfma16(a, hi, oacc[0][mb]);
-            oacc[0][mb] = mfma16(a, lo, oacc[0][mb]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int c = 0; c < NT; ++c)
+            oacc[c][mb] = mfma16(a, hi[c], oacc[c][mb]);
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+            oacc[c][mb] = mfma16(a, lo[c], oacc[c][mb]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    // Values that are operands as they are.
+    template <int NT, class Value>
+    __device__ __forceinline__ void row_values(Value value, const float (*pv)[8])
+    {
+        half8 hi[NT], lo[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+            split_nearest(pv[c], &hi[c], &lo[c]);
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+            value_products<NT>(value(mb), mb, hi, lo);
     }
 
     // The value offsets join their channels.
     __device__ __forceinline__ void add_offsets(int group)
     {
-        float z = 0.0f;
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb) {
-            if (mb % 2 == 0 && (16 * mb & (group - 1)) == 0)
-                z = sum_rows(zacc[mb / 2]);
-            oacc[0][mb] += z;
+        for (int c = 0; c < CT; ++c) {
+            float z = 0.0f;
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) {
+                if (mb % 2 == 0 && (16 * mb & (group - 1)) == 0)
+                    z = sum_rows(zacc[c][mb / 2]);
+                oacc[c][mb] += z;
+            }
         }
     }
 
@@ -1414,14 +1481,14 @@ __host__ __device__ constexpr int direct_waves(int D)
 template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
 {
-    constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves;
+    constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves, CT = direct_tiles(D, KB, ROWS), PER = 16 * CT;
     constexpr bool kAhead = D < 256;  // (two blocks' loads do not fit the registers of the widest heads)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const Item it = find_item(sp, blockIdx.x + sp.direct0, kDirectRows);
+    const Item it = find_item(sp, blockIdx.x + sp.direct0, PER);
     const AttnParams& p = sp.seg[it.seg];
-    const int G = p.G, left = min(it.rows - it.r0, kDirectRows);
+    const int G = p.G, left = min(it.rows - it.r0, PER);
     const Blocks bl(sp, p, it, left);
 
     typedef Builder<D, KG == 0, KB, VB, M16, 1> Build;
@@ -1433,105 +1500,121 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
         return r;
     };
     typename Build::Loads raw = prefetch(bl.v0 + wave);
-    Rows<D, KG, ROT, 1, true> T;
+    Rows<D, KG, ROT, CT, true> T;
     T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
-    {
-        const int rc = min(hh, left - 1);
-        T.lim[0] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
-        T.load_query(0, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        const int rc = min(16 * c + hh, left - 1);
+        T.lim[c] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
+        T.load_query(c, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
     }
     T.init();
     float* meta = (float*)(lds + wave * direct_region(D, p.ring || p.sink));
     float* st = meta + meta_bytes(D) / 4;
-    for (int v = bl.v0 + wave; v < bl.v1; v += W) {
-        const Span s(p, bl, v);
-        float l[1][8], pv[8], shift, back;
-        lds_order();
-        if (!ROWS || bl.coded(v)) {
-            const typename Build::Loads now = raw;
-            if constexpr (kAhead)
-                raw = prefetch(v + W);
-            const int live = min(32, p.nq - s.t0);
-            const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
-            const float f = B.value_scales(now, live, st, to_one<VB>());
+    // (two loops, so that the registers of a wave's tiles have one place in each)
+    const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
+        constexpr int NT = decltype(tiles_now)::value;
+        for (int v = bl.v0 + wave; v < bl.v1; v += W) {
+            const Span s(p, bl, v);
+            float l[NT][8], pv[NT][8], shift[NT], back;
             lds_order();
-            const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
-            if constexpr (KG == 0)
-                T.template channel_scores<true>(key, meta, ksm, lane, l[0]);
-            else
-                T.group_scores(key, meta, B.kaff, lane, l[0]);
-            T.template settle<1>(l, f, s.t0, s.off, s.live, lane, &shift, &back);
-            T.exponentials(0, l[0], shift, back, pv);
-            T.group_values([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
-            if constexpr (!kAhead)
-                raw = prefetch(v + W);
-        } else {
-            const RowBlock rb(p, it.unit, bl, v, D);
-            Build A = B;  // (the addresses below are made here, not kept in registers over the loop)
-            asm volatile("" : "+v"(A.lane));
-            // Values are transposed through LDS, 128 channels at a time: a lane has 8
-            // channels of tokens t and t + 4, neighbours in the operand, 16 such
-            // pairs and 4 lanes of channels at a time: two lanes per bank.
-            constexpr int NV = (D < 128 ? D : 128) / 32;
-            u32x4 kw[2 * NKB];
-            uint16_t* vt = (uint16_t*)st;
-            const int pair = A.lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (A.lane & 3);
-            const uint32_t keep = (t0 < rb.live ? 0xFFFFu : 0u) | (t0 + 4 < rb.live ? 0xFFFF0000u : 0u);
+            if (!ROWS || bl.coded(v)) {
+                const typename Build::Loads now = raw;
+                if constexpr (kAhead)
+                    raw = prefetch(v + W);
+                const int live = min(32, p.nq - s.t0);
+                const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
+                const float f = B.value_scales(now, live, st, to_one<VB>());
+                lds_order();
+                const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
+                if constexpr (KG == 0)
+                    T.template channel_scores<NT, true>(key, meta, ksm, lane, l);
+                else
+                    T.template group_scores<NT>(key, meta, B.kaff, lane, l);
+                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
 #pragma unroll
-            for (int u = 0; u < D / 32; u += NV) {
-                u32x4 vw[NV][2];
+                for (int c = 0; c < NT; ++c)
+                    T.exponentials(c, l[c], shift[c], back, pv[c]);
+                T.template group_values<NT>([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
+                if constexpr (!kAhead)
+                    raw = prefetch(v + W);
+            } else {
+                const RowBlock rb(p, it.unit, bl, v, D);
+                Build A = B;  // (the addresses below are made here, not kept in registers over the loop)
+                asm volatile("" : "+v"(A.lane));
+                // Values are transposed through LDS, 128 channels at a time: a lane has 8
+                // channels of tokens t and t + 4, neighbours in the operand, 16 such
+                // pairs and 4 lanes of channels at a time: two lanes per bank.
+                constexpr int NV = (D < 128 ? D : 128) / 32;
+                u32x4 kw[2 * NKB];
+                uint16_t* vt = (uint16_t*)st;
+                const int pair = A.lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (A.lane & 3);
+                const uint32_t keep = (t0 < rb.live ? 0xFFFFu : 0u) | (t0 + 4 < rb.live ? 0xFFFF0000u : 0u);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
+                for (int u = 0; u < D / 32; u += NV) {
+                    u32x4 vw[NV][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
+                            vw[i][h] = *(const u32x4*)(row + 32 * (u + i));
+                    }
+                    if (u + NV >= D / 32) {
+#pragma unroll
+                        for (int i = 0; i < 2 * NKB; ++i)
+                            kw[i] = A.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
+                    }
 #pragma unroll
                     for (int i = 0; i < NV; ++i)
-                        vw[i][h] = *(const u32x4*)(row + 32 * (u + i));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            *(uint32_t*)(vt + (32 * (u + i) + c8 + j) * kVtPitch + 2 * pair) =
+                                __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (u + NV >= D / 32) {
+                A.row_scales(meta);
+                lds_order();
+                const auto key = [&](int e, int kb) { return A.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); };
+                if constexpr (KG == 0)
+                    T.template channel_scores<NT, false>(key, nullptr, p.sm_log2, lane, l);
+                else
+                    T.template group_scores<NT>(key, meta, false, lane, l);
+                T.template settle<NT>(l, 1.0f, s.t0, s.off, s.live, lane, shift, &back);
 #pragma unroll
-                    for (int i = 0; i < 2 * NKB; ++i)
-                        kw[i] = A.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
-                }
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *(uint32_t*)(vt + (32 * (u + i) + c8 + j) * kVtPitch + 2 * pair) =
-                            __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
-                __builtin_amdgcn_sched_barrier(0);
+                for (int c = 0; c < NT; ++c)
+                    T.exponentials(c, l[c], shift[c], back, pv[c]);
+                T.template row_values<NT>([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
+                raw = prefetch(v + W);
             }
-            A.row_scales(meta);
-            lds_order();
-            const auto key = [&](int e, int kb) { return A.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); };
-            if constexpr (KG == 0)
-                T.template channel_scores<false>(key, nullptr, p.sm_log2, lane, l[0]);
-            else
-                T.group_scores(key, meta, false, lane, l[0]);
-            T.template settle<1>(l, 1.0f, s.t0, s.off, s.live, lane, &shift, &back);
-            T.exponentials(0, l[0], shift, back, pv);
-            T.row_values([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
-            raw = prefetch(v + W);
         }
-    }
-
+    };
+    if (CT == 1 || left <= 16)
+        walk(std::integral_constant<int, 1>{});
+    else
+        walk(std::integral_constant<int, CT>{});
     T.add_offsets(p.v_group);
 
     // ---- the waves' partials merged
-    const float inv = T.inverse(), l = sum_rows(T.lsum[0]);
+    const float inv = T.inverse();
     float* lo = (float*)lds;
     float* lml = lo + W * 16 * merge_pitch(D);
-    __syncthreads();
-    if (hh < left) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        if (16 * c >= left)
+            break;
+        const float l = sum_rows(T.lsum[c]);
+        __syncthreads();
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb)
-            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[0][mb] * inv;
+            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
         if (qg == 0)
-            *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[0], l);
-    }
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < left * (D / 4); idx += kDirectThreads) {
-        const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
-        merge_row<D>(sp, lo, lml, 0, W, r, d, (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + r));
+            *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < min(left - 16 * c, 16) * (D / 4); idx += kDirectThreads) {
+            const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
+            merge_row<D>(sp, lo, lml, 0, W, r, d, (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + 16 * c + r));
+        }
     }
 }
 
