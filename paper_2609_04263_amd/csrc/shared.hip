@@ -41,20 +41,22 @@ Kind image_kind(int D, int rows)
 }
 
 // Whether the direct kernel takes everything: `rows` the most that a unit of the
-// prefix has, `work` the 32-token blocks of all 16-row tiles of both segments.
-// The direct kernel converts a block's codes for every tile, the image kernel once
-// per 128 or 256 rows, which costs it half as much per tile and block (D = 256:
-// two thirds); but a call has to pay its launch beside the direct one's, the
-// conversion before its first product, the merge of a wave's partials and the
-// join of more of them: 16 to 25 us.  Direct / image, us, at `work` in 1024s:
-//     D = 64    64 rows  15 / 21 (4)   33 / 36 (32)   256 rows  15 / 29 (8)   21 / 32 (16)
-//     D = 128   64 rows  23 / 32 (8)   94 / 91 (64)   256 rows  33 / 50 (16)  51 / 59 (32)
-//     D = 256   64 rows  43 / 48 (8)  205 / 181 (64)  256 rows  54 / 58 (8)   73 / 68 (16)
+// prefix has, `work` the 32-token blocks of all 16-row tiles of both segments, k
+// the direct kernel's.  It converts a block's codes once per one or two tiles, the
+// image kernel once per 128 or 256 rows; but a call of that one has to pay a
+// launch of its own, the conversion before its first product, the merge of a wave's
+// partials and the join of more of them: 16 to 25 us.  Direct / image, us, at
+// `work` in 1024s:
+//     two tiles  D = 64    64 rows  30 / 39 (32)   256 rows  43 / 50 (64)   72 / 71 (128)
+//                D = 128   64 rows  45 / 57 (32)   256 rows  72 / 77 (64)   97 / 94 (96)
+//                rotated                           256 rows  60 / 67 (32)   94 / 91 (69)
+//     one tile   D = 128, per-channel keys         256 rows  45 / 52 (16)   71 / 60 (32)
+//                D = 256   64 rows  43 / 48 (8)    128 rows  49 / 50 (8)    69 / 61 (16)
 // Units of two tiles would leave most of an image kernel's waves idle: 32 rows of
-// 8192 tokens, 8 prefixes, 21 / 30, 52 / 70 and 110 / 141 us.
-bool all_direct(int D, int rows, long long work)
+// 8192 tokens, 8 prefixes, D = 256, 110 / 141 us.
+bool all_direct(int D, int rows, long long work, const Kind& k)
 {
-    return rows <= 2 * kTile || work <= (D == 256 ? 12 : 40) * 1024;
+    return rows <= 2 * kTile || work <= (D == 256 ? 12 : k.per == kTile ? 24 : 64) * 1024;
 }
 
 // Ranges that a segment of `tiles` tiles is cut into, at most.
@@ -181,8 +183,8 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
         most = rows > most ? rows : most;
         work += (long long)a.H * ceil_div(rows, kTile) * nb[0];
     }
-    const bool direct = kernels ? kernels == 1 : all_direct(D, most, work);
     const Kind few = direct_kind(D, a.k_bits, a.ring > 0 || a.sink > 0);
+    const bool direct = kernels ? kernels == 1 : all_direct(D, most, work, few);
     const Kind kind[2] = {direct ? few : image_kind(D, most),
                           direct || (!kernels && own <= 2 * kTile) ? few : image_kind(D, own)};
     p->tiles0 = 0;

@@ -23,8 +23,8 @@
 //                  wave that takes part in a block repeats the work on its
 //                  scales: 3 to 15% slower, in either order of the halves.)
 //   direct_kernel  little work, or few rows per unit (a suffix's queries, few
-//                  samples): 16 rows, four waves, each with blocks of its own,
-//                  whose codes become operands in registers.
+//                  samples): 16 or 32 rows, four waves, each with blocks of its
+//                  own, whose codes become operands in registers.
 //
 // Operands are in the order in which the cache stores its codes, that of
 // v_mfma_f32_16x16x32_f16 (a 1 KiB fragment is one 16-byte piece per lane).
@@ -155,7 +155,8 @@ __host__ __device__ constexpr int row_waves(int D, int n16)
 constexpr int kDirectWaves = 4, kDirectThreads = 64 * kDirectWaves;
 
 // 16-row tiles of a wave, which shares a block's codes between them: as many as
-// fit the registers beside wide codes or the conversion of fp16 tokens.
+// fit the registers beside wide codes or the conversion of fp16 tokens (96
+// sequences at D = 64: 24.5 us, 31 with one tile).
 __host__ __device__ constexpr int direct_tiles(int D, int bits, bool fp16)
 {
     return D == 256 || bits == 8 || fp16 ? 1 : 2;
