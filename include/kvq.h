@@ -344,7 +344,8 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * once per 16 query rows (sequence, query, head of a group) of its group, of
  * calls of much work once per 128 (D = 256) or 256, instead of once per
  * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16), and its limits.
- * Products have 22 bits or more, sums are fp32 and run in an order that depends
+ * Products have 22 bits or more (a value at least 2^-31 of the largest value of
+ * its prefix and suffix, whatever that one's weight), sums are fp32 and run in an order that depends
  * on the shapes, the groups and the lengths alone, so a call gives the same
  * bits every time. */
 

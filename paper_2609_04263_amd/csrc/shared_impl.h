@@ -782,8 +782,10 @@ struct Rows {
         float bias = kPBits;
         *back = 1.0f;
         if (f != vf) {
-            const int d = (int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23);  // log2(f / vf)
-            const float r = __uint_as_float((uint32_t)min(max(127 + d, 0), 254) << 23);
+            // log2(f / vf); from 2^40 on the products of the smaller values vanish
+            // beside the others, but their probabilities are to be counted
+            const int d = min((int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23), 100);
+            const float r = __uint_as_float((uint32_t)max(127 + d, 0) << 23);
             if (vf == 0.0f || d < 0) {
                 if (vf != 0.0f) {
 #pragma unroll

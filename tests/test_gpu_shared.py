@@ -299,6 +299,23 @@ def test_values_of_all_magnitudes(name, first):
 
 
 @pytest.mark.parametrize("first", [[0, 3], [0, 33]])
+@pytest.mark.parametrize("name", ["tiny_b16", "gqa12b", "hadamard"])
+def test_values_beside_enormous_ones(name, first):
+    """Powers of two of blocks further apart than one binary32 number reaches (fp32 metadata, no fp16 tokens)."""
+    fmt, D = CASES[name]
+    caches = []
+    for n, U, nm in ((300, 1, "p"), (200, first[-1], "s")):
+        K, V = synth.kv_tokens(49, U, n, 2, D, name=nm)
+        f = synth.bf16_bits_to_f32(V) * np.where(np.arange(n) // 64 % 2 == 0, np.float32(1e32), np.float32(0))[
+            None, :, None, None]
+        caches.append(Pair(fmt, U, 2, D, n).append(K, synth.to_bf16_bits(f.astype(np.float32))))
+    Q = synth.queries(50, first[-1], 8, D).reshape(first[-1], 1, 8, D)
+    want = reference(*caches, first, Q, D ** -0.5)
+    for k in range(3):
+        close(call(*caches, first, Q, D ** -0.5, kernels=k), want, what=f"kernels={k}")
+
+
+@pytest.mark.parametrize("first", [[0, 3], [0, 33]])
 @pytest.mark.parametrize("name", ["tiny_b16", "kivi", "hadamard"])
 def test_values_of_zero(name, first):
     fmt, D = CASES[name]
