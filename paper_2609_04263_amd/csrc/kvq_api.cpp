@@ -1005,12 +1005,11 @@ static kvq_status shared_caches(const kvq_cache* prefix, const kvq_cache* suffix
 
 static size_t shared_workspace_layout(const kvq_cache* suffix, int C, int H_q, size_t* off_ml)
 {
-    const size_t rows = (size_t)suffix->B * C * H_q;
-    const size_t S = kvq::shared_split_bound(suffix->B, suffix->H, suffix->D, C, H_q / suffix->H);
-    const size_t o_ml = round_up(rows * S * suffix->D * sizeof(float), 256);
+    const size_t partials = kvq::shared_partials_bound(suffix->B, suffix->H, suffix->D, C, H_q / suffix->H);
+    const size_t o_ml = round_up(partials * suffix->D * sizeof(float), 256);
     if (off_ml)
         *off_ml = o_ml;
-    return o_ml + rows * S * 2 * sizeof(float);
+    return o_ml + partials * 2 * sizeof(float);
 }
 
 kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* suffix, int C, int H_q, size_t* bytes)

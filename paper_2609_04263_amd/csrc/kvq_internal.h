@@ -252,8 +252,8 @@ struct SharedParams {
 };
 // Fills S, bps, tiles0, items0, tile0 and the kernels' items from the rest.
 void shared_plan(SharedParams* p, int D, int B, int kernels);
-// Upper bound of S0 + S1 for any lengths and groups.
-int shared_split_bound(int B, int H, int D, int C, int G);
+// Upper bound of (S0 + S1) rows for any lengths and groups and up to C queries.
+size_t shared_partials_bound(int B, int H, int D, int C, int G);
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream);
 
 }  // namespace kvq

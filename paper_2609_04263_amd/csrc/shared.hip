@@ -209,19 +209,21 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
     p->direct_items = p->items0 + items1 - p->image_items;
 }
 
-int shared_split_bound(int B, int H, int D, int C, int G)
+size_t shared_partials_bound(int B, int H, int D, int C, int G)
 {
-    // The groups' tiles are never fewer than one group's of all rows, nor those
-    // of any format than of the one with the most rows per tile; either kernel may
-    // take them.
-    const auto splits = [&](long long units, int rows, const Kind& k) {
-        return shared_splits(units * ceil_div(rows, k.per), k.round);
+    // A segment of `units` units of u rows is cut into S <= max(1, round / tiles)
+    // ranges, its tiles never fewer than units ceil(u / per) (the groups' not fewer
+    // than one group's of all rows): units u S <= max(units u, round min(u, per)).
+    // Unlike S this does not fall as C grows.
+    const auto segment = [&](size_t units, int u) {
+        size_t most = units * u;
+        for (const Kind& k : {image_kind(D, u), direct_kind(D, 2, false)}) {
+            const size_t cut = (size_t)k.round * (u < k.per ? u : k.per);
+            most = cut > most ? cut : most;
+        }
+        return most;
     };
-    const auto most = [&](long long units, int rows) {
-        const int image = splits(units, rows, image_kind(D, rows)), direct = splits(units, rows, direct_kind(D, 2, false));
-        return image > direct ? image : direct;
-    };
-    return most(H, B * C * G) + most((long long)B * H, C * G);
+    return segment(H, B * C * G) + segment((size_t)B * H, C * G);
 }
 
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream)

@@ -341,6 +341,15 @@ def test_same_bits_every_time_and_after_a_larger_call():
     assert torch.equal(call(prefix, suffix, [0, 5, 9], Q, 128 ** -0.5, stream=side), got)
 
 
+@pytest.mark.parametrize("C", [1, 16, 17, 32])
+def test_a_workspace_of_more_queries(C):
+    # fewer rows are cut into more ranges
+    prefix, suffix, Q, got = run("tiny_b16", [0, 1], 9000, 50, G=1, H=1, C=C, chunk=True, seed=51)
+    ws = suffix.gpu.shared_workspace(prefix.gpu, 1, 33)
+    ws.fill_(255)
+    assert torch.equal(call(prefix, suffix, [0, 1], Q, 64 ** -0.5, chunk=True, ws=ws), got)
+
+
 @pytest.mark.parametrize("name,C", [("kivi", 1), ("tiny_b16", 20), ("hadamard", 1)])
 def test_captured_calls_replay(name, C):
     fmt, D = CASES[name]

@@ -84,3 +84,11 @@ def test_workspace(kvq):
         # it does not depend on the lengths
         p.restore(0), s.restore(100)
         assert s.shared_workspace_bytes(p, 8, 10) == need
+
+
+def test_a_workspace_serves_every_smaller_call(kvq):
+    # (up to C queries: what a call of fewer needs is never more)
+    for D, B, H_q in ((64, 1, 2), (64, 4, 8), (128, 1, 4), (128, 3, 32), (256, 2, 4)):
+        p, s = pair(kvq, D=D, P=1, B=B, f=configs.make_format(k_group=64))
+        need = [s.shared_workspace_bytes(p, H_q, c) for c in range(1, 400)]
+        assert need == sorted(need)
