@@ -1502,7 +1502,10 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
             B.load(r, bl.nearest(v));
         return r;
     };
-    typename Build::Loads raw = prefetch(bl.v0 + wave);
+    int vc = bl.v0 + wave;  // this wave's first block after the sink's
+    while (ROWS && vc < bl.nsb)
+        vc += W;
+    typename Build::Loads raw = prefetch(vc);
     Rows<D, KG, ROT, CT, true> T;
     T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
 #pragma unroll
@@ -1517,31 +1520,14 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     // (two loops, so that the registers of a wave's tiles have one place in each)
     const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
         constexpr int NT = decltype(tiles_now)::value;
-        for (int v = bl.v0 + wave; v < bl.v1; v += W) {
-            const Span s(p, bl, v);
-            float l[NT][8], pv[NT][8], shift[NT], back;
-            lds_order();
-            if (!ROWS || bl.coded(v)) {
-                const typename Build::Loads now = raw;
-                if constexpr (kAhead)
-                    raw = prefetch(v + W);
-                const int live = min(32, p.nq - s.t0);
-                const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
-                const float f = B.value_scales(now, live, st, to_one<VB>());
+        // (loops of one kind of block, sink rows, codes, window rows: a loop of all
+        // spills the registers that their branches differ in)
+        int v = bl.v0 + wave;
+        const auto fp16_blocks = [&](int end) __attribute__((always_inline)) {
+            for (; v < end; v += W) {
+                const Span s(p, bl, v);
+                float l[NT][8], pv[NT][8], shift[NT], back;
                 lds_order();
-                const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
-                if constexpr (KG == 0)
-                    T.template channel_scores<NT, true>(key, meta, ksm, lane, l);
-                else
-                    T.template group_scores<NT>(key, meta, B.kaff, lane, l);
-                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-                    T.exponentials(c, l[c], shift[c], back, pv[c]);
-                T.template group_values<NT>([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
-                if constexpr (!kAhead)
-                    raw = prefetch(v + W);
-            } else {
                 const RowBlock rb(p, it.unit, bl, v, D);
                 Build A = B;  // (the addresses below are made here, not kept in registers over the loop)
                 asm volatile("" : "+v"(A.lane));
@@ -1588,7 +1574,35 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                 for (int c = 0; c < NT; ++c)
                     T.exponentials(c, l[c], shift[c], back, pv[c]);
                 T.template row_values<NT>([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
-                raw = prefetch(v + W);
+            }
+        };
+        const int codes = ROWS ? min(bl.v1, bl.nsb + bl.ncb) : bl.v1;
+        for (int part = 0; part < (ROWS ? 2 : 1); ++part) {
+            if constexpr (ROWS)
+                fp16_blocks(part ? bl.v1 : min(bl.v1, bl.nsb));
+            for (; v < codes; v += W) {
+                const Span s(p, bl, v);
+                float l[NT][8], pv[NT][8], shift[NT], back;
+                lds_order();
+                const typename Build::Loads now = raw;
+                if constexpr (kAhead)
+                    raw = prefetch(v + W);
+                const int live = min(32, p.nq - s.t0);
+                const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
+                const float f = B.value_scales(now, live, st, to_one<VB>());
+                lds_order();
+                const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
+                if constexpr (KG == 0)
+                    T.template channel_scores<NT, true>(key, meta, ksm, lane, l);
+                else
+                    T.template group_scores<NT>(key, meta, B.kaff, lane, l);
+                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    T.exponentials(c, l[c], shift[c], back, pv[c]);
+                T.template group_values<NT>([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
+                if constexpr (!kAhead)
+                    raw = prefetch(v + W);
             }
         }
     };
