@@ -372,6 +372,33 @@ def test_captured_calls_replay(name, C):
         assert torch.equal(call(prefix, suffix, [0, 2, 5], Q, D ** -0.5), got)
 
 
+@pytest.mark.parametrize("kernels", [1, 2])
+@pytest.mark.parametrize("name", ["kivi", "gqa12b"])
+def test_each_kernel_replays_beside_another_graph(name, kernels):
+    """Two captured calls of one kernel, each with a workspace of its own, replayed at once on two streams."""
+    fmt, D = CASES[name]
+    prefix, suffix, Q, _ = run(name, [0, 20], 700, 77, C=3, seed=52)
+    want = call(prefix, suffix, [0, 20], Q, D ** -0.5, kernels=kernels)
+    dq, H_q, C = dev_bf16(Q), Q.shape[2], 3
+    outs, graphs = [], []
+    for _ in range(2):
+        O, ws = torch.zeros_like(want), suffix.gpu.shared_workspace(prefix.gpu, H_q, C)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call_kernel(prefix.gpu, suffix.gpu, [0, 20], dq, H_q, C, D ** -0.5, O, ws, True, kernels)
+        outs.append(O)
+        graphs.append((g, ws, torch.cuda.Stream()))
+    for i in range(4):
+        for O in outs:
+            O.zero_()
+        torch.cuda.synchronize()
+        for g, _, stream in graphs:
+            with torch.cuda.stream(stream):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(O, want) for O in outs), i
+
+
 @pytest.mark.parametrize("name", ["tiny_b1", "kivi", "gqa12b", "hadamard", "sink32_window"])
 def test_serving_a_prompt_with_samples(name):
     """The calls together, as a sampling loop makes them: two prompts, three samples each behind them, the
