@@ -1544,7 +1544,8 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                     u32x4 vw[NV][2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const uint16_t* row = rb.v + (uint32_t)((rb.first + min(t0 + 4 * h, rb.live - 1)) % rb.ring * D + c8);
+                        const int t = min(t0 + 4 * h, rb.live - 1);
+                        const uint16_t* row = rb.v + (uint32_t)((rb.first + t) % rb.ring * D + c8);
 #pragma unroll
                         for (int i = 0; i < NV; ++i)
                             vw[i][h] = *(const u32x4*)(row + 32 * (u + i));
@@ -1559,7 +1560,8 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             *(uint32_t*)(vt + (32 * (u + i) + c8 + j) * kVtPitch + 2 * pair) =
-                                __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1], j & 1 ? 0x07060302u : 0x05040100u) & keep;
+                                keep & __builtin_amdgcn_perm(vw[i][1][j >> 1], vw[i][0][j >> 1],
+                                                         j & 1 ? 0x07060302u : 0x05040100u);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 A.row_scales(meta);
@@ -1573,7 +1575,8 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
                     T.exponentials(c, l[c], shift[c], back, pv[c]);
-                T.template row_values<NT>([&](int mb) { return *(const half8*)(vt + (16 * mb + hh) * kVtPitch + 8 * qg); }, pv);
+                const uint16_t* at = vt + hh * kVtPitch + 8 * qg;
+                T.template row_values<NT>([&](int mb) { return *(const half8*)(at + 16 * mb * kVtPitch); }, pv);
             }
         };
         const int codes = ROWS ? min(bl.v1, bl.nsb + bl.ncb) : bl.v1;
@@ -1645,8 +1648,9 @@ hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
         launch_kernel(rows ? image_kernel<D, KG, KB, VB, M16, ROT, true> : image_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
                       dim3(p.image_items), dim3(64 * waves(D)), (size_t)image_lds(D, KG == 0), stream, p);
     if (p.direct_items > 0)
-        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true> : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow>, dim3(p.direct_items), dim3(kDirectThreads),
-                      (size_t)direct_lds(D, rows), stream, p);
+        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true>
+                           : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
+                      dim3(p.direct_items), dim3(kDirectThreads), (size_t)direct_lds(D, rows), stream, p);
     return hipGetLastError();
 }
 

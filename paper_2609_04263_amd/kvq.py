@@ -78,8 +78,8 @@ def _load() -> C.CDLL:
     for name in ("kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section", "kvq_cache_reset",
                  "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_project_workspace_bytes",
                  "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
-                 "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
-                 "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
+                 "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
+                 "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
                  "kvq_prefill_attn_shared", "kvq_time_launches"):
         getattr(L, name).restype = I
     return L
@@ -89,8 +89,8 @@ _lib = _load()
 EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section",
             "kvq_cache_reset", "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_cache_destroy",
             "kvq_project_workspace_bytes", "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
-            "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc", "kvq_prefill_attn",
-            "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
+            "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
+            "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
             "kvq_prefill_attn_shared", "kvq_time_launches")
 
 
