@@ -344,10 +344,12 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * once per 16 query rows (sequence, query, head of a group) of its group, of
  * calls of much work once per 128 (D = 256) or 256, instead of once per
  * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16), and its limits.
- * Products have 22 bits or more (a value at least 2^-31 of the largest value of
- * its prefix and suffix, whatever that one's weight), sums are fp32 and run in an order that depends
- * on the shapes, the groups and the lengths alone, so a call gives the same
- * bits every time. */
+ * A product of a weight and a value is off by at most 2^-22 of the weight times
+ * its token's largest value, or by 2^-32 of the largest such product of the
+ * row, whatever the sizes of other tokens' values (values of coded tokens below
+ * 2^100, of fp16 tokens below 65504).  Sums are fp32 and run in an order that
+ * depends on the shapes, the groups and the lengths alone, so a call gives the
+ * same bits every time. */
 
 /* Workspace bytes for calls of up to C queries per sequence at any lengths and
  * groups of these caches (contents need no initialization; calls that share a

@@ -54,10 +54,23 @@
 // direct_kernel: vector operations of the conversions, and at small sizes the
 // latency of one block after another.
 //
-// Softmax: online per column in base 2, the running maximum raised only when a
-// block exceeds it by more than kTau; probabilities are at most 2^(kTau +
-// kPBits).  Causal rows (suffix segments of a chunk) are masked per column, and
-// blocks that no row of a wave sees are skipped.
+// Softmax: online per column in base 2, by the size of the products rather than
+// that of the weights.  A token's values are multiplied by its own power of two f_t
+// (largest magnitude 2^11 to 2^12), and its score x_t (log2 units) is taken as
+//     x'_t = x_t - log2 f_t + 10,
+// so that a reference R that follows max x' makes p'_t = 2^(x'_t - R + kPBits) and
+// f_t v_t fp16 operands with all of their bits wherever p v is not negligible beside the
+// row's largest product, however far apart values and weights are:
+//     sum_t p'_t (f_t v_t) = 2^(kPBits + 10) sum_t 2^(x_t - R) v_t,
+//     sum_t p'_t (f_t / 2^10) = 2^kPBits sum_t 2^(x_t - R).
+// (With one power of two per block, for which the probabilities of smaller values made
+// up, outputs beside blocks of values 2^20 times theirs and no weight were up to 8e-4
+// off, D = 256; they are 4e-7 off with these.)  The scores' accumulators start at
+// 10 - log2 f_t, so it costs a softmax no operation; a block costs its tokens' maxima,
+// listed calls -2 to +2%.  R is an integer, raised only when a block exceeds it by more
+// than kTau: rescaling is exact, p' at most 2^(kTau + kPBits).  Causal rows
+// (suffix segments of a chunk) are masked per column, and blocks that no row of a wave
+// sees are skipped.
 #pragma once
 
 #include <type_traits>
@@ -105,9 +118,10 @@ __host__ __device__ constexpr int parts(int D)
     return waves(D) / images(D);
 }
 
-// LDS: the images, per image its scales and offsets ([group][32]
-// each) and two scalars, then per wave room to pass a block's scales and
-// offsets between lanes.  The merge of the waves reuses it from the start.
+// LDS: the images, per image its key scales and offsets ([group][32] each), its
+// tokens' powers of two (see TokenPowers) and two scalars, then per wave room to
+// pass a block's scales and offsets between lanes.  The merge of the waves reuses
+// it from the start.
 __host__ __device__ constexpr int key_bytes(int D, bool hilo)
 {
     return 64 * D * (hilo ? 2 : 1);
@@ -120,7 +134,7 @@ __host__ __device__ constexpr int image_bytes(int D, bool hilo)
 
 __host__ __device__ constexpr int meta_bytes(int D)
 {
-    return 2 * (D / 32) * 128 + 16;
+    return 2 * (D / 32) * 128 + 256 + 16;
 }
 
 __host__ __device__ constexpr int stage_bytes(int D)
@@ -162,8 +176,8 @@ __host__ __device__ constexpr int direct_tiles(int D, int bits, bool fp16)
     return D == 256 || bits == 8 || fp16 ? 1 : 2;
 }
 
-// Per wave: a block's key scales, offsets and scalars, then its value scales and
-// offsets, or (fp16 tokens) its values transposed, [D][kVtPitch].
+// Per wave: what an image has of scales, offsets and powers, then the block's value
+// scales and offsets, or (fp16 tokens) its values transposed, [D][kVtPitch].
 constexpr int kVtPitch = 40;  // halves
 
 __host__ __device__ constexpr int direct_region(int D, bool fp16)
@@ -209,15 +223,78 @@ __device__ __forceinline__ float wave_max(float x)
     return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(max_rows(x))));
 }
 
-// A power of two f with x f in (2^8, 2^12], its exponent a multiple of four, so
-// that neighbouring blocks mostly share it (x >= 0; f is kept within 2^-115 .. 2^113).
+// A power of two f with x f in (2^11, 2^12] (x >= 0; f is kept within 2^-115 .. 2^113).
 __device__ __forceinline__ float scale_to_range(float x)
 {
-    const uint32_t e = min(max(((__float_as_uint(x) >> 23) + 4) & ~3u, 26u), 254u);  // x < 2^(e - 127)
+    const uint32_t e = min(max((__float_as_uint(x) >> 23) + 1, 26u), 254u);  // x < 2^(e - 127)
     return __uint_as_float((254 + 12 - e) << 23);
 }
 
+// The larger of two pairs of 16-bit numbers, and of what a swap of lanes gives.
+__device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+template <class Swapped>
+__device__ __forceinline__ uint32_t max_swapped(const Swapped& x)
+{
+    return max_pairs(x[0], x[1]);
+}
+
+// The powers of two of a token's values: f brings its largest magnitude x (below
+// 2^(e - 127)) to 2^12 at most; start is what its scores begin with, 10 - log2 f;
+// weight, 2^-start, makes p' a weight again.  e >= 101 (f <= 2^38) leaves room
+// for every coded token, whose scale is 1e-8 or more.
+struct TokenPowers {
+    static constexpr uint32_t kLeast = 101;
+    uint32_t e;
+    __device__ __forceinline__ explicit TokenPowers(uint32_t e_, uint32_t least = kLeast) : e(min(max(e_, least), 254u)) {}
+    // Of a row of fp16 numbers with the sum of squares n2: f within fp16, 2^-8 .. 2^15
+    static __device__ __forceinline__ TokenPowers of_row(float n2)
+    {
+        return TokenPowers((uint32_t)max(127 + (((int)(__float_as_uint(n2) >> 23) - 125) >> 1), 0), 124);
+    }
+    __device__ __forceinline__ float f(int log2_pre = 0) const { return __uint_as_float((266 + log2_pre - e) << 23); }
+    __device__ __forceinline__ float start() const { return (float)((int)e - 129); }
+    __device__ __forceinline__ float weight() const { return __uint_as_float((256 - e) << 23); }
+};
+
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float add_squares(const u32x4& w, float sum)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f16x2 x = __builtin_bit_cast(f16x2, (uint32_t)w[j]);
+        sum = __builtin_amdgcn_fdot2(x, x, sum, false);
+    }
+    return sum;
+}
+
+// fp16 pairs (f_j, f_(j + 4)) of powers of two (natural order), and a value operand times them.
+__device__ __forceinline__ u32x4 pack_powers(const float* at)
+{
+    const float4 a = *(const float4*)at, b = *(const float4*)(at + 4);
+    const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[j], (_Float16)y[j]});
+    return w;
+}
+
+__device__ __forceinline__ half8 times_powers(const u32x4& v, const u32x4& f)
+{
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        w[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, (uint32_t)v[j]) *
+                                                __builtin_bit_cast(f16x2, (uint32_t)f[j]));
+    return __builtin_bit_cast(half8, w);
+}
+
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // fp32 -> fp16 hi + lo, both to nearest: |v - hi - lo| <= 2^-23 |v| (2^-25
@@ -448,16 +525,42 @@ struct Builder {
         }
     }
 
-    // The value scales of a coded block to st, [group][32]; returns the power of
-    // two (pre included) that they were multiplied with.
-    __device__ __forceinline__ float value_scales(const Loads& r, int live, float* st, float pre = 1.0f) const
+    // The value scales of a coded block, times 2^LOG2_PRE and each token's power of
+    // two, to st, [group][32], and the powers (start, weight: [32] each) to at.  Whether a
+    // token has 2^66 or more (uniform).
+    template <int LOG2_PRE>
+    __device__ __forceinline__ bool value_scales(const Loads& r, int live, float* st, float* at) const
     {
         float sv[NM], zv[NM];
         const float mid = coding<VB>(vaff).mid;
         widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
-        const float f = range_scale(sv, zv, mid, nv) * pre;
-        put(st, sv, zv, f, nv);
-        return f;
+        // |offset| + mid scale, their upper 16 bits in pairs: the largest of a token's
+        // groups, which are 32 / NM lanes apart
+        uint32_t any = 0;
+#pragma unroll
+        for (int e = 0; e < NM; e += 2) {
+            const uint32_t a = __float_as_uint(fmaf(mid, sv[e], fabsf(zv[e])));
+            const uint32_t b = NM > 1 ? __float_as_uint(fmaf(mid, sv[NM > 1 ? e + 1 : e], fabsf(zv[NM > 1 ? e + 1 : e]))) : 0u;
+            uint32_t top = NM * lane < nv ? __builtin_amdgcn_perm(b, a, 0x07060302u) : 0u;
+            if constexpr (NM == 4)
+                top = max_pairs(top, __builtin_amdgcn_update_dpp(0, top, 0x128, 0xF, 0xF, false));  // row_ror 8
+            if constexpr (NM > 1)
+                top = max_swapped(__builtin_amdgcn_permlane16_swap(top, top, false, false));
+            top = max_swapped(__builtin_amdgcn_permlane32_swap(top, top, false, false));
+            any = max_pairs(any, top);
+#pragma unroll
+            for (int i = e; i < e + 2 && i < NM; ++i) {
+                const TokenPowers t(((i & 1 ? top >> 16 : top & 0xFFFFu) >> 7) + 1);
+                sv[i] *= t.f(LOG2_PRE);
+                zv[i] *= t.f(LOG2_PRE);
+                if (NM * lane < 32) {
+                    at[NM * lane + i] = t.start();
+                    at[32 + NM * lane + i] = t.weight();
+                }
+            }
+        }
+        put(st, sv, zv, 1.0f, nv);
+        return __any(max(any & 0xFFFFu, any >> 16) >= (127 + 66) << 7);
     }
 
     // Eight reconstructed elements of the codes' operand a, hi + lo; s: their
@@ -503,7 +606,7 @@ struct Builder {
     }
 
     // This wave's part of the image of a coded block whose first `live` tokens
-    // exist.  img: the image; meta: its scales; st: this wave's stage.
+    // exist.  img: the image; meta: its scales and powers; st: this wave's stage.
     __device__ __forceinline__ void coded_image(const Loads& r, int live, uint8_t* img, float* meta, float* st) const
     {
         const float ksm = KH || part == 0 ? key_scales(r, live, meta, st) : 0.0f;
@@ -518,7 +621,8 @@ struct Builder {
                 *(half8*)(at + 64 * D) = lo;
         }
         lds_order();
-        const float vf = value_scales(r, live, st);
+        // (every wave of the block writes the same powers)
+        const bool huge = value_scales<0>(r, live, st, meta + 2 * D);
         lds_order();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -529,8 +633,8 @@ struct Builder {
             *(half8*)(at + 64 * D) = lo;
         }
         if (part == 0 && lane == 0) {
-            meta[2 * D] = vf;
-            meta[2 * D + 1] = ksm;
+            meta[2 * D + 64] = ksm;
+            meta[2 * D + 65] = huge;
         }
     }
 
@@ -565,7 +669,9 @@ struct Builder {
             row[j] = (uint32_t)((first + min(8 * (lane >> 4) + perm4(j), live - 1)) % ring * D + (lane & 15));
     }
 
-    __device__ __forceinline__ half8 value_row_piece(const uint16_t* vr, const uint32_t* row, int live, int i) const
+    // (times the tokens' powers)
+    __device__ __forceinline__ half8 value_row_piece(const uint16_t* vr, const uint32_t* row, const u32x4& powers, int live,
+                                                     int i) const
     {
         uint16_t h[8];
 #pragma unroll
@@ -577,7 +683,14 @@ struct Builder {
             w[j] = 8 * (lane >> 4) + j < live ? h[2 * j] : 0u;
             w[j] |= 8 * (lane >> 4) + j + 4 < live ? (uint32_t)h[2 * j + 1] << 16 : 0u;
         }
-        return __builtin_bit_cast(half8, w);
+        return times_powers(w, powers);
+    }
+
+    // A row's powers to at (start, weight), `start` more of the scores' start.
+    __device__ __forceinline__ void put_powers(const TokenPowers& t, int token, float* at, int start) const
+    {
+        at[token] = t.start() + (float)start;
+        at[32 + token] = t.weight() * __uint_as_float((uint32_t)(127 - start) << 23);
     }
 
     // The scales of fp16 rows: ones (times the softmax scale for code operands).
@@ -593,14 +706,26 @@ struct Builder {
             }
         }
         if (lane == 0) {
-            meta[2 * D] = 1.0f;
-            meta[2 * D + 1] = p.sm_log2;
+            meta[2 * D + 64] = p.sm_log2;
+            meta[2 * D + 65] = 0.0f;
         }
     }
 
     __device__ __forceinline__ void rows_image(const uint16_t* kr, const uint16_t* vr, int first, int ring, int live,
-                                               uint8_t* img, float* meta) const
+                                               uint8_t* img, float* meta, float* st) const
     {
+        // the tokens' powers: half a row per lane
+        const int token = lane >> 1;
+        const uint16_t* half_row = vr + (uint32_t)((first + min(token, live - 1)) % ring * D + D / 2 * (lane & 1));
+        float n2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            n2 = add_squares(*(const u32x4*)(half_row + 8 * i), n2);
+        const TokenPowers t = TokenPowers::of_row(n2 + dpp_f32<0xB1>(n2));  // quad_perm [1, 0, 3, 2]
+        st[token] = t.f();
+        put_powers(t, token, meta + 2 * D, 0);
+        lds_order();
+        const u32x4 powers = pack_powers(st + 8 * (lane >> 4));
         const half8 zero = {};
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
@@ -614,7 +739,7 @@ struct Builder {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             uint8_t* at = img + key_bytes(D, KH) + 1024 * (NV * part + i) + 16 * lane;
-            *(half8*)at = value_row_piece(vr, row, live, i);
+            *(half8*)at = value_row_piece(vr, row, powers, live, i);
             *(half8*)(at + 64 * D) = zero;
         }
         row_scales(meta);
@@ -626,14 +751,21 @@ struct Builder {
 // A power of two <= 1 by which scales in range_scale's range are at most one
 // (mid scale <= 2^12): the row side's operand x scale is no larger than x then.
 template <int BITS>
-__device__ __forceinline__ float to_one()
+__host__ __device__ constexpr int log2_to_one()
 {
-    return (BITS == 8 ? 128.0f : BITS == 4 ? 8.0f : 2.0f) / 4096.0f;
+    return BITS == 8 ? -5 : BITS == 4 ? -9 : -11;
+}
+
+template <int BITS>
+__device__ __forceinline__ constexpr float to_one()
+{
+    return 1.0f / (float)(1 << -log2_to_one<BITS>());
 }
 
 // A wave's state: NT tiles of 16 query rows (columns of the MFMAs).  KG: key
 // group size / 32 (0: per-channel scales).  ROT: rotated queries, hi + lo.
-// DIRECT: direct_kernel's, which takes value offsets apart.
+// DIRECT: direct_kernel's, which takes value offsets apart.  (The scores l of a block
+// include the tokens' starts; nl: where a block's starts and weights are.)
 template <int D, int KG, bool ROT, int CT, bool DIRECT>
 struct Rows {
     static constexpr int NKB = D / 32, NMB = D / 16;
@@ -647,8 +779,8 @@ struct Rows {
     float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg (ZM), or over group j
     floatx4 oacc[CT][NMB];
     float zacc[CT][DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
-    float m[CT], lsum[CT];   // running max (log2 units), lane partial sum (times 2^kPBits)
-    float vf;                // power of two that the accumulated values carry (uniform)
+    float m[CT], lsum[CT];   // reference of the probabilities (an integer), lane partial sum (times 2^kPBits)
+    bool apart;              // a token is so large that the sums are taken apart (uniform)
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
     int lim0, lim1;          // the least and the most of the wave's rows (uniform)
 
@@ -734,7 +866,7 @@ struct Rows {
 
     __device__ __forceinline__ void init()
     {
-        vf = 0.0f;
+        apart = false;
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
 #pragma unroll
@@ -761,13 +893,12 @@ struct Rows {
         }
     }
 
-    // Masks, the running maxima, and the values' power of two f (accumulators
-    // follow the largest values); shift and back are for probabilities().  The block is tokens t0
-    // .. t0 + 31 (tail indices; with `off` = the sink's size for sink blocks),
-    // the first `live` of which exist.
+    // Masks and the running references; shift is for probabilities().  The block is
+    // tokens t0 .. t0 + 31 (tail indices; with `off` = the sink's size for sink
+    // blocks), the first `live` of which exist.
     template <int NT>
-    __device__ __forceinline__ void settle(float (*l)[8], float f, int t0, int off, int live, int lane, float* shift,
-                                           float* back)
+    __device__ __forceinline__ void settle(float (*l)[8], const float* nl, bool huge, int t0, int off, int live, int lane,
+                                           float* shift)
     {
         const int qg = lane >> 4;
         if (live < 32 || t0 + 32 > lim0 + off) {
@@ -779,37 +910,13 @@ struct Rows {
                     l[c][k] = 8 * qg + k < valid ? l[c][k] : kNegInf;
             }
         }
-        float bias = kPBits;
-        *back = 1.0f;
-        if (f != vf) {
-            // log2(f / vf); from 2^40 on the products of the smaller values vanish
-            // beside the others, but their probabilities are to be counted
-            const int d = min((int)(__float_as_uint(f) >> 23) - (int)(__float_as_uint(vf) >> 23), 100);
-            const float r = __uint_as_float((uint32_t)max(127 + d, 0) << 23);
-            if (vf == 0.0f || d < 0) {
-                if (vf != 0.0f) {
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) {
-#pragma unroll
-                        for (int mb = 0; mb < NMB; ++mb)
-                            oacc[c][mb] *= r;
-                        scale_offsets(c, r);
-                    }
-                }
-                vf = f;
-            } else {
-                // smaller values: their probabilities make up for it
-                bias = kPBits - (float)d;
-                *back = r;
-            }
-        }
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             float bm = fmaxf(fmaxf(fmaxf(l[c][0], l[c][1]), fmaxf(l[c][2], l[c][3])),
                              fmaxf(fmaxf(l[c][4], l[c][5]), fmaxf(l[c][6], l[c][7])));
             if (__any(bm > m[c] + kTau)) {
                 bm = max_rows(bm);
-                const float mn = bm > m[c] + kTau ? bm : m[c];
+                const float mn = bm > m[c] + kTau ? __builtin_rintf(bm) : m[c];
                 const float alpha = m[c] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m[c] - mn);
                 m[c] = mn;
                 lsum[c] *= alpha;
@@ -819,31 +926,61 @@ struct Rows {
                 scale_offsets(c, alpha);
             }
             // (a column that has seen no token keeps m = -inf and gets zeros)
-            shift[c] = bias - (m[c] == kNegInf ? 0.0f : m[c]);
+            shift[c] = kPBits - (m[c] == kNegInf ? 0.0f : m[c]);
+        }
+        // Beside products of 2^66 and more the probabilities of small values leave
+        // binary32's range, but their weights are to be counted.
+        apart |= huge;
+        if (apart) {
+            float start[8];
+            load_natural(nl + 8 * qg, start);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                float top = kNegInf, sum = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    top = fmaxf(top, l[c][k] - start[k]);
+                top = max_rows(top);
+                top = top == kNegInf ? 0.0f : top;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    sum += __builtin_amdgcn_exp2f(l[c][k] - start[k] - top);
+                lsum[c] = fmaf(sum, __builtin_amdgcn_exp2f(top + shift[c]), lsum[c]);
+            }
         }
     }
 
-    // The probabilities of tile c in operand order, summed.
-    __device__ __forceinline__ void exponentials(int c, const float* l, float shift, float back, float* pv)
+    // The probabilities of tile c in operand order; summed as weights.
+    __device__ __forceinline__ void exponentials(int c, const float* l, const float* weight, float shift, float* pv)
     {
         float ps = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             pv[j] = __builtin_amdgcn_exp2f(l[perm4(j)] + shift);
-            ps += pv[j];
+            ps = fmaf(pv[j], weight[perm4(j)], ps);
         }
-        lsum[c] = fmaf(ps, back, lsum[c]);
+        lsum[c] += apart ? 0.0f : ps;
     }
 
     template <int NT>
-    __device__ __forceinline__ void probabilities(const float (*l)[8], const float* shift, float back, half8* ph, half8* pl)
+    __device__ __forceinline__ void probabilities(const float (*l)[8], const float* nl, const float* shift, int lane,
+                                                  half8* ph, half8* pl)
     {
+        float weight[8];
+        load_natural(nl + 32 + 8 * (lane >> 4), weight);
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             float pv[8];
-            exponentials(c, l[c], shift[c], back, pv);
+            exponentials(c, l[c], weight, shift[c], pv);
             split_nearest(pv, &ph[c], &pl[c]);
         }
+    }
+
+    static __device__ __forceinline__ void load_natural(const float* at, float* x)
+    {
+        const float4 a = *(const float4*)at, b = *(const float4*)(at + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+        x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     }
 
     // ---- The matrix products of an image in LDS.  Its fragments are read in the
@@ -894,9 +1031,9 @@ struct Rows {
     __device__ __forceinline__ void image_scores(half8* ring, const uint8_t* fb, const float* meta, bool affine, int lane,
                                                  float (*l)[8])
     {
-        const int qg = lane >> 4, hh = lane & 15;
+        const int qg = lane >> 4;
         constexpr int PER = KH ? 2 : 1, GF = KS * PER;  // fragments of a key piece, and of a group
-        const float ksm = KH ? meta[2 * D + 1] : 0.0f;
+        const float ksm = KH ? meta[2 * D + 64] : 0.0f;
         floatx4 S[NT], acc[NT], s4;
 #pragma unroll
         for (int k = 0; k < NKF; ++k) {
@@ -904,7 +1041,7 @@ struct Rows {
             if (kk == 0) {
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                    S[c] = *(const floatx4*)(meta + 2 * D + 8 * qg + 4 * e);
                 if constexpr (!KH && ZM) {
                     if (affine)
                         add_offset_products<NT>(S, meta, e, lane);
@@ -935,7 +1072,7 @@ struct Rows {
                 for (int c = 0; c < NT; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        S[c][i] = KH ? acc[c][i] * ksm : fmaf(s4[i], acc[c][i], S[c][i]);
+                        S[c][i] = fmaf(KH ? ksm : s4[i], acc[c][i], S[c][i]);
                 if constexpr (!KH && !ZM) {
                     if (affine)
                         add_group_offset<NT>(S, meta, g, e, lane);
@@ -988,7 +1125,7 @@ struct Rows {
             floatx4 S[NT];
 #pragma unroll
             for (int c = 0; c < NT; ++c)
-                S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                S[c] = *(const floatx4*)(meta + 2 * D + 8 * qg + 4 * e);
             if constexpr (ZM) {
                 if (affine)
                     add_offset_products<NT>(S, meta, e, lane);
@@ -1041,10 +1178,11 @@ struct Rows {
             sn[j] = x[perm4(j)];
     }
 
-    // The same with per-channel scales (CODED: scales s at st, offsets z D further):
+    // The same with per-channel scales (s at st, offsets z D further):
     // sum_d q_d (s_d c_d + z_d) = (q s) . c + q . z.
-    template <int NT, bool CODED, class Key>
-    __device__ __forceinline__ void channel_scores(Key key, const float* st, float ksm, int lane, float (*l)[8])
+    template <int NT, class Key>
+    __device__ __forceinline__ void channel_scores(Key key, const float* st, float ksm, const float* nl, int lane,
+                                                   float (*l)[8])
     {
         const int qg = lane >> 4;
         floatx4 acc[NT][2];
@@ -1057,28 +1195,19 @@ struct Rows {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
             half8 hi[NT], lo[NT];
-            if constexpr (CODED) {
-                float sn[8], zn[8];
-                load_scales(st + 32 * kb + 8 * qg, sn);
-                load_scales(st + D + 32 * kb + 8 * qg, zn);
+            float sn[8], zn[8];
+            load_scales(st + 32 * kb + 8 * qg, sn);
+            load_scales(st + D + 32 * kb + 8 * qg, zn);
 #pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    float x[8];
+            for (int c = 0; c < NT; ++c) {
+                float x[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float qf = (float)q[c][kb][j] + (ROT ? (float)ql[c][ROT ? kb : 0][j] : 0.0f);
-                        x[j] = qf * sn[j];
-                        z[c] = fmaf(qf, zn[j], z[c]);
-                    }
-                    split_nearest(x, &hi[c], &lo[c]);
+                for (int j = 0; j < 8; ++j) {
+                    const float qf = (float)q[c][kb][j] + (ROT ? (float)ql[c][ROT ? kb : 0][j] : 0.0f);
+                    x[j] = qf * sn[j];
+                    z[c] = fmaf(qf, zn[j], z[c]);
                 }
-            } else {
-#pragma unroll
-                for (int c = 0; c < NT; ++c) {
-                    hi[c] = q[c][kb];
-                    if constexpr (ROT)
-                        lo[c] = ql[c][kb];
-                }
+                split_nearest(x, &hi[c], &lo[c]);
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -1086,22 +1215,55 @@ struct Rows {
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
                     acc[c][e] = mfma16(a, hi[c], acc[c][e]);
-                if constexpr (CODED || ROT) {
 #pragma unroll
-                    for (int c = 0; c < NT; ++c)
-                        acc[c][e] = mfma16(a, lo[c], acc[c][e]);
-                }
+                for (int c = 0; c < NT; ++c)
+                    acc[c][e] = mfma16(a, lo[c], acc[c][e]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        float start[8];
+        load_natural(nl + 8 * qg, start);
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-            const float zs = CODED ? sum_rows(z[c]) : 0.0f;
+            const float zs = sum_rows(z[c]);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    l[c][4 * e + i] = (acc[c][e][i] + zs) * ksm;
+                    l[c][4 * e + i] = fmaf(acc[c][e][i] + zs, ksm, start[4 * e + i]);
+        }
+    }
+
+    // The same of fp16 rows, key(e, kb) after load(e); sm: what their products take.
+    template <int NT, class Load, class Key>
+    __device__ __forceinline__ void row_scores(Load load, Key key, float sm, const float* nl, int lane, float (*l)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            load(e);
+            floatx4 acc[NT];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+                acc[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+                const half8 a = key(e, kb);
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    acc[c] = mfma16(a, q[c][kb], acc[c]);
+                if constexpr (ROT) {
+#pragma unroll
+                    for (int c = 0; c < NT; ++c)
+                        acc[c] = mfma16(a, ql[c][kb], acc[c]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const floatx4 start = *(const floatx4*)(nl + 8 * (lane >> 4) + 4 * e);
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    l[c][4 * e + i] = fmaf(sm, acc[c][i], start[i]);
         }
     }
 
@@ -1179,8 +1341,16 @@ struct Rows {
         }
     }
 
-    // The partial of tile c, unscaled: m, l and this lane's channels 16 mb + 4 qg .. + 3 of row lane % 16.
-    __device__ __forceinline__ float inverse() const { return vf == 0.0f ? 0.0f : 1.0f / vf; }
+    // The partial of tile c: (m, l) with l in [1, 2), so that m is a weight's and not
+    // that of a product, and what the accumulators (of 2^(kPBits + 10) `pre`; this lane's
+    // channels 16 mb + 4 qg .. + 3 of row lane % 16) take.  Powers of two.
+    __device__ __forceinline__ float2 partial(int c, int log2_pre, float* scale) const
+    {
+        const uint32_t u = __float_as_uint(sum_rows(lsum[c])), e = u >> 23;  // e = 0: no token seen
+        *scale = e ? __uint_as_float((254 - e) << 23) * __uint_as_float((uint32_t)(117 - log2_pre) << 23) : 0.0f;
+        return e ? make_float2(m[c] + (float)((int)e - 127), __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u))
+                 : make_float2(kNegInf, 0.0f);
+    }
 };
 
 // ------------------------------------------------------------ work items
@@ -1382,7 +1552,7 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
                 B.coded_image(raw, min(32, p.nq - 32 * (mine - bl.nsb)), img, meta, st);
             } else {
                 const RowBlock rb(p, it.unit, bl, mine, D);
-                B.rows_image(rb.k, rb.v, rb.first, rb.ring, rb.live, img, meta);
+                B.rows_image(rb.k, rb.v, rb.first, rb.ring, rb.live, img, meta, st);
             }
         }
         raw = prefetch(mine + NI);
@@ -1415,12 +1585,12 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
                 const float* meta = (const float*)(metas + i * BM);
                 const Span s(p, bl, v + i);
                 const bool affine = B.kaff && (!ROWS || bl.coded(v + i));  // (fp16 rows have no offsets)
-                const float f = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D])));
-                float l[NT][8], shift[NT], back;
+                const bool huge = __builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D + 65])) != 0;
+                float l[NT][8], shift[NT];
                 half8 ph[NT], pl[NT];
                 T.template image_scores<NT>(ring, fb, meta, affine, lane, l);
-                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
-                T.template probabilities<NT>(l, shift, back, ph, pl);
+                T.template settle<NT>(l, meta + 2 * D, huge, s.t0, s.off, s.live, lane, shift);
+                T.template probabilities<NT>(l, meta + 2 * D, shift, lane, ph, pl);
                 T.template image_values<NT>(ring, fb, next, ph, pl);
                 i = j;
             }
@@ -1438,23 +1608,23 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
         walk(std::integral_constant<int, CT>{});
 
     // ---- partials: of each wave when its rows are its own, else merged in LDS
-    const float inv = T.inverse();
-    float* lo = (float*)lds;                          // [waves][16][pitch]
+    float* lo = (float*)lds;                     // [waves][16][pitch]
     float* lml = lo + W * 16 * merge_pitch(D);   // [waves][16][2]
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         if (R * c >= nt16)
             break;
-        const float l = sum_rows(T.lsum[c]);
+        float scale;
+        const float2 ml = T.partial(c, 0, &scale);
         const int r = 16 * (rw + R * c) + hh;
         if (BW == 1) {
             if (r < left) {
                 const size_t row = (size_t)it.part * sp.rows + global_row(sp, it, G, it.r0 + r);
 #pragma unroll
                 for (int mb = 0; mb < NMB; ++mb)
-                    *(floatx4*)(sp.part_o + row * D + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
+                    *(floatx4*)(sp.part_o + row * D + 16 * mb + 4 * qg) = T.oacc[c][mb] * scale;
                 if (qg == 0)
-                    *(float2*)(sp.part_ml + 2 * row) = make_float2(T.m[c], l);
+                    *(float2*)(sp.part_ml + 2 * row) = ml;
             }
             continue;
         }
@@ -1462,9 +1632,9 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
             sync_lds();
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb)
-            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
+            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * scale;
         if (qg == 0)
-            *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
+            *(float2*)(lml + 2 * (wave * 16 + hh)) = ml;
         sync_lds();
         for (int idx = threadIdx.x; idx < 16 * R * (D / 4); idx += 64 * W) {
             const int row = idx / (D / 4), d = 4 * (idx % (D / 4)), w = row >> 4, rr = 16 * (w + R * c) + (row & 15);
@@ -1485,7 +1655,9 @@ template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
 {
     constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves, CT = direct_tiles(D, KB, ROWS), PER = 16 * CT;
-    constexpr bool kAhead = D < 256;  // (two blocks' loads do not fit the registers of the widest heads)
+    // (two blocks' loads, or both halves of a block of fp16 keys, do not fit the
+    // registers of the widest heads)
+    constexpr bool kAhead = D < 256;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -1505,7 +1677,9 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     int vc = bl.v0 + wave;  // this wave's first block after the sink's
     while (ROWS && vc < bl.nsb)
         vc += W;
-    typename Build::Loads raw = prefetch(vc);
+    typename Build::Loads raw;
+    if constexpr (kAhead || !ROWS)
+        raw = prefetch(vc);
     Rows<D, KG, ROT, CT, true> T;
     T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
 #pragma unroll
@@ -1526,7 +1700,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
         const auto fp16_blocks = [&](int end) __attribute__((always_inline)) {
             for (; v < end; v += W) {
                 const Span s(p, bl, v);
-                float l[NT][8], pv[NT][8], shift[NT], back;
+                float l[NT][8], pv[NT][8], shift[NT], weight[8];
                 lds_order();
                 const RowBlock rb(p, it.unit, bl, v, D);
                 Build A = B;  // (the addresses below are made here, not kept in registers over the loop)
@@ -1535,7 +1709,9 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                 // channels of tokens t and t + 4, neighbours in the operand, 16 such
                 // pairs and 4 lanes of channels at a time: two lanes per bank.
                 constexpr int NV = (D < 128 ? D : 128) / 32;
-                u32x4 kw[2 * NKB];
+                constexpr int KN = kAhead ? 2 * NKB : NKB;  // key pieces at a time
+                u32x4 kw[KN];
+                float n2[2] = {0.0f, 0.0f};  // sums of squares of tokens t0 and t0 + 4
                 uint16_t* vt = (uint16_t*)st;
                 const int pair = A.lane >> 2, t0 = 2 * (pair & ~3) + (pair & 3), c8 = 8 * (A.lane & 3);
                 const uint32_t keep = (t0 < rb.live ? 0xFFFFu : 0u) | (t0 + 4 < rb.live ? 0xFFFF0000u : 0u);
@@ -1550,9 +1726,14 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                         for (int i = 0; i < NV; ++i)
                             vw[i][h] = *(const u32x4*)(row + 32 * (u + i));
                     }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
+                            n2[h] = add_squares(vw[i][h], n2[h]);
                     if (u + NV >= D / 32) {
 #pragma unroll
-                        for (int i = 0; i < 2 * NKB; ++i)
+                        for (int i = 0; i < KN; ++i)
                             kw[i] = A.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
                     }
 #pragma unroll
@@ -1564,45 +1745,72 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                                                          j & 1 ? 0x07060302u : 0x05040100u);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                A.row_scales(meta);
+                // the tokens' powers: starts and weights, and (where a coded block has its key
+                // offsets) fp16 pairs for the transposed values
+                float* nl = meta + 2 * D;
+                uint32_t* pairs = (uint32_t*)(meta + D);
+                {
+                    uint32_t f2 = 0;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        n2[h] += dpp_f32<0xB1>(n2[h]);  // the four lanes of a token
+                        n2[h] += dpp_f32<0x4E>(n2[h]);
+                        const TokenPowers t = TokenPowers::of_row(n2[h]);
+                        A.put_powers(t, t0 + 4 * h, nl, log2_to_one<VB>());
+                        f2 |= (uint32_t)f32_to_f16_bits(t.f()) << (16 * h);
+                    }
+                    pairs[pair] = f2;
+                }
                 lds_order();
-                const auto key = [&](int e, int kb) { return A.key_row_piece(kw[e * NKB + kb], rb.live, e * NKB + kb); };
-                if constexpr (KG == 0)
-                    T.template channel_scores<NT, false>(key, nullptr, p.sm_log2, lane, l);
-                else
-                    T.template group_scores<NT>(key, meta, false, lane, l);
-                T.template settle<NT>(l, 1.0f, s.t0, s.off, s.live, lane, shift, &back);
+                const auto load = [&](int e) {
+#pragma unroll
+                    for (int i = NKB; i < NKB + KN && !kAhead && e == 1; ++i)
+                        kw[i - NKB] = A.load_key_row(rb.k, rb.first, rb.ring, rb.live, i);
+                };
+                const auto key = [&](int e, int kb) {
+                    return A.key_row_piece(kw[(e * NKB + kb) % KN], rb.live, e * NKB + kb);
+                };
+                T.template row_scores<NT>(load, key, p.sm_log2, nl, lane, l);
+                T.template settle<NT>(l, nl, false, s.t0, s.off, s.live, lane, shift);
+                T.load_natural(nl + 32 + 8 * qg, weight);
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    T.exponentials(c, l[c], shift[c], back, pv[c]);
+                    T.exponentials(c, l[c], weight, shift[c], pv[c]);
                 const uint16_t* at = vt + hh * kVtPitch + 8 * qg;
-                T.template row_values<NT>([&](int mb) { return *(const half8*)(at + 16 * mb * kVtPitch); }, pv);
+                const u32x4 powers = *(const u32x4*)(pairs + 4 * qg);
+                T.template row_values<NT>(
+                    [&](int mb) { return times_powers(*(const u32x4*)(at + 16 * mb * kVtPitch), powers); }, pv);
             }
         };
         const int codes = ROWS ? min(bl.v1, bl.nsb + bl.ncb) : bl.v1;
         for (int part = 0; part < (ROWS ? 2 : 1); ++part) {
             if constexpr (ROWS)
                 fp16_blocks(part ? bl.v1 : min(bl.v1, bl.nsb));
+            if constexpr (!kAhead && ROWS) {
+                if (v < codes)
+                    raw = prefetch(v);
+            }
             for (; v < codes; v += W) {
                 const Span s(p, bl, v);
-                float l[NT][8], pv[NT][8], shift[NT], back;
+                float l[NT][8], pv[NT][8], shift[NT], weight[8], *nl = meta + 2 * D;
                 lds_order();
                 const typename Build::Loads now = raw;
                 if constexpr (kAhead)
                     raw = prefetch(v + W);
                 const int live = min(32, p.nq - s.t0);
                 const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
-                const float f = B.value_scales(now, live, st, to_one<VB>());
+                const bool huge = B.template value_scales<log2_to_one<VB>()>(now, live, st, nl);
                 lds_order();
                 const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
                 if constexpr (KG == 0)
-                    T.template channel_scores<NT, true>(key, meta, ksm, lane, l);
+                    T.template channel_scores<NT>(key, meta, ksm, nl, lane, l);
                 else
                     T.template group_scores<NT>(key, meta, B.kaff, lane, l);
-                T.template settle<NT>(l, f, s.t0, s.off, s.live, lane, shift, &back);
+                T.template settle<NT>(l, nl, huge, s.t0, s.off, s.live, lane, shift);
+                T.load_natural(nl + 32 + 8 * qg, weight);
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    T.exponentials(c, l[c], shift[c], back, pv[c]);
+                    T.exponentials(c, l[c], weight, shift[c], pv[c]);
                 T.template group_values<NT>([&](int mb) { return B.value_codes(now, mb); }, st, p.v_group, B.vaff, pv, lane);
                 if constexpr (!kAhead)
                     raw = prefetch(v + W);
@@ -1616,20 +1824,20 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     T.add_offsets(p.v_group);
 
     // ---- the waves' partials merged
-    const float inv = T.inverse();
     float* lo = (float*)lds;
     float* lml = lo + W * 16 * merge_pitch(D);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         if (16 * c >= left)
             break;
-        const float l = sum_rows(T.lsum[c]);
+        float scale;
+        const float2 ml = T.partial(c, log2_to_one<VB>(), &scale);
         __syncthreads();
 #pragma unroll
         for (int mb = 0; mb < NMB; ++mb)
-            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * inv;
+            *(floatx4*)(lo + (wave * 16 + hh) * merge_pitch(D) + 16 * mb + 4 * qg) = T.oacc[c][mb] * scale;
         if (qg == 0)
-            *(float2*)(lml + 2 * (wave * 16 + hh)) = make_float2(T.m[c], l);
+            *(float2*)(lml + 2 * (wave * 16 + hh)) = ml;
         __syncthreads();
         for (int idx = threadIdx.x; idx < min(left - 16 * c, 16) * (D / 4); idx += kDirectThreads) {
             const int r = idx / (D / 4), d = 4 * (idx % (D / 4));
