@@ -343,13 +343,15 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * has sink tokens and a window of its own).  The codes of a prefix are read
  * once per 16 query rows (sequence, query, head of a group) of its group, of
  * calls of much work once per 128 (D = 256) or 256, instead of once per
- * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16), and its limits.
+ * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16).
+ * Queries and coded tokens may have any magnitude below 2^100, fp16 tokens (window,
+ * sink) below 65504.  Every query row is scaled by a power of two of its own, so
+ * the size of queries beside that of the softmax scale costs no precision.
  * A product of a weight and a value is off by at most 2^-22 of the weight times
  * its token's largest value, or by 2^-32 of the largest such product of the
- * row, whatever the sizes of other tokens' values (values of coded tokens below
- * 2^100, of fp16 tokens below 65504).  Sums are fp32 and run in an order that
- * depends on the shapes, the groups and the lengths alone, so a call gives the
- * same bits every time. */
+ * row, whatever the sizes of other tokens' values.  Sums are fp32 and run in an
+ * order that depends on the shapes, the groups and the lengths alone, so a call
+ * gives the same bits every time. */
 
 /* Workspace bytes for calls of up to C queries per sequence at any lengths and
  * groups of these caches (contents need no initialization; calls that share a

@@ -65,9 +65,9 @@
 //     sum_t p'_t (f_t / 2^10) = 2^kPBits sum_t 2^(x_t - R).
 // (With one power of two per block, for which the probabilities of smaller values made
 // up, outputs beside blocks of values 2^20 times theirs and no weight were up to 8e-4
-// off, D = 256; they are 4e-7 off with these.)  The scores' accumulators start at
-// 10 - log2 f_t, so it costs a softmax no operation; a block costs its tokens' maxima,
-// listed calls -2 to +2%.  R is an integer, raised only when a block exceeds it by more
+// off, D = 256; they are 4e-7 off with these.)  The scores are multiplied
+// by their query's power of two anyway, so the addition of 10 - log2 f_t costs nothing;
+// a block costs its tokens' maxima, listed calls -2 to +2%.  R is an integer, raised only when a block exceeds it by more
 // than kTau: rescaling is exact, p' at most 2^(kTau + kPBits).  Causal rows
 // (suffix segments of a chunk) are masked per column, and blocks that no row of a wave
 // sees are skipped.
@@ -777,6 +777,7 @@ struct Rows {
     static constexpr int NZ = ZM ? (NG + 3) / 4 : NG;
     half8 q[CT][NKB], ql[ROT ? CT : 1][ROT ? NKB : 1];
     float qz[CT][NZ];        // lane (col, qg): the query's sum over group 4 j + qg (ZM), or over group j
+    float qinv[CT];          // q and qz are this column's query divided by it
     floatx4 oacc[CT][NMB];
     float zacc[CT][DIRECT ? D / 32 : 1];  // this lane's sum of p x value offset, at the first 32 channels of each group
     float m[CT], lsum[CT];   // reference of the probabilities (an integer), lane partial sum (times 2^kPBits)
@@ -784,7 +785,12 @@ struct Rows {
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
     int lim0, lim1;          // the least and the most of the wave's rows (uniform)
 
-    // Query rows of tile c, this lane's at src (channels 32 kb + 8 qg .. + 7 of it).
+    // Query rows of tile c, this lane's at src (channels 32 kb + 8 qg .. + 7 of it),
+    // each times a power of two of its own that brings its largest element to 2^7 ..
+    // 2^8 (the transform adds at most four bits): fp16 operands of small queries would
+    // be subnormal.  (Per row, not per workgroup: a row of a padded batch may hold
+    // anything.)  Queries of 2^-10: 1e-5 off without it, 3e-4 with per-channel keys;
+    // 5e-7 and 7e-7 with it.  It costs the scores of keys in groups a product.
     __device__ __forceinline__ void load_query(int c, const uint16_t* src, float rot_c, int lane)
     {
         const int qg = lane >> 4;
@@ -798,6 +804,15 @@ struct Rows {
                 v[kb][2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
             }
         }
+        float top = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                top = fmaxf(top, fabsf(v[kb][j]));
+        const uint32_t e = max(__float_as_uint(max_rows(top)) >> 23, 34u);  // top < 2^(e - 126)
+        const float g = __uint_as_float((261 - e) << 23) * (ROT ? rot_c : 1.0f);
+        qinv[c] = __uint_as_float((e - 7) << 23);
         if constexpr (ROT) {
             // the transform's butterflies commute: channel bits 0..2 and 5.. are
             // in this lane's registers, bits 3 and 4 are lanes 16 and 32 apart
@@ -844,7 +859,7 @@ struct Rows {
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                x[j] = v[kb][perm4(j)] * (ROT ? rot_c : 1.0f);
+                x[j] = v[kb][perm4(j)] * g;
                 sum[kb / KS] += x[j];
             }
             if constexpr (ROT)
@@ -1026,6 +1041,18 @@ struct Rows {
                 S[c][i] = fmaf(z[i], qz[c][g], S[c][i]);
     }
 
+    // The scores of half e from its sums and the tokens' starts; sm: what the sums take beside the query's power.
+    template <int NT>
+    __device__ __forceinline__ void finish(const floatx4* S, float sm, const float* nl, int e, int lane, float (*l)[8]) const
+    {
+        const floatx4 start = *(const floatx4*)(nl + 8 * (lane >> 4) + 4 * e);
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                l[c][4 * e + i] = fmaf(S[c][i], sm * qinv[c], start[i]);
+    }
+
     // The scores of the image at fb; the ring holds its first fragments.
     template <int NT>
     __device__ __forceinline__ void image_scores(half8* ring, const uint8_t* fb, const float* meta, bool affine, int lane,
@@ -1041,7 +1068,7 @@ struct Rows {
             if (kk == 0) {
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    S[c] = *(const floatx4*)(meta + 2 * D + 8 * qg + 4 * e);
+                    S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
                 if constexpr (!KH && ZM) {
                     if (affine)
                         add_offset_products<NT>(S, meta, e, lane);
@@ -1072,19 +1099,14 @@ struct Rows {
                 for (int c = 0; c < NT; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        S[c][i] = fmaf(KH ? ksm : s4[i], acc[c][i], S[c][i]);
+                        S[c][i] = KH ? acc[c][i] : fmaf(s4[i], acc[c][i], S[c][i]);
                 if constexpr (!KH && !ZM) {
                     if (affine)
                         add_group_offset<NT>(S, meta, g, e, lane);
                 }
             }
-            if (kk == NKF / 2 - 1) {
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        l[c][4 * e + i] = S[c][i];
-            }
+            if (kk == NKF / 2 - 1)
+                finish<NT>(S, KH ? ksm : 1.0f, meta + 2 * D, e, lane, l);
         }
     }
 
@@ -1125,7 +1147,7 @@ struct Rows {
             floatx4 S[NT];
 #pragma unroll
             for (int c = 0; c < NT; ++c)
-                S[c] = *(const floatx4*)(meta + 2 * D + 8 * qg + 4 * e);
+                S[c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (ZM) {
                 if (affine)
                     add_offset_products<NT>(S, meta, e, lane);
@@ -1160,11 +1182,7 @@ struct Rows {
                         add_group_offset<NT>(S, meta, g, e, lane);
                 }
             }
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    l[c][4 * e + i] = S[c][i];
+            finish<NT>(S, 1.0f, meta + 2 * D, e, lane, l);
         }
     }
 
@@ -1221,16 +1239,16 @@ struct Rows {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        float start[8];
-        load_natural(nl + 8 * qg, start);
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            const float zs = sum_rows(z[c]);
+        for (int c = 0; c < NT; ++c)
+            z[c] = sum_rows(z[c]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+            floatx4 S[NT];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    l[c][4 * e + i] = fmaf(acc[c][e][i] + zs, ksm, start[4 * e + i]);
+            for (int c = 0; c < NT; ++c)
+                S[c] = acc[c][e] + z[c];
+            finish<NT>(S, ksm, nl, e, lane, l);
         }
     }
 
@@ -1258,12 +1276,7 @@ struct Rows {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            const floatx4 start = *(const floatx4*)(nl + 8 * (lane >> 4) + 4 * e);
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    l[c][4 * e + i] = fmaf(sm, acc[c][i], start[i]);
+            finish<NT>(acc, sm, nl, e, lane, l);
         }
     }
 
