@@ -341,8 +341,8 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * A prefix and its suffix are attended as if they were one cache (sinks,
  * window and coded groups are those of the two caches as they are: a suffix
  * has sink tokens and a window of its own).  The codes of a prefix are read
- * once per 16 query rows (sequence, query, head of a group) of its group, of
- * calls of much work once per 128 (D = 256) or 256, instead of once per
+ * once per 16 or 32 query rows (sequence, query, head of a group) of its group,
+ * of calls of much work once per 128 (D = 256) or 256, instead of once per
  * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16).
  * Queries and coded tokens may have any magnitude below 2^100, fp16 tokens (window,
  * sink) below 65504.  Every query row is scaled by a power of two of its own, so

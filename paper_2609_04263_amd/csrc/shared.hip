@@ -23,21 +23,35 @@ int ceil_div(int a, int b)
     return (a + b - 1) / b;
 }
 
+// Key group size / 32, 0 for per-channel keys.
+int key_groups(const AttnParams& a)
+{
+    return a.k_axis == KVQ_PER_CHANNEL ? 0 : a.k_group / 32;
+}
+
 // How a segment's rows are taken.
 struct Kind {
     bool direct;
     int per, step, round;  // rows per item, blocks that a range is a multiple of, items of a round
+    int most;              // direct: the work up to which it takes everything (all_direct), in 1024s
 };
 
-Kind direct_kind(int D, int bits, bool fp16)
+Kind direct_kind(int D, int kg, int bits, bool rot, bool fp16)
 {
-    return {true, kTile * shr::direct_tiles(D, bits, fp16), shr::kDirectWaves, kDirectRound};
+    const int tiles = shr::direct_tiles(D, kg, bits, rot, fp16);
+    const int most = D == 256 ? 12 : tiles == 2 ? 64 : bits == 8 || fp16 ? 24 : 40;
+    return {true, kTile * tiles, shr::kDirectWaves, kDirectRound, most};
+}
+
+Kind direct_kind(int D, const AttnParams& a)
+{
+    return direct_kind(D, key_groups(a), a.k_bits, a.rotate, a.ring > 0 || a.sink > 0);
 }
 
 Kind image_kind(int D, int rows)
 {
     const int per = shr::item_rows(D), n16 = ceil_div(rows < per ? rows : per, 16);
-    return {false, per, shr::waves(D) / shr::row_waves(D, n16), kImageRound};
+    return {false, per, shr::waves(D) / shr::row_waves(D, n16), kImageRound, 0};
 }
 
 // Whether the direct kernel takes everything: `rows` the most that a unit of the
@@ -47,16 +61,20 @@ Kind image_kind(int D, int rows)
 // launch of its own, the conversion before its first product, the merge of a wave's
 // partials and the join of more of them: 16 to 25 us.  Direct / image, us, at
 // `work` in 1024s:
-//     two tiles  D = 64    64 rows  30 / 39 (32)   256 rows  43 / 50 (64)   72 / 71 (128)
-//                D = 128   64 rows  45 / 57 (32)   256 rows  72 / 77 (64)   97 / 94 (96)
-//                rotated                           256 rows  60 / 67 (32)   94 / 91 (69)
-//     one tile   D = 128, per-channel keys         256 rows  45 / 52 (16)   71 / 60 (32)
-//                D = 256   64 rows  43 / 48 (8)    128 rows  49 / 50 (8)    69 / 61 (16)
+//     two tiles  D = 64    64 rows  29 / 37 (32)   256 rows  42 / 48 (64)   72 / 70 (128)
+//                D = 128   64 rows  44 / 53 (32)   256 rows  71 / 77 (64)   98 / 94 (96)
+//     one tile, no wide codes or fp16 tokens
+//                D = 128, rotated   128 rows  52 / 57 (32)  72 / 68 (48)    256 rows  51 / 68 (32)  90 / 84 (64)
+//                groups of 32       128 rows  58 / 72 (32)  81 / 88 (48)    256 rows  56 / 74 (32)  99 / 98 (64)
+//     one tile   D = 128, per-channel keys   64 rows  40 / 44 (16)  52 / 51 (24)   256 rows  63 / 62 (32)
+//                8 bits                      64 rows  32 / 32 (8)   62 / 51 (24)   256 rows  79 / 62 (32)
+//                D = 64, 8 bits              64 rows  33 / 36 (32)                 256 rows  31 / 36 (32)  54 / 48 (64)
+//                D = 256   64 rows  44 / 46 (8)   128 rows  49 / 52 (8)  69 / 62 (16)   256 rows  54 / 66 (9)
 // Units of two tiles would leave most of an image kernel's waves idle: 32 rows of
 // 8192 tokens, 8 prefixes, D = 256, 110 / 141 us.
-bool all_direct(int D, int rows, long long work, const Kind& k)
+bool all_direct(int rows, long long work, const Kind& k)
 {
-    return rows <= 2 * kTile || work <= (D == 256 ? 12 : k.per == kTile ? 24 : 64) * 1024;
+    return rows <= 2 * kTile || work <= k.most * 1024;
 }
 
 // Ranges that a segment of `tiles` tiles is cut into, at most.
@@ -183,8 +201,8 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
         most = rows > most ? rows : most;
         work += (long long)a.H * ceil_div(rows, kTile) * nb[0];
     }
-    const Kind few = direct_kind(D, a.k_bits, a.ring > 0 || a.sink > 0);
-    const bool direct = kernels ? kernels == 1 : all_direct(D, most, work, few);
+    const Kind few = direct_kind(D, a);
+    const bool direct = kernels ? kernels == 1 : all_direct(most, work, few);
     const Kind kind[2] = {direct ? few : image_kind(D, most),
                           direct || (!kernels && own <= 2 * kTile) ? few : image_kind(D, own)};
     p->tiles0 = 0;
@@ -217,7 +235,7 @@ size_t shared_partials_bound(int B, int H, int D, int C, int G)
     // Unlike S this does not fall as C grows.
     const auto segment = [&](size_t units, int u) {
         size_t most = units * u;
-        for (const Kind& k : {image_kind(D, u), direct_kind(D, 2, false)}) {
+        for (const Kind& k : {image_kind(D, u), direct_kind(D, 2, 2, false, false)}) {
             const size_t cut = (size_t)k.round * (u < k.per ? u : k.per);
             most = cut > most ? cut : most;
         }
@@ -229,9 +247,8 @@ size_t shared_partials_bound(int B, int H, int D, int C, int G)
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
-    const int kg = a.k_axis == KVQ_PER_CHANNEL ? 0 : a.k_group / 32;
     hipError_t e = hipErrorInvalidValue;
-    switch (1000 * D + kg) {
+    switch (1000 * D + key_groups(a)) {
 #define KVQ_FAMILY(D, KG)                           \
     case 1000 * D + KG:                             \
         e = launch_shared_##D##_##KG(p, stream);        \

@@ -169,11 +169,14 @@ __host__ __device__ constexpr int row_waves(int D, int n16)
 constexpr int kDirectWaves = 4, kDirectThreads = 64 * kDirectWaves;
 
 // 16-row tiles of a wave, which shares a block's codes between them: as many as
-// fit the registers beside wide codes or the conversion of fp16 tokens (96
-// sequences at D = 64: 24.5 us, 31 with one tile).
-__host__ __device__ constexpr int direct_tiles(int D, int bits, bool fp16)
+// fit the registers beside wide codes or the conversion of fp16 tokens and, at
+// D = 128, the lo halves of rotated queries or the scales of groups of 32.  Two tiles /
+// one, us: 96 sequences at D = 64 26 / 37, D = 128 (4-bit groups of 64) 256 rows
+// 50 / 50 (16384 tokens), 71 / 89 (32768); where two spill, 32 sequences of 4096 tokens
+// and more: rotated 41 / 31, 4-bit groups of 32 62 / 34, 2-bit 50 / 28.
+__host__ __device__ constexpr int direct_tiles(int D, int kg, int bits, bool rot, bool fp16)
 {
-    return D == 256 || bits == 8 || fp16 ? 1 : 2;
+    return D == 256 || bits == 8 || fp16 || (D == 128 && (kg == 1 || rot)) ? 1 : 2;
 }
 
 // Per wave: what an image has of scales, offsets and powers, then the block's value
@@ -1667,7 +1670,7 @@ __host__ __device__ constexpr int direct_waves(int D)
 template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
 __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
 {
-    constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves, CT = direct_tiles(D, KB, ROWS), PER = 16 * CT;
+    constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves, CT = direct_tiles(D, KG, KB, ROT, ROWS), PER = 16 * CT;
     // (two blocks' loads, or both halves of a block of fp16 keys, do not fit the
     // registers of the widest heads)
     constexpr bool kAhead = D < 256;
