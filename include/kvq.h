@@ -344,8 +344,8 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
  * once per 16 or 32 query rows (sequence, query, head of a group) of its group,
  * of calls of much work once per 128 (D = 256) or 256, instead of once per
  * sequence.  H_q as for kvq_decode_attn (H_q / H_kv <= 16).
- * Queries and coded tokens may have any magnitude below 2^100, fp16 tokens (window,
- * sink) below 65504.  Every query row is scaled by a power of two of its own, so
+ * Queries may have any magnitude below 2^100, coded tokens below 2^64, fp16 tokens
+ * (window, sink) below 65504.  Every query row is scaled by a power of two of its own, so
  * the size of queries beside that of the softmax scale costs no precision.
  * A product of a weight and a value is off by at most 2^-22 of the weight times
  * its token's largest value, or by 2^-32 of the largest such product of the

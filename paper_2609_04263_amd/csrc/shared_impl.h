@@ -67,7 +67,7 @@
 // up, outputs beside blocks of values 2^20 times theirs and no weight were up to 8e-4
 // off, D = 256; they are 4e-7 off with these.)  The scores are multiplied
 // by their query's power of two anyway, so the addition of 10 - log2 f_t costs nothing;
-// a block costs its tokens' maxima, listed calls -2 to +2%.  R is an integer, raised only when a block exceeds it by more
+// a block costs its tokens' maxima: -4 to +3% with the queries' powers.  R is an integer, raised only when a block exceeds it by more
 // than kTau: rescaling is exact, p' at most 2^(kTau + kPBits).  Causal rows
 // (suffix segments of a chunk) are masked per column, and blocks that no row of a wave
 // sees are skipped.
@@ -216,6 +216,12 @@ __device__ __forceinline__ float dpp_f32(float x)
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, false));
 }
 
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t x)
+{
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, false);
+}
+
 // The largest x >= 0 of the wave.
 __device__ __forceinline__ float wave_max(float x)
 {
@@ -276,18 +282,7 @@ __device__ __forceinline__ float add_squares(const u32x4& w, float sum)
     return sum;
 }
 
-// fp16 pairs (f_j, f_(j + 4)) of powers of two (natural order), and a value operand times them.
-__device__ __forceinline__ u32x4 pack_powers(const float* at)
-{
-    const float4 a = *(const float4*)at, b = *(const float4*)(at + 4);
-    const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-    u32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        w[j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[j], (_Float16)y[j]});
-    return w;
-}
-
+// A value operand times its tokens' powers, fp16 pairs (f_j, f_(j + 4)).
 __device__ __forceinline__ half8 times_powers(const u32x4& v, const u32x4& f)
 {
     u32x4 w;
@@ -534,7 +529,7 @@ struct Builder {
     template <int LOG2_PRE>
     __device__ __forceinline__ bool value_scales(const Loads& r, int live, float* st, float* at) const
     {
-        float sv[NM], zv[NM];
+        float sv[NM], zv[NM], start[NM], weight[NM];
         const float mid = coding<VB>(vaff).mid;
         widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
         // |offset| + mid scale, their upper 16 bits in pairs: the largest of a token's
@@ -546,7 +541,7 @@ struct Builder {
             const uint32_t b = NM > 1 ? __float_as_uint(fmaf(mid, sv[NM > 1 ? e + 1 : e], fabsf(zv[NM > 1 ? e + 1 : e]))) : 0u;
             uint32_t top = NM * lane < nv ? __builtin_amdgcn_perm(b, a, 0x07060302u) : 0u;
             if constexpr (NM == 4)
-                top = max_pairs(top, __builtin_amdgcn_update_dpp(0, top, 0x128, 0xF, 0xF, false));  // row_ror 8
+                top = max_pairs(top, dpp_u32<0x128>(top));  // row_ror 8
             if constexpr (NM > 1)
                 top = max_swapped(__builtin_amdgcn_permlane16_swap(top, top, false, false));
             top = max_swapped(__builtin_amdgcn_permlane32_swap(top, top, false, false));
@@ -556,10 +551,15 @@ struct Builder {
                 const TokenPowers t(((i & 1 ? top >> 16 : top & 0xFFFFu) >> 7) + 1);
                 sv[i] *= t.f(LOG2_PRE);
                 zv[i] *= t.f(LOG2_PRE);
-                if (NM * lane < 32) {
-                    at[NM * lane + i] = t.start();
-                    at[32 + NM * lane + i] = t.weight();
-                }
+                start[i] = t.start();
+                weight[i] = t.weight();
+            }
+        }
+        if (part == 0 && NM * lane < 32) {
+#pragma unroll
+            for (int e = 0; e < NM; ++e) {
+                at[NM * lane + e] = start[e];
+                at[32 + NM * lane + e] = weight[e];
             }
         }
         put(st, sv, zv, 1.0f, nv);
@@ -624,7 +624,6 @@ struct Builder {
                 *(half8*)(at + 64 * D) = lo;
         }
         lds_order();
-        // (every wave of the block writes the same powers)
         const bool huge = value_scales<0>(r, live, st, meta + 2 * D);
         lds_order();
 #pragma unroll
@@ -672,9 +671,7 @@ struct Builder {
             row[j] = (uint32_t)((first + min(8 * (lane >> 4) + perm4(j), live - 1)) % ring * D + (lane & 15));
     }
 
-    // (times the tokens' powers)
-    __device__ __forceinline__ half8 value_row_piece(const uint16_t* vr, const uint32_t* row, const u32x4& powers, int live,
-                                                     int i) const
+    __device__ __forceinline__ u32x4 value_row_piece(const uint16_t* vr, const uint32_t* row, int live, int i) const
     {
         uint16_t h[8];
 #pragma unroll
@@ -686,7 +683,7 @@ struct Builder {
             w[j] = 8 * (lane >> 4) + j < live ? h[2 * j] : 0u;
             w[j] |= 8 * (lane >> 4) + j + 4 < live ? (uint32_t)h[2 * j + 1] << 16 : 0u;
         }
-        return times_powers(w, powers);
+        return w;
     }
 
     // A row's powers to at (start, weight), `start` more of the scores' start.
@@ -714,21 +711,15 @@ struct Builder {
         }
     }
 
+    // The image of a block of fp16 rows in two parts, a barrier between them: the
+    // rows, whose tokens' largest magnitudes among this wave's values (pairs of fp16,
+    // tokens 8 qg + j and + 4) go to st; then the values times their tokens' powers, from
+    // the maxima of all of the block's waves (their stages lie at sts).  (Every wave
+    // reading all of the values for their maxima is a read's latency more per turn: 158
+    // us instead of 145, 200 KIVI tokens after 2048 at D = 256.)
     __device__ __forceinline__ void rows_image(const uint16_t* kr, const uint16_t* vr, int first, int ring, int live,
                                                uint8_t* img, float* meta, float* st) const
     {
-        // the tokens' powers: half a row per lane
-        const int token = lane >> 1;
-        const uint16_t* half_row = vr + (uint32_t)((first + min(token, live - 1)) % ring * D + D / 2 * (lane & 1));
-        float n2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-            n2 = add_squares(*(const u32x4*)(half_row + 8 * i), n2);
-        const TokenPowers t = TokenPowers::of_row(n2 + dpp_f32<0xB1>(n2));  // quad_perm [1, 0, 3, 2]
-        st[token] = t.f();
-        put_powers(t, token, meta + 2 * D, 0);
-        lds_order();
-        const u32x4 powers = pack_powers(st + 8 * (lane >> 4));
         const half8 zero = {};
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
@@ -739,13 +730,62 @@ struct Builder {
         }
         uint32_t row[8];
         value_rows(first, ring, live, row);
+        u32x4 top = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             uint8_t* at = img + key_bytes(D, KH) + 1024 * (NV * part + i) + 16 * lane;
-            *(half8*)at = value_row_piece(vr, row, powers, live, i);
+            const u32x4 v = value_row_piece(vr, row, live, i);
+            *(u32x4*)at = v;
             *(half8*)(at + 64 * D) = zero;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                top[j] = max_pairs(top[j], v[j] & 0x7FFF7FFFu);
         }
         row_scales(meta);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t x = top[j];
+            x = max_pairs(x, dpp_u32<0xB1>(x));  // the 16 lanes of a token
+            x = max_pairs(x, dpp_u32<0x4E>(x));
+            x = max_pairs(x, dpp_u32<0x141>(x));
+            x = max_pairs(x, dpp_u32<0x140>(x));
+            top[j] = x;
+        }
+        if ((lane & 15) == 0)
+            *(u32x4*)(st + (lane >> 2)) = top;
+    }
+
+    __device__ __forceinline__ void rows_scale(const uint8_t* sts, uint8_t* img, float* meta) const
+    {
+        const int qg = lane >> 4;
+        u32x4 f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            f[j] = 0;
+#pragma unroll
+        for (int q = 0; q < PB; ++q) {
+            const u32x4 x = *(const u32x4*)(sts + stage_bytes(D) * q + 16 * qg);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                f[j] = max_pairs(f[j], x[j]);
+        }
+        // fp16 exponents E, at least 11: a magnitude is below 2^(E - 14), f = 2^(26 - E)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            f[j] = max_pairs(f[j] & 0x7C007C00u, 0x2C002C00u);
+        if (part == 0 && (lane & 15) == 0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                put_powers(TokenPowers(113 + (f[k & 3] >> (k < 4 ? 10 : 26) & 31)), 8 * qg + k, meta + 2 * D, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            f[j] = 0xA400A400u - f[j];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            uint8_t* at = img + key_bytes(D, KH) + 1024 * (NV * part + i) + 16 * lane;
+            *(half8*)at = times_powers(*(const u32x4*)at, f);
+        }
     }
 };
 
@@ -946,7 +986,7 @@ struct Rows {
             // (a column that has seen no token keeps m = -inf and gets zeros)
             shift[c] = kPBits - (m[c] == kNegInf ? 0.0f : m[c]);
         }
-        // Beside products of 2^66 and more the probabilities of small values leave
+        // Beside values of 2^66 and more the probabilities of small ones leave
         // binary32's range, but their weights are to be counted.
         apart |= huge;
         if (apart) {
@@ -1561,9 +1601,9 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
     float* st = (float*)(metas + NI * BM + stage_bytes(D) * wave);
     const auto build = [&](int v) __attribute__((always_inline)) {  // the turn that starts at block v
         const int mine = v + own;
+        uint8_t* img = lds + own * BI;
+        float* meta = (float*)(metas + own * BM);
         if (mine < bl.v1) {
-            uint8_t* img = lds + own * BI;
-            float* meta = (float*)(metas + own * BM);
             if (!ROWS || bl.coded(mine)) {
                 B.coded_image(raw, min(32, p.nq - 32 * (mine - bl.nsb)), img, meta, st);
             } else {
@@ -1572,6 +1612,13 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
             }
         }
         raw = prefetch(mine + NI);
+        if constexpr (ROWS) {
+            if (v < bl.nsb || min(v + NI, bl.v1) > bl.nsb + bl.ncb) {  // a turn with fp16 rows
+                sync_lds();
+                if (mine < bl.v1 && !bl.coded(mine))
+                    B.rows_scale(metas + NI * BM + stage_bytes(D) * own * PB, img, meta);
+            }
+        }
     };
     // (two loops, so that the registers of a wave's tiles have one place in each)
     const auto walk = [&](auto tiles_now) __attribute__((always_inline)) {
