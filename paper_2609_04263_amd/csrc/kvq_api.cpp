@@ -1023,6 +1023,26 @@ kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* 
     return KVQ_OK;
 }
 
+// A checked call's parameters and plan, without its tensors.
+static kvq::SharedParams shared_params(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
+                                       int H_q, float sm_scale, int kernels)
+{
+    const int P = prefix->B, B = suffix->B;
+    kvq::SharedParams p = {};
+    p.seg[0] = shared_segment(prefix, H_q, sm_scale);
+    p.seg[1] = shared_segment(suffix, H_q, sm_scale);
+    p.rows = (size_t)B * C * H_q;
+    p.C = C;
+    p.H_q = H_q;
+    p.P = P;
+    p.rotate = suffix->fmt.rotate;
+    p.rot_c = rotation_constant(suffix->D);
+    for (int g = 0; g <= P; ++g)
+        p.first[g] = first ? first[g] : B / P * g;
+    kvq::shared_plan(&p, suffix->D, B, kernels);
+    return p;
+}
+
 // The queries of the newest C tokens of every sequence; `self` tells whether
 // those tokens have to be in the suffix.
 static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
@@ -1045,22 +1065,11 @@ static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, 
     size_t off_ml;
     if (ws_bytes < shared_workspace_layout(suffix, C, H_q, &off_ml))
         return KVQ_ERR_WORKSPACE;
-    kvq::SharedParams p = {};
-    p.seg[0] = shared_segment(prefix, H_q, sm_scale);
-    p.seg[1] = shared_segment(suffix, H_q, sm_scale);
+    kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, sm_scale, kernels);
     p.q = (const uint16_t*)Q;
     p.out = (float*)O;
     p.part_o = (float*)workspace;
     p.part_ml = (float*)((uint8_t*)workspace + off_ml);
-    p.rows = (size_t)B * C * H_q;
-    p.C = C;
-    p.H_q = H_q;
-    p.P = P;
-    p.rotate = suffix->fmt.rotate;
-    p.rot_c = rotation_constant(suffix->D);
-    for (int g = 0; g <= P; ++g)
-        p.first[g] = first ? first[g] : B / P * g;
-    kvq::shared_plan(&p, suffix->D, B, kernels);
     return kvq::launch_shared(p, suffix->D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
@@ -1158,6 +1167,13 @@ int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src, int in_pl
     memcpy(pairs, ops.get(), sizeof(kvq::GatherOp) * (size_t)n);
     *ordered = dep;
     return n;
+}
+
+size_t kvq_internal_shared_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C, int H_q,
+                                    int kernels)
+{
+    const kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, 1.0f, kernels);
+    return (size_t)(p.S[0] + p.S[1]) * p.rows;
 }
 
 int kvq_internal_project_tile(int M, int N)

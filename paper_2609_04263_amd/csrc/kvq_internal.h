@@ -271,5 +271,8 @@ extern "C" int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src
 extern "C" kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
                                                const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
                                                size_t ws_bytes, int self, void* stream, int kernels);
+// The partials that such a call writes (of arguments that it would not refuse).
+extern "C" size_t kvq_internal_shared_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
+                                               int H_q, int kernels);
 extern "C" int kvq_internal_prefill_ranges(const kvq_cache* cache, int C, int H_q);
 extern "C" int kvq_internal_prefill_tile_rows(const kvq_cache* cache, int C, int H_q);
