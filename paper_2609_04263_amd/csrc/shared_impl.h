@@ -47,10 +47,10 @@
 // fp16 tokens (window, sink) are operands as they are, with a lo half of zero.
 //
 // What bounds them (MI355X): image_kernel, 64 sequences x 4 heads per KV head, 32768
-// rotated tokens at D = 128, 102 us: the matrix pipes 0.40 and the vector pipes 0.36 of
+// rotated tokens at D = 128, 91 us: the matrix pipes 0.43 and the vector pipes 0.40 of
 // its waves' time, which add up instead of overlapping whatever the waves' order,
 // priority or number (sixteen waves at D = 128: 15% slower); without LDS reads 2% faster.
-// 850 TFLOP/s of executed products, where a large library product reaches 1160.
+// 940 TFLOP/s of executed products, where a large library product reaches 1160.
 // direct_kernel: vector operations of the conversions, and at small sizes the
 // latency of one block after another.
 //
