@@ -239,17 +239,11 @@ __device__ __forceinline__ float scale_to_range(float x)
     return __uint_as_float((254 + 12 - e) << 23);
 }
 
-// The larger of two pairs of 16-bit numbers, and of what a swap of lanes gives.
+// The larger of two pairs of 16-bit numbers.
 __device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b)
 {
     typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-
-template <class Swapped>
-__device__ __forceinline__ uint32_t max_swapped(const Swapped& x)
-{
-    return max_pairs(x[0], x[1]);
 }
 
 // The powers of two of a token's values: f brings its largest magnitude x (below
@@ -386,11 +380,11 @@ __device__ __forceinline__ half8 centred(const uint32_t* w, int k, uint32_t cent
 
 // The loads of one wave's part of a coded block: NK key pieces and NV value
 // pieces per lane, and of the block's key and value scales and offsets (at most
-// D of each) D / 64 numbers in NW words.
-template <int KB, int VB, int NK, int NV, int NW>
+// D of each) NM = D / 64 numbers, the keys' in NW words.
+template <int KB, int VB, int NK, int NV, int NM, int NW>
 struct Raw {
     uint32_t k[NK * KB / 4], v[NV * VB / 4];
-    uint32_t ks[NW], kz[NW], vs[NW], vz[NW];
+    uint32_t ks[NW], kz[NW], vs[NM], vz[NM];
 };
 
 // N bytes (2 to 128, aligned to N or 16) from global memory, streaming.
@@ -421,12 +415,14 @@ template <int D, bool KH, int KB, int VB, bool M16, int PB>
 struct Builder {
     static constexpr int NKB = D / 32, NMB = D / 16, NK = 2 * NKB / PB, NV = NMB / PB;
     static constexpr int NM = D / 64, ESZ = M16 ? 2 : 4;  // numbers of a lane, and their bytes
-    typedef Raw<KB, VB, NK, NV, (NM * ESZ + 3) / 4> Loads;
+    typedef Raw<KB, VB, NK, NV, NM, (NM * ESZ + 3) / 4> Loads;
     const AttnParams& p;
     int unit, part, lane;
     int nk, nv;        // key and value scales of a block
     bool kaff, vaff;
-    const uint8_t *k, *v, *ks, *vs;  // this lane's pieces and numbers of block 0
+    const uint8_t *k, *v, *ks;       // this lane's pieces and numbers of block 0
+    const uint8_t* vs;               // the unit's value scales
+    uint32_t vlane;                  // this lane's first of a block
     long dkz, dvz;                   // offsets - scales (0 when symmetric: the scales once more)
 
     // key piece i of the lane: half block and 32-channel block
@@ -444,7 +440,8 @@ struct Builder {
         k = (const uint8_t*)p.kc + ((ub0 * 2 + half(0)) * 64 + lane) * (NKB * KB) + kblock(0) * KB;
         v = (const uint8_t*)p.vc + (ub0 * 64 + lane) * (NMB * VB) + NV * part * VB;
         ks = (const uint8_t*)p.ks + (ub0 * nk + min(NM * lane, nk - NM)) * ESZ;
-        vs = (const uint8_t*)p.vs + (ub0 * nv + min(NM * lane, nv - NM)) * ESZ;
+        vs = (const uint8_t*)p.vs + ub0 * nv * ESZ;
+        vlane = (nv < 64 ? lane & 31 : lane) * ESZ;
         dkz = kaff ? (const uint8_t*)p.kz - (const uint8_t*)p.ks : 0;
         dvz = vaff ? (const uint8_t*)p.vz - (const uint8_t*)p.vs : 0;
     }
@@ -463,22 +460,40 @@ struct Builder {
         const uint8_t *a = ks + (size_t)blk * (nk * ESZ), *b = vs + (size_t)blk * (nv * ESZ);
         load_bytes<NM * ESZ>(a, r.ks);
         load_bytes<NM * ESZ>(a + dkz, r.kz);
-        load_bytes<NM * ESZ>(b, r.vs);
-        load_bytes<NM * ESZ>(b + dvz, r.vz);
+        // Value numbers 64 e + lane, so that a lane's are all of one token, lane % 32
+        // (past the last group: the first ones once more).
+#pragma unroll
+        for (int e = 0; e < NM; ++e) {
+            const uint8_t* at = b + (64 * e < nv ? 64 * e * ESZ : 0);
+            load_bytes<ESZ>(at + vlane, r.vs + e);
+            load_bytes<ESZ>(at + dvz + vlane, r.vz + e);
+        }
     }
 
-    // This lane's scales, and offsets of the centred codes.  Dead tokens (number i
-    // is token i % 32 of a group, unless `whole`) give zeros.
-    __device__ __forceinline__ void widen(const uint32_t* s, const uint32_t* z, bool aff, float mid, int live, bool whole,
-                                          float* sv, float* zv) const
+    // A scale and the offset of its centred codes; zeros of a dead token.
+    __device__ __forceinline__ void widen(uint16_t s, uint16_t z, bool aff, float mid, bool on, float* sv, float* zv) const
+    {
+        widen(f16_bits_to_f32(s), f16_bits_to_f32(z), aff, mid, on, sv, zv);
+    }
+
+    __device__ __forceinline__ void widen(float s, float z, bool aff, float mid, bool on, float* sv, float* zv) const
+    {
+        *sv = on ? s : 0.0f;
+        *zv = on && aff ? fmaf(mid, *sv, z) : 0.0f;
+    }
+
+    // This lane's key scales and offsets (number NM lane + e is token (NM lane + e) % 32
+    // of a group, unless `whole`).
+    __device__ __forceinline__ void widen_keys(const Loads& r, float mid, int live, bool whole, float* sv, float* zv) const
     {
 #pragma unroll
         for (int e = 0; e < NM; ++e) {
-            sv[e] = M16 ? f16_bits_to_f32((uint16_t)(s[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(s[e]);
-            zv[e] = M16 ? f16_bits_to_f32((uint16_t)(z[e >> 1] >> (16 * (e & 1)))) : __uint_as_float(z[e]);
             const bool on = whole || ((NM * lane + e) & 31) < live;
-            sv[e] = on ? sv[e] : 0.0f;
-            zv[e] = on && aff ? fmaf(mid, sv[e], zv[e]) : 0.0f;
+            if constexpr (M16)
+                widen((uint16_t)(r.ks[e >> 1] >> (16 * (e & 1))), (uint16_t)(r.kz[e >> 1] >> (16 * (e & 1))), kaff, mid, on,
+                      sv + e, zv + e);
+            else
+                widen(__uint_as_float(r.ks[e]), __uint_as_float(r.kz[e]), kaff, mid, on, sv + e, zv + e);
         }
     }
 
@@ -512,7 +527,7 @@ struct Builder {
     {
         float sv[NM], zv[NM];
         const float mid = coding<KB>(kaff).mid;
-        widen(r.ks, r.kz, kaff, mid, live, KH, sv, zv);
+        widen_keys(r, mid, live, KH, sv, zv);
         if constexpr (KH) {
             const float f = range_scale(sv, zv, mid, nk) * pre;
             put(st, sv, zv, f, nk);
@@ -529,41 +544,31 @@ struct Builder {
     template <int LOG2_PRE>
     __device__ __forceinline__ bool value_scales(const Loads& r, int live, float* st, float* at) const
     {
-        float sv[NM], zv[NM], start[NM], weight[NM];
+        float sv[NM], zv[NM], top = 0.0f;
         const float mid = coding<VB>(vaff).mid;
-        widen(r.vs, r.vz, vaff, mid, live, false, sv, zv);
-        // |offset| + mid scale, their upper 16 bits in pairs: the largest of a token's
-        // groups, which are 32 / NM lanes apart
-        uint32_t any = 0;
+        const bool on = (lane & 31) < live;
 #pragma unroll
-        for (int e = 0; e < NM; e += 2) {
-            const uint32_t a = __float_as_uint(fmaf(mid, sv[e], fabsf(zv[e])));
-            const uint32_t b = NM > 1 ? __float_as_uint(fmaf(mid, sv[NM > 1 ? e + 1 : e], fabsf(zv[NM > 1 ? e + 1 : e]))) : 0u;
-            uint32_t top = NM * lane < nv ? __builtin_amdgcn_perm(b, a, 0x07060302u) : 0u;
-            if constexpr (NM == 4)
-                top = max_pairs(top, dpp_u32<0x128>(top));  // row_ror 8
-            if constexpr (NM > 1)
-                top = max_swapped(__builtin_amdgcn_permlane16_swap(top, top, false, false));
-            top = max_swapped(__builtin_amdgcn_permlane32_swap(top, top, false, false));
-            any = max_pairs(any, top);
-#pragma unroll
-            for (int i = e; i < e + 2 && i < NM; ++i) {
-                const TokenPowers t(((i & 1 ? top >> 16 : top & 0xFFFFu) >> 7) + 1);
-                sv[i] *= t.f(LOG2_PRE);
-                zv[i] *= t.f(LOG2_PRE);
-                start[i] = t.start();
-                weight[i] = t.weight();
-            }
+        for (int e = 0; e < NM; ++e) {
+            if constexpr (M16)
+                widen((uint16_t)r.vs[e], (uint16_t)r.vz[e], vaff, mid, on, sv + e, zv + e);
+            else
+                widen(__uint_as_float(r.vs[e]), __uint_as_float(r.vz[e]), vaff, mid, on, sv + e, zv + e);
+            top = fmaxf(top, fmaf(mid, sv[e], fabsf(zv[e])));
         }
-        if (part == 0 && NM * lane < 32) {
+        auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+        const TokenPowers t((__float_as_uint(top) >> 23) + 1);
+        // (numbers past the last group go to room that nobody reads)
 #pragma unroll
-            for (int e = 0; e < NM; ++e) {
-                at[NM * lane + e] = start[e];
-                at[32 + NM * lane + e] = weight[e];
-            }
+        for (int e = 0; e < NM; ++e) {
+            st[64 * e + lane] = sv[e] * t.f(LOG2_PRE);
+            st[D + 64 * e + lane] = zv[e] * t.f(LOG2_PRE);
         }
-        put(st, sv, zv, 1.0f, nv);
-        return __any(max(any & 0xFFFFu, any >> 16) >= (127 + 66) << 7);
+        if (part == 0 && lane < 32) {
+            at[lane] = t.start();
+            at[32 + lane] = t.weight();
+        }
+        return __any(top >= 0x1p66f);
     }
 
     // Eight reconstructed elements of the codes' operand a, hi + lo; s: their
@@ -955,8 +960,7 @@ struct Rows {
     // tokens t0 .. t0 + 31 (tail indices; with `off` = the sink's size for sink
     // blocks), the first `live` of which exist.
     template <int NT>
-    __device__ __forceinline__ void settle(float (*l)[8], const float* nl, bool huge, int t0, int off, int live, int lane,
-                                           float* shift)
+    __device__ __forceinline__ void settle(float (*l)[8], const float* nl, int t0, int off, int live, int lane, float* shift)
     {
         const int qg = lane >> 4;
         if (live < 32 || t0 + 32 > lim0 + off) {
@@ -988,7 +992,6 @@ struct Rows {
         }
         // Beside values of 2^66 and more the probabilities of small ones leave
         // binary32's range, but their weights are to be counted.
-        apart |= huge;
         if (apart) {
             float start[8];
             load_natural(nl + 8 * qg, start);
@@ -1638,6 +1641,7 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
             int i = seen(bw);
             if (i >= n)
                 return;
+            T.apart |= __any(((const uint32_t*)(metas + min(lane, n - 1) * BM))[2 * D + 65] != 0);
             half8 ring[T.kAhead];
 #pragma unroll
             for (int k = 0; k < T.kAhead; ++k)
@@ -1648,11 +1652,10 @@ __global__ __launch_bounds__(64 * waves(D), waves(D) / 4) void image_kernel(Shar
                 const float* meta = (const float*)(metas + i * BM);
                 const Span s(p, bl, v + i);
                 const bool affine = B.kaff && (!ROWS || bl.coded(v + i));  // (fp16 rows have no offsets)
-                const bool huge = __builtin_amdgcn_readfirstlane(__float_as_uint(meta[2 * D + 65])) != 0;
                 float l[NT][8], shift[NT];
                 half8 ph[NT], pl[NT];
                 T.template image_scores<NT>(ring, fb, meta, affine, lane, l);
-                T.template settle<NT>(l, meta + 2 * D, huge, s.t0, s.off, s.live, lane, shift);
+                T.template settle<NT>(l, meta + 2 * D, s.t0, s.off, s.live, lane, shift);
                 T.template probabilities<NT>(l, meta + 2 * D, shift, lane, ph, pl);
                 T.template image_values<NT>(ring, fb, next, ph, pl);
                 i = j;
@@ -1834,7 +1837,7 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                     return A.key_row_piece(kw[(e * NKB + kb) % KN], rb.live, e * NKB + kb);
                 };
                 T.template row_scores<NT>(load, key, p.sm_log2, nl, lane, l);
-                T.template settle<NT>(l, nl, false, s.t0, s.off, s.live, lane, shift);
+                T.template settle<NT>(l, nl, s.t0, s.off, s.live, lane, shift);
                 T.load_natural(nl + 32 + 8 * qg, weight);
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
@@ -1862,14 +1865,14 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
                     raw = prefetch(v + W);
                 const int live = min(32, p.nq - s.t0);
                 const float ksm = B.key_scales(now, live, meta, meta, to_one<KB>());
-                const bool huge = B.template value_scales<log2_to_one<VB>()>(now, live, st, nl);
+                T.apart |= B.template value_scales<log2_to_one<VB>()>(now, live, st, nl);
                 lds_order();
                 const auto key = [&](int e, int kb) { return B.key_codes(now, e * NKB + kb); };
                 if constexpr (KG == 0)
                     T.template channel_scores<NT>(key, meta, ksm, nl, lane, l);
                 else
                     T.template group_scores<NT>(key, meta, B.kaff, lane, l);
-                T.template settle<NT>(l, nl, huge, s.t0, s.off, s.live, lane, shift);
+                T.template settle<NT>(l, nl, s.t0, s.off, s.live, lane, shift);
                 T.load_natural(nl + 32 + 8 * qg, weight);
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
