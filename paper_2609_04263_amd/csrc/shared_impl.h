@@ -47,10 +47,10 @@
 // fp16 tokens (window, sink) are operands as they are, with a lo half of zero.
 //
 // What bounds them (MI355X): image_kernel, 64 sequences x 4 heads per KV head, 32768
-// rotated tokens at D = 128, 91 us: the matrix pipes 0.43 and the vector pipes 0.40 of
+// rotated tokens at D = 128, 92 us: the matrix pipes 0.42 and the vector pipes 0.39 of
 // its waves' time, which add up instead of overlapping whatever the waves' order,
 // priority or number (sixteen waves at D = 128: 15% slower); without LDS reads 2% faster.
-// 940 TFLOP/s of executed products, where a large library product reaches 1160.
+// 930 TFLOP/s of executed products, where a large library product reaches 1160.
 // direct_kernel: vector operations of the conversions, and at small sizes the
 // latency of one block after another.
 //
@@ -65,12 +65,12 @@
 //     sum_t p'_t (f_t / 2^10) = 2^kPBits sum_t 2^(x_t - R).
 // (With one power of two per block, for which the probabilities of smaller values made
 // up, outputs beside blocks of values 2^20 times theirs and no weight were up to 8e-4
-// off, D = 256; they are 4e-7 off with these.)  The scores are multiplied
-// by their query's power of two anyway, so the addition of 10 - log2 f_t costs nothing;
-// a block costs its tokens' maxima: -4 to +3% with the queries' powers.  R is an integer, raised only when a block exceeds it by more
-// than kTau: rescaling is exact, p' at most 2^(kTau + kPBits).  Causal rows
-// (suffix segments of a chunk) are masked per column, and blocks that no row of a wave
-// sees are skipped.
+// off, D = 256; they are 4e-7 off with these.)  The scores are multiplied by
+// their query's power of two anyway, so the addition of 10 - log2 f_t costs nothing; a
+// block costs its tokens' maxima: -3 to +4% of listed calls with the queries' powers.
+// R is an integer, raised only when a block exceeds it by more than kTau: rescaling is
+// exact, p' at most 2^(kTau + kPBits).  Causal rows (suffix segments of a chunk) are
+// masked per column, and blocks that no row of a wave sees are skipped.
 #pragma once
 
 #include <type_traits>
