@@ -230,6 +230,86 @@ kvq_status kvq_merge_adapter(const void* W, int d_in, int d_q, int d_kv, const v
 kvq_status kvq_append(kvq_cache* cache, const void* K, const void* V, int n_new,
                       const kvq_format* fmt, void* stream);
 
+/* ---- Rotary positions of queries and keys, and the RMS norm of each head that
+ * some models put before them: what a layer does between its projection and its
+ * attention.  The paper does not place positions; this library takes them where
+ * its path has room for them, before keys are coded.
+ *
+ * A row x of D channels (bf16) becomes, in binary32 without contraction,
+ *   norm (weight w given)   r = fl(1 / sqrt(sum x^2 / D + eps)), the right side
+ *                           in binary64;  y = fl(fl(x r) w);  else y = x
+ *   pair (a, b), angle      f = frac(t turns[i]) of a turn (t the position, the
+ *                           product exact);  c, s = fl(scale cos, scale sin);
+ *                           a' = fl(fl(a c) - fl(b s)), b' = fl(fl(b c) + fl(a s))
+ * and is rounded once to bf16.  Pair i < rot / 2 is channels (i, i + rot / 2)
+ * or, interleaved, (2 i, 2 i + 1); channels from rot on are y.  So results are
+ * functions of the input, bit for bit but for the roundings of the sum of
+ * squares and of c and s, which a binary64 evaluation shares in all but about
+ * one of 10^8 cases. */
+#define KVQ_ROPE_PAIRS 128
+enum { KVQ_ROPE_HALF = 0, KVQ_ROPE_INTERLEAVED = 1 };
+typedef struct {
+    int32_t rot;    /* rotated channels of a head: 0 to D, a multiple of 16 */
+    int32_t layout; /* KVQ_ROPE_HALF or KVQ_ROPE_INTERLEAVED */
+    float scale;    /* multiplies cosines and sines */
+    float eps;      /* of the norms, >= 0 (a row of zeros needs more) */
+    double turns[KVQ_ROPE_PAIRS]; /* turns (of 2 pi) per position of pair i < rot / 2, at most 1 in magnitude */
+} kvq_rope;
+
+/* Fill *rope (host memory) with the frequencies f_i = base^(-2 i / rot) radians
+ * per position, scaled for contexts `factor` (>= 1) times the original:
+ *   KVQ_ROPE_PLAIN   as they are (factor and what follows are not read)
+ *   KVQ_ROPE_LINEAR  f_i / factor
+ *   KVQ_ROPE_BASE    of a base multiplied by factor^(rot / (rot - 2)), which
+ *                    leaves the first and divides the last by factor
+ *   KVQ_ROPE_BANDS   by the waves w_i = original f_i / (2 pi) that pair i makes
+ *                    in the original length: k f_i + (1 - k) f_i / factor with
+ *                    k = (w_i - low) / (high - low) clamped to [0, 1]
+ *   KVQ_ROPE_YARN    the same with k falling linearly in i from 1 at pair
+ *                    floor(d(high)) to 0 at ceil(d(low)), both within [0, rot - 1],
+ *                    d(w) = rot ln(original / (2 pi w)) / (2 ln base) being the
+ *                    pair of w waves; scale = 0.1 ln(factor) + 1 (else 1)
+ * eps is set to 1e-6.  A caller may change any field, or fill in frequencies of
+ * its own.  rot a multiple of 16 up to 256, base > 1. */
+enum { KVQ_ROPE_PLAIN = 0, KVQ_ROPE_LINEAR = 1, KVQ_ROPE_BASE = 2, KVQ_ROPE_BANDS = 3, KVQ_ROPE_YARN = 4 };
+kvq_status kvq_rope_init(kvq_rope* rope, int rot, int layout, double base, int scaling, double factor,
+                         double original, double low, double high);
+
+/* Norm and rotate the queries and keys of n tokens of B sequences.
+ *   rope            host memory, read during the call
+ *   Q, Qo  bf16 [B][n][H_q][D]   (NULL with H_q == 0: no queries)
+ *   K, Ko  bf16 [B][n][H_kv][D]  (NULL with H_kv == 0: no keys)
+ *                   (the natural views of the projection's outputs); an output
+ *                   may be its input, and must not overlap anything else
+ *   q_norm, k_norm  bf16 [D], the weights of the norms; NULL: no norm
+ *   pos             device int32 [B][n], the tokens' positions (any order, equal
+ *                   or negative ones too: the depths of a drafted tree),
+ *                   aligned to 4 bytes; NULL: token i of every sequence is at
+ *                   pos0 + i
+ * D 64, 128 or 256; rope->rot <= D; B n (H_q + H_kv) below 2^31.  n == 0 is a
+ * no-op. */
+kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B, int n, int H_q, int H_kv, int D,
+                       const void* q_norm, const void* k_norm, const int32_t* pos, int pos0, void* Qo, void* Ko,
+                       void* stream);
+
+/* kvq_append of keys that are normed and rotated on the way: the storage bytes
+ * are those that kvq_append writes of kvq_rope_qk's Ko and of V, without Ko
+ * ever reaching memory.
+ *   K, V   bf16 [B][n_in][H_kv][D]
+ *   rows   device int32 [B][n_new]: token j appended to sequence b is row
+ *          rows[b][j] of its n_in (the accepted ones of drafted tokens; any
+ *          order, the same row more than once; an entry outside 0 .. n_in - 1
+ *          is taken as the nearest of them), aligned to 4 bytes; NULL: the
+ *          first n_new rows
+ *   Q, Qo  bf16 [B][n_new][H_q][D]: these tokens' queries, as kvq_rope_qk; NULL
+ *          with H_q == 0: none.  With rows there must be none.
+ *   q_norm, k_norm, pos [B][n_new], pos0  as kvq_rope_qk, of the tokens appended
+ * Everything else as kvq_append. */
+kvq_status kvq_append_rope(kvq_cache* cache, const kvq_rope* rope, const void* K, const void* V, int n_in,
+                           const int32_t* rows, int n_new, const void* Q, int H_q, const void* q_norm,
+                           const void* k_norm, const int32_t* pos, int pos0, void* Qo, const kvq_format* fmt,
+                           void* stream);
+
 /* Copy sequences between caches: sequence b of dst becomes the first n tokens
  * of sequence rows[b] of src, for every b (forking a prompt's cache into
  * samples, reordering beams, moving the survivors of a batch together).

@@ -6,7 +6,7 @@ Every source is compiled by hipcc for gfx950 only, in-tree, into
 * ``-fhip-fp32-correctly-rounded-divide-sqrt`` and
   ``-fno-gpu-flush-denormals-to-zero``: IEEE binary32 division and denormals,
   so the coder's scales and codes are bit-exact;
-* ``-ffp-contract=off`` for ``append.hip`` (no fused multiply-add in the coder);
+* ``-ffp-contract=off`` for ``append.hip`` and ``rope.hip`` (no fused multiply-add in the coder and the rotation);
 * packed fp32 instructions disabled for all device code;
 * mixed-precision FMA instructions (v_fma_mix*/v_mad_mix*) disabled: the
   attention kernel splits fp32 operands into fp16 hi + lo parts, and on
@@ -39,6 +39,7 @@ _NO_NANS = ["-fno-honor-nans"]
 # prefill kernels once per head size, the shared-prefix kernels once per (head
 # size, key group / 32, 0 for per-channel keys).
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
+         ("append.hip", "append_rope", ["-ffp-contract=off", "-DKVQ_APPEND_ROPE"]), ("rope.hip", "rope", ["-ffp-contract=off"]),
          ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
          ("gather.hip", "gather", []), ("shared.hip", "shared", [])]
 UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64, 128, 256)]

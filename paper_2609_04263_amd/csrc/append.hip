@@ -24,12 +24,88 @@
 // key piece P is row + 16 (P % 4); value piece (octet o, channel d) belongs
 // to lane d % 16 + 16 o.
 
+#include <type_traits>
+
 #include "coder.h"
 #include "kvq_device.h"
 #include "kvq_internal.h"
+#include "rope.h"
 
 namespace kvq {
 namespace {
+
+// The kernels are built for two kinds of parameters P: AppendParams, and
+// AppendRopeParams, whose keys are normed and rotated (rope.h) and rounded to
+// bf16 as they are loaded, so that the coder sees what kvq_rope_qk would have
+// written, and whose rows may be chosen by an index.
+template <typename P>
+constexpr bool kRope = std::is_same<P, AppendRopeParams>::value;
+
+// Row [sequence, token] of kin and vin that token i of the call is taken from.
+template <typename P>
+__device__ __forceinline__ size_t input_row(const P& p, int b, int i)
+{
+    if constexpr (kRope<P>) {
+        const int r = p.rows ? p.rows[(size_t)b * p.n_new + i] : i;
+        return (size_t)b * p.n_in + min(max(r, 0), p.n_in - 1);
+    } else {
+        return (size_t)b * p.n_new + i;
+    }
+}
+
+// Position of token i of the call.
+__device__ __forceinline__ int input_position(const AppendRopeParams& p, int b, int i)
+{
+    return p.rope.pos ? p.rope.pos[(size_t)b * p.n_new + i] : p.rope.pos0 + i;
+}
+
+// A key row held by D / 8 consecutive lanes, eight channels each (piece P of the
+// row): normed, rotated and rounded to bf16.  Every lane computes the angles of
+// four pairs; in the half layout a piece and its partner rot / 16 pieces on need
+// the same eight, and each other's channels (16 exchanges).
+template <int D>
+__device__ __forceinline__ void rope_row8(const RopeArgs& r, int t, int P, float* v)
+{
+#pragma clang fp contract(off)
+    if (r.wk) {
+        const float f = norm_factor(row_sum<D / 8>(squares8(v)), D, r.eps);
+        float g[8];
+        widen8(*(const u32x4*)(r.wk + 8 * P), g);
+        norm8(v, f, g);
+    }
+    if (r.layout == KVQ_ROPE_HALF) {
+        const int hp = r.rot / 16, lane = threadIdx.x & 63;
+        const bool in = P < 2 * hp, up = in && P >= hp;
+        const int base = up ? 8 * (P - hp) + 4 : 8 * P, other = in ? (up ? lane - hp : lane + hp) : lane;
+        float2 mine[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            mine[j] = in ? rope_cos_sin(t, r.turns[base + j], r.scale) : make_float2(1.0f, 0.0f);
+        float c[8], s[8], y[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float oc = __shfl(mine[j].x, other), os = __shfl(mine[j].y, other);
+            c[j] = up ? oc : mine[j].x, s[j] = up ? os : mine[j].y;
+            c[j + 4] = up ? mine[j].x : oc, s[j + 4] = up ? mine[j].y : os;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            y[e] = __shfl(v[e], other);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = v[e] * c[e], b = y[e] * s[e];
+            v[e] = in ? (up ? a + b : a - b) : v[e];
+        }
+    } else if (8 * P < r.rot) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 cs = rope_cos_sin(t, r.turns[4 * P + j], r.scale);
+            turn_pair(v[2 * j], v[2 * j + 1], cs.x, cs.y);
+        }
+    }
+    const u32x4 w = narrow8(v);
+    widen8(w, v);
+}
 
 constexpr int kThreads = 256;
 constexpr int kBlockTok = 32;
@@ -98,7 +174,8 @@ struct RowStage {
 
     // Issue the loads (bf16 input for tokens of this call, fp16 window slots
     // for tokens appended earlier).
-    __device__ void load(const AppendParams& p, int which, int b, int h, int tb)
+    template <typename P>
+    __device__ __forceinline__ void load(const P& p, int which, int b, int h, int tb)
     {
         const uint16_t* in = which ? p.vin : p.kin;
         const uint16_t* ring = which ? p.vr : p.kr;
@@ -107,14 +184,16 @@ struct RowStage {
             const int t = tb + row(k), d8 = chan(k);
             w[k] = u32x4{0u, 0u, 0u, 0u};
             if (t >= p.q0 && t < p.q1)
-                w[k] = t >= p.n0 ? *(const u32x4*)(in + (((size_t)b * p.n_new + (t - p.n0)) * p.H + h) * D + d8)
+                w[k] = t >= p.n0 ? *(const u32x4*)(in + (input_row(p, b, t - p.n0) * p.H + h) * D + d8)
                                  : *(const u32x4*)(ring + (((size_t)b * p.H + h) * p.ring + t % p.ring) * D + d8);
         }
     }
 
     // The eight values of step k as the coder sees them: widened to fp32; for
-    // tokens of this call rotated, and rounded to fp16 when a window exists.
-    __device__ __forceinline__ void widen(const AppendParams& p, int tb, int k, float* v) const
+    // tokens of this call (keys: turned to their positions) rotated, and rounded
+    // to fp16 when a window exists.
+    template <bool KEYS, typename P>
+    __device__ __forceinline__ void widen(const P& p, int b, int tb, int k, float* v) const
     {
         const int t = tb + row(k);
         const bool fresh = !(t >= p.q0 && t < p.q1) || t >= p.n0;  // bf16 (zero rows: zero words)
@@ -130,6 +209,10 @@ struct RowStage {
             }
         }
         const bool input = t >= p.q0 && t < p.q1 && t >= p.n0;
+        if constexpr (KEYS && kRope<P>) {
+            if (input)  // (all lanes of a row or none)
+                rope_row8<D>(p.rope, input_position(p, b, t - p.n0), chan(k) >> 3, v);
+        }
         if (p.rotate) {
             float r[8];
 #pragma unroll
@@ -161,8 +244,8 @@ __device__ __forceinline__ void copy_out(const uint8_t* src, uint8_t* dst, int b
 // per-channel keys is one whole group), written piece by piece: value pieces
 // keep the bits of tokens appended earlier.  vcode: 32 D bytes of LDS for the
 // value codes [token][D].
-template <int D>
-__device__ __forceinline__ void edge_block(const AppendParams& p, int unit, int tb, uint8_t* vcode)
+template <int D, typename Params>
+__device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, uint8_t* vcode)
 {
     const int b = unit / p.H, h = unit % p.H;
     const int lo = max(p.q0, tb), hi = min(p.q1, tb + kBlockTok);
@@ -180,7 +263,7 @@ __device__ __forceinline__ void edge_block(const AppendParams& p, int unit, int 
         for (int k = 0; k < RowStage<D>::kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8, t = tb + i;
             float x[8];
-            kst.widen(p, tb, k, x);
+            kst.template widen<true>(p, b, tb, k, x);
             float s, z;
             piece_group_stats(x, lanes, p.k_mode, kb, &s, &z);
             round_meta(p.meta16, &s, &z);
@@ -209,7 +292,7 @@ __device__ __forceinline__ void edge_block(const AppendParams& p, int unit, int 
     for (int k = 0; k < RowStage<D>::kSteps; ++k) {
         const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8, t = tb + i;
         float x[8];
-        vst.widen(p, tb, k, x);
+        vst.template widen<false>(p, b, tb, k, x);
         float s, z;
         piece_group_stats(x, vlanes, p.v_mode, vb, &s, &z);
         round_meta(p.meta16, &s, &z);
@@ -311,8 +394,8 @@ __device__ __forceinline__ float row_ror8(float v)
 // Vector work bounds it.  A KIVI chunk of 2048 tokens (B = 32, 8 heads of 128,
 // 348 MB) took 164 us with rows staged in LDS, one thread per channel for the
 // statistics, codes as bytes and 64-bit shifts; 115 now, window rows included.
-template <int D, bool PERCH, int KB, int VB>
-__global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
+template <int D, bool PERCH, int KB, int VB, typename Params>
+__global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
 {
     constexpr int PPT = D / 8, kOut = 4 * D * (KB > VB ? KB : VB);
     // a section's pieces, and the value codes by token (edge_block: all of it)
@@ -349,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
         for (int k = 0; k < kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8;
             float x[8], s, z;
-            kst.widen(p, tb, k, x);
+            kst.template widen<true>(p, b, tb, k, x);
             piece_group_stats(x, lanes, p.k_mode, KB, &s, &z);
             round_meta(p.meta16, &s, &z);
             if (P % lanes == 0) {
@@ -366,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
         float x[kSteps][8], mn[8], mx[8];
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
-            kst.widen(p, tb, k, x[k]);
+            kst.template widen<true>(p, b, tb, k, x[k]);
         const bool aff = p.k_mode == KVQ_AFFINE;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -438,7 +521,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
     for (int k = 0; k < kSteps; ++k) {
         const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8;
         float x[8], s, z;
-        vst.widen(p, tb, k, x);
+        vst.template widen<false>(p, b, tb, k, x);
         piece_group_stats(x, vlanes, p.v_mode, VB, &s, &z);
         round_meta(p.meta16, &s, &z);
         if (P % vlanes == 0) {
@@ -512,8 +595,45 @@ __device__ __forceinline__ float group_reduce(float v, int g, bool is_max, float
     return v;
 }
 
+// Channel d = threadIdx.x of a row of D threads (value x), normed by weights w
+// (null: not), rotated and rounded to bf16; the row passes through xs [D].
 template <int D>
-__global__ __launch_bounds__(D) void append_token_kernel(AppendParams p)
+__device__ __forceinline__ float rope_channel(const RopeArgs& r, int t, float x, const uint16_t* w, float* xs)
+{
+#pragma clang fp contract(off)
+    __shared__ double sums[D / 64];
+    const int d = threadIdx.x;
+    float2 cs = make_float2(1.0f, 0.0f);
+    const bool half = r.layout == KVQ_ROPE_HALF;
+    const int other = half ? (d < r.rot / 2 ? d + r.rot / 2 : d - r.rot / 2) : d ^ 1;
+    if (d < r.rot)
+        cs = rope_cos_sin(t, r.turns[half ? min(d, other) : d >> 1], r.scale);
+    if (w) {
+        double sum = row_sum<32>((double)x * (double)x);
+        sum += __shfl_xor(sum, 32);
+        if constexpr (D > 64) {
+            if ((d & 63) == 0)
+                sums[d >> 6] = sum;
+            __syncthreads();
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i)
+                sum += sums[i];
+        }
+        x = (x * norm_factor(sum, D, r.eps)) * bf16_to_f32(w[d]);
+    }
+    xs[d] = x;
+    __syncthreads();
+    if (d < r.rot) {
+        const float a = x * cs.x, b = xs[other] * cs.y;
+        x = d > other ? a + b : a - b;
+    }
+    __syncthreads();  // xs may be written again
+    return bf16_to_f32(f32_to_bf16(x));
+}
+
+template <int D, typename Params>
+__global__ __launch_bounds__(D) void append_token_kernel(Params p)
 {
     __shared__ float xs[2][D];
     __shared__ float red[8 * 4];
@@ -521,9 +641,11 @@ __global__ __launch_bounds__(D) void append_token_kernel(AppendParams p)
     const int t = p.n0, tau = t & 31, j = t & 7;
     const size_t blk = (size_t)unit * (p.T / kBlockTok) + (size_t)(t / kBlockTok);
     const size_t vpi = value_piece<D>(blk, tau >> 3, d);
-    const size_t in = ((size_t)b * p.H + h) * D + d;  // n_new == 1
+    const size_t in = (input_row(p, b, 0) * p.H + h) * D + d;  // n_new == 1
     float x[2] = {bf16_to_f32(p.kin[in]), bf16_to_f32(p.vin[in])};
     const uint64_t old = load_piece(p.vc, vpi, p.v_bits);
+    if constexpr (kRope<Params>)
+        x[0] = rope_channel<D>(p.rope, input_position(p, b, 0), x[0], p.rope.wk, xs[0]);
     if (p.rotate) {
         xs[0][d] = x[0];
         xs[1][d] = x[1];
@@ -599,16 +721,16 @@ __global__ __launch_bounds__(D) void append_token_kernel(AppendParams p)
 template <int D>
 constexpr int kRingRows = kThreads / (D / 8);
 
-template <int D>
-__global__ __launch_bounds__(kThreads) void append_ring_kernel(AppendParams p, int hi)
+template <int D, typename Params>
+__global__ __launch_bounds__(kThreads) void append_ring_kernel(Params p, int hi)
 {
     const int unit = blockIdx.y;
     const int b = unit / p.H, h = unit % p.H;
     const int c8 = 8 * ((int)threadIdx.x % (D / 8));
     const int t = p.ring_lo + kRingRows<D> * (int)blockIdx.x + (int)threadIdx.x / (D / 8);
-    const size_t at = (((size_t)b * p.n_new + (t - p.n0)) * p.H + h) * D + c8;
     u32x4 w[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
     if (t < hi) {
+        const size_t at = (input_row(p, b, t - p.n0) * p.H + h) * D + c8;
         w[0] = *(const u32x4*)(p.kin + at);
         w[1] = *(const u32x4*)(p.vin + at);
     }
@@ -619,6 +741,10 @@ __global__ __launch_bounds__(kThreads) void append_ring_kernel(AppendParams p, i
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             v[e] = __uint_as_float((e & 1) ? ww[e >> 1] & 0xFFFF0000u : ww[e >> 1] << 16);
+        if constexpr (kRope<Params>) {
+            if (q == 0 && t < hi)
+                rope_row8<D>(p.rope, input_position(p, b, t - p.n0), c8 >> 3, v);
+        }
         if (p.rotate)  // (every lane of a row takes part)
             rotate8<D>(v, c8 >> 3, p.rot_c);
         if (t < hi) {
@@ -631,61 +757,60 @@ __global__ __launch_bounds__(kThreads) void append_ring_kernel(AppendParams p, i
     }
 }
 
-template <int D, bool PERCH>
-void launch_blocks(const AppendParams& p, int blocks, int units, hipStream_t stream)
+template <int D, bool PERCH, typename P>
+void launch_blocks(const P& p, int blocks, int units, hipStream_t stream)
 {
     const dim3 g(blocks, units), t(kThreads);
     if (p.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
-        launch_kernel((append_block_kernel<D, PERCH, 8, 8>), g, t, 0, stream, p);
+        launch_kernel((append_block_kernel<D, PERCH, 8, 8, P>), g, t, 0, stream, p);
     else if (p.k_bits == 4 && p.v_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 4, 4>), g, t, 0, stream, p);
+        launch_kernel((append_block_kernel<D, PERCH, 4, 4, P>), g, t, 0, stream, p);
     else if (p.k_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 4, 2>), g, t, 0, stream, p);
+        launch_kernel((append_block_kernel<D, PERCH, 4, 2, P>), g, t, 0, stream, p);
     else if (p.v_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 2, 4>), g, t, 0, stream, p);
+        launch_kernel((append_block_kernel<D, PERCH, 2, 4, P>), g, t, 0, stream, p);
     else
-        launch_kernel((append_block_kernel<D, PERCH, 2, 2>), g, t, 0, stream, p);
+        launch_kernel((append_block_kernel<D, PERCH, 2, 2, P>), g, t, 0, stream, p);
 }
 
-template <int D>
-hipError_t launch_append_d(const AppendParams& p, hipStream_t stream)
+template <int D, typename P>
+hipError_t launch_append_d(const P& p, hipStream_t stream)
 {
     const int units = p.B * p.H;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
-        launch_kernel(append_token_kernel<D>, dim3(units), dim3(D), 0, stream, p);
+        launch_kernel((append_token_kernel<D, P>), dim3(units), dim3(D), 0, stream, p);
         return hipGetLastError();
     }
     if (p.q1 > p.q0) {
         const int blocks = (p.q1 + kBlockTok - 1) / kBlockTok - p.q0 / kBlockTok;
         if (p.k_axis == KVQ_PER_CHANNEL)
-            launch_blocks<D, true>(p, blocks, units, stream);
+            launch_blocks<D, true, P>(p, blocks, units, stream);
         else
-            launch_blocks<D, false>(p, blocks, units, stream);
+            launch_blocks<D, false, P>(p, blocks, units, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
     int n1 = p.n0 + p.n_new;
     if (p.ring && n1 > p.ring_lo) {
-        launch_kernel(append_ring_kernel<D>, dim3((n1 - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, units), dim3(kThreads), 0,
+        launch_kernel((append_ring_kernel<D, P>), dim3((n1 - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, units), dim3(kThreads), 0,
                       stream, p, n1);
         return hipGetLastError();
     }
     return hipSuccess;
 }
 
-template <int D>
-hipError_t launch_rows_d(const AppendParams& p, int hi, hipStream_t stream)
+template <int D, typename P>
+hipError_t launch_rows_d(const P& p, int hi, hipStream_t stream)
 {
     if (hi > p.ring_lo)
-        launch_kernel(append_ring_kernel<D>, dim3((hi - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, p.B * p.H), dim3(kThreads), 0,
+        launch_kernel((append_ring_kernel<D, P>), dim3((hi - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, p.B * p.H), dim3(kThreads), 0,
                       stream, p, hi);
     return hipGetLastError();
 }
 
-}  // namespace
-
-hipError_t launch_append_rows(const AppendParams& p, int D, int hi, hipStream_t stream)
+template <typename P>
+hipError_t launch_rows(const P& p, int D, int hi, hipStream_t stream)
 {
     switch (D) {
     case 64:
@@ -699,7 +824,8 @@ hipError_t launch_append_rows(const AppendParams& p, int D, int hi, hipStream_t 
     }
 }
 
-hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream)
+template <typename P>
+hipError_t launch(const P& p, int D, hipStream_t stream)
 {
     switch (D) {
     case 64:
@@ -711,6 +837,25 @@ hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream)
     default:
         return hipErrorInvalidValue;
     }
+}
+
+}  // namespace
+
+// Built for one kind of parameters per object.
+#ifdef KVQ_APPEND_ROPE
+typedef AppendRopeParams Params;
+#else
+typedef AppendParams Params;
+#endif
+
+hipError_t launch_append_rows(const Params& p, int D, int hi, hipStream_t stream)
+{
+    return launch_rows(p, D, hi, stream);
+}
+
+hipError_t launch_append(const Params& p, int D, hipStream_t stream)
+{
+    return launch(p, D, stream);
 }
 
 }  // namespace kvq

@@ -553,7 +553,13 @@ kvq_status kvq_merge_adapter(const void* W, int d_in, int d_q, int d_kv, const v
     return kvq::launch_merge(p, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
-kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, const kvq_format* fmt, void* stream)
+}  // extern "C"
+
+namespace {
+
+// The checks and the parameters of an append of n_new tokens, and its launches
+// (P: kvq::AppendParams or kvq::AppendRopeParams).
+kvq_status check_append(const kvq_cache* c, const void* K, const void* V, int n_new, const kvq_format* fmt)
 {
     if (!c || !fmt || n_new < 0)
         return KVQ_ERR_ARG;
@@ -563,10 +569,13 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, con
         return KVQ_OK;
     if (!K || !V || !aligned16(K) || !aligned16(V))
         return KVQ_ERR_ARG;
-    if ((long long)c->n + n_new > c->T_max)
-        return KVQ_ERR_CAPACITY;
+    return (long long)c->n + n_new > c->T_max ? KVQ_ERR_CAPACITY : KVQ_OK;
+}
+
+template <typename P>
+kvq_status run_append(kvq_cache* c, const void* K, const void* V, int n_new, P p, void* stream)
+{
     const kvq_format& f = c->fmt;
-    kvq::AppendParams p = {};
     p.kc = at<uint32_t>(c, 0);
     p.ks = at<float>(c, 1);
     p.kz = at<float>(c, 2);
@@ -594,7 +603,7 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, con
     const int n0 = c->n, n1 = n0 + n_new, S = f.sink;
     if (n0 < S) {
         // sink tokens [n0, min(S, n1)): fp16 rows t of sections 8 and 9
-        kvq::AppendParams ps = p;
+        P ps = p;
         ps.kr = at<uint16_t>(c, 8);
         ps.vr = at<uint16_t>(c, 9);
         ps.n0 = n0;
@@ -616,6 +625,172 @@ kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, con
     }
     c->n = n1;
     return KVQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvq_status kvq_append(kvq_cache* c, const void* K, const void* V, int n_new, const kvq_format* fmt, void* stream)
+{
+    const kvq_status st = check_append(c, K, V, n_new, fmt);
+    if (st != KVQ_OK || n_new == 0)
+        return st;
+    return run_append(c, K, V, n_new, kvq::AppendParams{}, stream);
+}
+
+// ------------------------------------------------------------ positions
+
+kvq_status kvq_rope_init(kvq_rope* rope, int rot, int layout, double base, int scaling, double factor,
+                         double original, double low, double high)
+{
+    if (!rope || rot < 0 || rot > 2 * KVQ_ROPE_PAIRS || rot % 16 != 0)
+        return KVQ_ERR_ARG;
+    if ((layout != KVQ_ROPE_HALF && layout != KVQ_ROPE_INTERLEAVED) || !(base > 1.0) || !std::isfinite(base))
+        return KVQ_ERR_ARG;
+    if (scaling < KVQ_ROPE_PLAIN || scaling > KVQ_ROPE_YARN)
+        return KVQ_ERR_ARG;
+    if (scaling != KVQ_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor)))
+        return KVQ_ERR_ARG;
+    const bool by_waves = scaling == KVQ_ROPE_BANDS || scaling == KVQ_ROPE_YARN;
+    if (by_waves && !(original > 0.0 && std::isfinite(original) && low > 0.0 && high > low && std::isfinite(high)))
+        return KVQ_ERR_ARG;
+    const double two_pi = 6.283185307179586477;
+    kvq_rope r = {};
+    r.rot = rot;
+    r.layout = layout;
+    r.scale = scaling == KVQ_ROPE_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    r.eps = 1e-6f;
+    if (scaling == KVQ_ROPE_BASE)
+        base *= pow(factor, rot / (rot - 2.0));
+    // YaRN: pair (a real number) that makes w waves in the original length
+    const auto pair_of = [&](double w) { return rot * log(original / (two_pi * w)) / (2.0 * log(base)); };
+    double first = 0.0, last = 0.0;
+    if (scaling == KVQ_ROPE_YARN) {
+        first = fmax(floor(pair_of(high)), 0.0);
+        last = fmin(ceil(pair_of(low)), rot - 1.0);
+        if (!(last > first))
+            last = first + 1e-3;
+    }
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot), keep = 1.0;  // the share of the unscaled frequency
+        if (scaling == KVQ_ROPE_LINEAR)
+            keep = 0.0;
+        else if (scaling == KVQ_ROPE_BANDS)
+            keep = fmin(fmax((original * f / two_pi - low) / (high - low), 0.0), 1.0);
+        else if (scaling == KVQ_ROPE_YARN)
+            keep = 1.0 - fmin(fmax((i - first) / (last - first), 0.0), 1.0);
+        if (keep < 1.0)
+            f = f * (keep + (1.0 - keep) / factor);
+        r.turns[i] = f / two_pi;
+    }
+    *rope = r;
+    return KVQ_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The table of a call for heads of size D; n tokens from pos0 where pos is null.
+kvq_status rope_args(const kvq_rope* rope, int D, const void* q_norm, const void* k_norm, const int32_t* pos, int pos0,
+                     long long n, kvq::RopeArgs* out)
+{
+    if (!rope || rope->rot < 0 || rope->rot > D || rope->rot % 16 != 0)
+        return KVQ_ERR_ARG;
+    if (rope->layout != KVQ_ROPE_HALF && rope->layout != KVQ_ROPE_INTERLEAVED)
+        return KVQ_ERR_ARG;
+    if (!std::isfinite(rope->scale) || !aligned16(q_norm) || !aligned16(k_norm) || (uintptr_t)pos % 4)
+        return KVQ_ERR_ARG;
+    if ((q_norm || k_norm) && !(rope->eps >= 0.0f && std::isfinite(rope->eps)))
+        return KVQ_ERR_ARG;
+    // (a position times turns stays exact to 2^-54 of a turn below 2^31 turns)
+    for (int i = 0; i < rope->rot / 2; ++i)
+        if (!(fabs(rope->turns[i]) <= 1.0))
+            return KVQ_ERR_ARG;
+    if (!pos && pos0 + n - 1 > INT32_MAX)
+        return KVQ_ERR_ARG;
+    out->wq = (const uint16_t*)q_norm;
+    out->wk = (const uint16_t*)k_norm;
+    out->pos = pos;
+    out->pos0 = pos0;
+    out->rot = rope->rot;
+    out->layout = rope->layout;
+    out->scale = rope->scale;
+    out->eps = rope->eps;
+    memcpy(out->turns, rope->turns, sizeof(out->turns));
+    return KVQ_OK;
+}
+
+// Whether the B n rows of H heads can be rotated from x to y.
+bool rope_rows_ok(const void* x, const void* y, int H)
+{
+    return H == 0 ? !x && !y : H > 0 && x && y && aligned16(x) && aligned16(y);
+}
+
+}  // namespace
+
+extern "C" {
+
+kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B, int n, int H_q, int H_kv, int D,
+                       const void* q_norm, const void* k_norm, const int32_t* pos, int pos0, void* Qo, void* Ko,
+                       void* stream)
+{
+    if (B < 1 || n < 0 || (D != 64 && D != 128 && D != 256))
+        return KVQ_ERR_ARG;
+    if (!rope_rows_ok(Q, Qo, H_q) || !rope_rows_ok(K, Ko, H_kv) || (!Q && !K))
+        return KVQ_ERR_ARG;
+    const long long tokens = (long long)B * n, heads = (long long)H_q + H_kv;
+    if (tokens > INT32_MAX || heads > INT32_MAX || tokens * heads >= kvq::kRopeRows)
+        return KVQ_ERR_ARG;
+    kvq::RopeQkParams p = {};
+    const kvq_status st = rope_args(rope, D, Q ? q_norm : nullptr, K ? k_norm : nullptr, pos, pos0, n, &p.rope);
+    if (st != KVQ_OK || n == 0)
+        return st;
+    p.q = (const uint16_t*)Q;
+    p.k = (const uint16_t*)K;
+    p.qo = (uint16_t*)Qo;
+    p.ko = (uint16_t*)Ko;
+    p.tokens = (int)tokens;
+    p.n = n;
+    p.H_q = H_q;
+    p.H = H_kv;
+    return kvq::launch_rope(p, D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+}
+
+kvq_status kvq_append_rope(kvq_cache* c, const kvq_rope* rope, const void* K, const void* V, int n_in,
+                           const int32_t* rows, int n_new, const void* Q, int H_q, const void* q_norm,
+                           const void* k_norm, const int32_t* pos, int pos0, void* Qo, const kvq_format* fmt,
+                           void* stream)
+{
+    const kvq_status st = check_append(c, K, V, n_new, fmt);
+    if (st != KVQ_OK)
+        return st;
+    // (checked for no tokens too: a wrong call is refused at any size)
+    if ((uintptr_t)rows % 4 || (rows ? n_in < 1 || Q : n_in < n_new) || !rope_rows_ok(Q, Qo, H_q))
+        return KVQ_ERR_ARG;
+    const long long tokens = (long long)c->B * n_new;
+    if (tokens * ((long long)H_q + c->H) >= kvq::kRopeRows || (long long)c->B * n_in > INT32_MAX)
+        return KVQ_ERR_ARG;
+    kvq::AppendRopeParams p = {};
+    const kvq_status rs = rope_args(rope, c->D, Q ? q_norm : nullptr, k_norm, pos, pos0, n_new, &p.rope);
+    if (rs != KVQ_OK || n_new == 0)
+        return rs;
+    p.rows = rows;
+    p.n_in = n_in;
+    if (Q) {
+        kvq::RopeQkParams q = {};
+        q.q = (const uint16_t*)Q;
+        q.qo = (uint16_t*)Qo;
+        q.tokens = (int)tokens;
+        q.n = n_new;
+        q.H_q = H_q;
+        q.rope = p.rope;
+        q.rope.wk = nullptr;
+        if (kvq::launch_rope(q, c->D, (hipStream_t)stream) != hipSuccess)
+            return KVQ_ERR_DEVICE;
+    }
+    return run_append(c, K, V, n_new, p, stream);
 }
 
 }  // extern "C"

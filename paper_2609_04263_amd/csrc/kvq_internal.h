@@ -74,6 +74,41 @@ hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 // p.ring, from input token t - p.n0 (the sink tokens: ring = sink).
 hipError_t launch_append_rows(const AppendParams& p, int D, int hi, hipStream_t stream);
 
+// ------------------------------------------------------------------ rope
+// Rotary positions and norms of a call (kvq_rope and its other arguments).
+struct RopeArgs {
+    const uint16_t* wq;   // bf16 [D] norm weights, null: no norm
+    const uint16_t* wk;
+    const int32_t* pos;   // [B][n], null: token i of every sequence is at pos0 + i
+    int pos0;
+    int rot, layout;
+    float scale, eps;
+    double turns[KVQ_ROPE_PAIRS];
+};
+struct RopeQkParams {
+    const uint16_t* q;    // bf16 [B][n][H_q][D], null with H_q = 0
+    const uint16_t* k;    // bf16 [B][n][H][D], null with H = 0
+    uint16_t* qo;         // may be q and k themselves
+    uint16_t* ko;
+    int tokens, n;        // B n
+    int H_q, H;
+    int parts;            // waves that share a token's heads (set at launch)
+    RopeArgs rope;
+};
+// Upper bound of tokens (H_q + H) for 32-bit indexing of waves.
+constexpr long long kRopeRows = 1ll << 31;
+hipError_t launch_rope(const RopeQkParams& p, int D, hipStream_t stream);
+// An append whose keys are normed and rotated on the way (kvq_append_rope);
+// p.n_new tokens of the n_in that kin and vin have of every sequence, chosen by
+// rows [B][n_new] or the first ones.
+struct AppendRopeParams : AppendParams {
+    const int32_t* rows;
+    int n_in;
+    RopeArgs rope;
+};
+hipError_t launch_append(const AppendRopeParams& p, int D, hipStream_t stream);
+hipError_t launch_append_rows(const AppendRopeParams& p, int D, int hi, hipStream_t stream);
+
 // ---------------------------------------------------------------- gather
 constexpr int kGatherBatch = 8;     // operations a thread loads before it stores
 constexpr int kGatherBatches = 32;  // batches of one launch (2 KiB of kernel arguments)

@@ -31,6 +31,11 @@ class KvqError(RuntimeError):
         self.status = status
 
 
+class _Rope(C.Structure):  # kvq_rope
+    _fields_ = [("rot", C.c_int32), ("layout", C.c_int32), ("scale", C.c_float), ("eps", C.c_float),
+                ("turns", C.c_double * 128)]
+
+
 class Format(C.Structure):
     _fields_ = [(name, C.c_int32) for name in FORMAT_FIELDS]
 
@@ -64,6 +69,10 @@ def _load() -> C.CDLL:
     L.kvq_merge_adapter.argtypes = [P, I, I, I, P, P, I, C.c_float, P, P]
     L.kvq_project_append.argtypes = [P, I, I, P, I, I, P, P, I, C.c_float, P, P, I, P, S, P]
     L.kvq_append.argtypes = [P, P, P, I, Fp, P]
+    Rp = C.POINTER(_Rope)
+    L.kvq_rope_init.argtypes = [Rp, I, I] + [C.c_double, I] + [C.c_double] * 4
+    L.kvq_rope_qk.argtypes = [Rp, P, P, I, I, I, I, I, P, P, P, I, P, P, P]
+    L.kvq_append_rope.argtypes = [P, Rp, P, P, I, P, I, P, I, P, P, P, I, P, Fp, P]
     L.kvq_cache_gather.argtypes = [P, P, C.POINTER(C.c_int32), I, P]
     L.kvq_decode_workspace_bytes.argtypes = [P, I, C.POINTER(S)]
     L.kvq_decode_attn.argtypes = [P, P, I, C.c_float, P, P, S, P]
@@ -78,6 +87,7 @@ def _load() -> C.CDLL:
     for name in ("kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section", "kvq_cache_reset",
                  "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_project_workspace_bytes",
                  "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
+                 "kvq_rope_init", "kvq_rope_qk", "kvq_append_rope",
                  "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
                  "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
                  "kvq_prefill_attn_shared", "kvq_time_launches"):
@@ -89,7 +99,7 @@ _lib = _load()
 EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section",
             "kvq_cache_reset", "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_cache_destroy",
             "kvq_project_workspace_bytes", "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
-            "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
+            "kvq_rope_init", "kvq_rope_qk", "kvq_append_rope", "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
             "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
             "kvq_prefill_attn_shared", "kvq_time_launches")
 
@@ -143,6 +153,54 @@ def _ints(values, count: int, what: str):
     if len(a) != count:
         raise ValueError(f"{what}: {count} integers expected, got {len(a)}")
     return a, C.cast(a.buffer_info()[0], C.POINTER(C.c_int32))
+
+
+# ------------------------------------------------------------- positions
+
+ROPE_SCALINGS = ("plain", "linear", "base", "bands", "yarn")
+
+
+def _positions(t, count: int, what: str) -> None:
+    """Refuses what is not `count` int32 numbers in one piece (the library sees an address alone)."""
+    if t is not None and (t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous()):
+        raise ValueError(f"{what}: {count} contiguous int32 numbers expected")
+
+
+class Rope:
+    """Rotary positions of `rot` channels of a head (kvq_rope): frequencies base^(-2 i / rot), scaled for contexts
+    `factor` times `original`, or `turns`, turns per position of each of the rot / 2 pairs; and the norms' eps."""
+
+    def __init__(self, rot: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "plain",
+                 factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0, scale=None,
+                 eps: float = 1e-6, turns=None):
+        self.c = _Rope()
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling: one of {', '.join(ROPE_SCALINGS)} expected")
+        _check(_lib.kvq_rope_init(C.byref(self.c), rot, int(bool(interleaved)), base, ROPE_SCALINGS.index(scaling),
+                                  factor, original, low, high), "rope_init")
+        if turns is not None:
+            if len(turns) != rot // 2:
+                raise ValueError(f"turns: {rot // 2} numbers expected, got {len(turns)}")
+            self.c.turns[:rot // 2] = [float(x) for x in turns]
+        if scale is not None:
+            self.c.scale = scale
+        self.c.eps = eps
+
+    def qk(self, Q, K, Qo=None, Ko=None, q_norm=None, k_norm=None, pos=None, pos0: int = 0, stream=None) -> None:
+        """Qo, Ko (Q and K themselves where not given) <- bf16 Q [B, n, H_q, D] and K [B, n, H_kv, D] (either may be
+        None), normed by bf16 weights [D] where given and rotated to positions pos (device int32 [B, n], or None for
+        pos0, pos0 + 1, ..)."""
+        x = K if Q is None else Q
+        B, n, _, D = x.shape
+        if Q is not None and K is not None and K.shape[:2] + K.shape[3:] != (B, n, D):
+            raise ValueError("Q and K are of different tokens or head sizes")
+        _positions(pos, B * n, "pos")
+        Qo, Ko = Q if Qo is None else Qo, K if Ko is None else Ko
+        st = _lib.kvq_rope_qk(C.byref(self.c), _ptr(Q), _ptr(K), B, n, 0 if Q is None else Q.shape[2],
+                              0 if K is None else K.shape[2], D, _ptr(q_norm), _ptr(k_norm), _ptr(pos), pos0,
+                              _ptr(Qo), _ptr(Ko), _stream(stream))
+        if st:
+            _check(st, "rope_qk")
 
 
 # ------------------------------------------------------------------ cache
@@ -208,6 +266,24 @@ class Cache:
         st = _lib.kvq_append(self.handle, K.data_ptr(), V.data_ptr(), n_new, f, _stream(stream))
         if st:
             _check(st, "append")
+
+    def append_rope(self, rope: "Rope", K, V, n_new: int | None = None, rows=None, Q=None, Qo=None, q_norm=None,
+                    k_norm=None, pos=None, pos0: int = 0, fmt=None, stream=None) -> None:
+        """append of keys that `rope` norms and rotates on the way.  bf16 K, V [B, n_in, H_kv, D]; with rows (device
+        int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default).  Q, Qo
+        [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32 [B, n_new], or
+        None for pos0, pos0 + 1, .."""
+        n_in = K.shape[1]
+        if n_new is None:
+            n_new = n_in if rows is None else rows.shape[1]
+        _positions(rows, self.B * n_new, "rows")
+        _positions(pos, self.B * n_new, "pos")
+        f = self._fmt_ref if fmt is None else C.byref(Format.of(fmt))
+        st = _lib.kvq_append_rope(self.handle, C.byref(rope.c), K.data_ptr(), V.data_ptr(), n_in, _ptr(rows), n_new,
+                                  _ptr(Q), 0 if Q is None else Q.shape[-2], _ptr(q_norm), _ptr(k_norm), _ptr(pos),
+                                  pos0, _ptr(Qo), f, _stream(stream))
+        if st:
+            _check(st, "append_rope")
 
     def gather(self, src: "Cache", rows, n: int | None = None, stream=None) -> None:
         """Sequence b becomes the first n tokens (all by default) of src's
