@@ -454,6 +454,20 @@ kvq_status kvq_prefill_attn_shared(const kvq_cache* prefix, const kvq_cache* suf
                                    const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
                                    size_t ws_bytes, void* stream);
 
+/* Attention of drafted trees: the newest C tokens of every suffix (appended before
+ * the call) are drafts of which a query sees some, its ancestors and itself as a
+ * rule, beside the whole prefix and all suffix tokens before the drafts.
+ *   tree  device uint32 [B][C][ceil(C / 32)], aligned to 4 bytes: query i of
+ *         sequence b sees draft j where bit j % 32 of word j / 32 of tree[b][i] is
+ *         set; any pattern (bits from C on are not read).  A query that sees no
+ *         token at all gets zeros.
+ * B C ceil(C / 32) below 2^31; everything else, the workspace too, as
+ * kvq_prefill_attn_shared, which this is where bits 0 .. i are set.  One cache
+ * alone: an empty prefix of one sequence, first = {0, B}. */
+kvq_status kvq_tree_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                int C, int H_q, float sm_scale, const uint32_t* tree, void* O, void* workspace,
+                                size_t ws_bytes, void* stream);
+
 /* Measurement hook for benchmarks (not part of the method).  While set
  * (both events non-null), every kernel the library launches from this host
  * thread records stop_event when it completes, and the first of them after

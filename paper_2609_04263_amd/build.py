@@ -37,7 +37,7 @@ _NO_NANS = ["-fno-honor-nans"]
 # (source, object name, extra flags).  The decode split kernels are built
 # from one source, once per (head size, metadata width, key axis) family, the
 # prefill kernels once per head size, the shared-prefix kernels once per (head
-# size, key group / 32, 0 for per-channel keys).
+# size, key group / 32, 0 for per-channel keys), and those of drafted trees too.
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
          ("append.hip", "append_rope", ["-ffp-contract=off", "-DKVQ_APPEND_ROPE"]), ("rope.hip", "rope", ["-ffp-contract=off"]),
          ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
@@ -48,6 +48,7 @@ UNITS += [("attn_part.hip", f"attn_{d}_{m}_{pc}",
           for d in (64, 128, 256) for m in (0, 1) for pc in (0, 1)]
 UNITS += [("shared_part.hip", f"shared_{d}_{g}", _VGPR_MFMA + _NO_NANS + [f"-DKVQ_PART_D={d}", f"-DKVQ_PART_KG={g}"])
           for d in (64, 128, 256) for g in (0, 1, 2, 4, 8) if 32 * g <= d]
+UNITS += [(u[0], u[1].replace("shared", "tree"), u[2] + ["-DKVQ_PART_TREE"]) for u in UNITS if u[0] == "shared_part.hip"]
 SOURCES = sorted({u[0] for u in UNITS})
 
 

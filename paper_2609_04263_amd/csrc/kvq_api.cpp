@@ -1200,12 +1200,13 @@ kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* 
 
 // A checked call's parameters and plan, without its tensors.
 static kvq::SharedParams shared_params(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
-                                       int H_q, float sm_scale, int kernels)
+                                       int H_q, float sm_scale, int kernels, const uint32_t* tree = nullptr)
 {
     const int P = prefix->B, B = suffix->B;
     kvq::SharedParams p = {};
     p.seg[0] = shared_segment(prefix, H_q, sm_scale);
     p.seg[1] = shared_segment(suffix, H_q, sm_scale);
+    p.tree = tree;
     p.rows = (size_t)B * C * H_q;
     p.C = C;
     p.H_q = H_q;
@@ -1222,7 +1223,7 @@ static kvq::SharedParams shared_params(const kvq_cache* prefix, const kvq_cache*
 // those tokens have to be in the suffix.
 static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
                               int C, int H_q, float sm_scale, void* O, void* workspace, size_t ws_bytes, bool self,
-                              void* stream, int kernels = 0)
+                              void* stream, int kernels = 0, const uint32_t* tree = nullptr)
 {
     const kvq_status st = shared_caches(prefix, suffix, C, H_q);
     if (st != KVQ_OK)
@@ -1240,7 +1241,7 @@ static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, 
     size_t off_ml;
     if (ws_bytes < shared_workspace_layout(suffix, C, H_q, &off_ml))
         return KVQ_ERR_WORKSPACE;
-    kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, sm_scale, kernels);
+    kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, sm_scale, kernels, tree);
     p.q = (const uint16_t*)Q;
     p.out = (float*)O;
     p.part_o = (float*)workspace;
@@ -1259,6 +1260,32 @@ kvq_status kvq_prefill_attn_shared(const kvq_cache* prefix, const kvq_cache* suf
                                    size_t ws_bytes, void* stream)
 {
     return shared_attn(prefix, suffix, first, Q, C, H_q, sm_scale, O, workspace, ws_bytes, true, stream);
+}
+
+// (bits are indexed in 32 bits)
+static kvq_status tree_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q, int C,
+                            int H_q, float sm_scale, const uint32_t* tree, void* O, void* workspace, size_t ws_bytes,
+                            void* stream, int kernels)
+{
+    if (!tree || (uintptr_t)tree % 4)
+        return KVQ_ERR_ARG;
+    if (suffix && C > 0 && (double)suffix->B * C * ((C + 31) / 32) > INT32_MAX)
+        return KVQ_ERR_ARG;
+    return shared_attn(prefix, suffix, first, Q, C, H_q, sm_scale, O, workspace, ws_bytes, true, stream, kernels, tree);
+}
+
+kvq_status kvq_tree_attn_shared(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                int C, int H_q, float sm_scale, const uint32_t* tree, void* O, void* workspace,
+                                size_t ws_bytes, void* stream)
+{
+    return tree_attn(prefix, suffix, first, Q, C, H_q, sm_scale, tree, O, workspace, ws_bytes, stream, 0);
+}
+
+kvq_status kvq_internal_tree_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
+                                  int C, int H_q, float sm_scale, const uint32_t* tree, void* O, void* workspace,
+                                  size_t ws_bytes, void* stream, int kernels)
+{
+    return tree_attn(prefix, suffix, first, Q, C, H_q, sm_scale, tree, O, workspace, ws_bytes, stream, kernels);
 }
 
 kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, const void* Q,
@@ -1348,7 +1375,15 @@ size_t kvq_internal_shared_partials(const kvq_cache* prefix, const kvq_cache* su
                                     int kernels)
 {
     const kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, 1.0f, kernels);
-    return (size_t)(p.S[0] + p.S[1]) * p.rows;
+    return (size_t)p.parts * p.rows;
+}
+
+size_t kvq_internal_tree_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C, int H_q,
+                                  int kernels)
+{
+    static const uint32_t any = 0;  // (a plan reads no bits)
+    const kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, 1.0f, kernels, &any);
+    return (size_t)p.parts * p.rows;
 }
 
 int kvq_internal_project_tile(int M, int N)

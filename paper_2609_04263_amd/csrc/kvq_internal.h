@@ -273,21 +273,26 @@ struct SharedParams {
     AttnParams seg[2];   // the prefix and the suffix cache: sections and format; n = tokens - sink (may be negative)
     const uint16_t* q;   // bf16 [B][C][H_q][D]
     float* out;          // fp32 [B][C][H_q][D]
-    float* part_o;       // fp32 [S0 + S1][rows][D]  unnormalized partial outputs
-    float* part_ml;      // fp32 [S0 + S1][rows][2]  (running max in log2 units, sum)
+    float* part_o;       // fp32 [parts][rows][D]  unnormalized partial outputs
+    float* part_ml;      // fp32 [parts][rows][2]  (running max in log2 units, sum)
+    const uint32_t* tree;  // [B][C][ceil(C / 32)]: which of the newest C tokens a query sees, null: causal
     size_t rows;         // B C H_q
     int C, H_q, P;
     int S[2], bps[2];    // ranges of a tile, 32-token blocks per range
+    int parts;           // partials of a row: S[0] + S[1], and one of the drafts
     int tiles0, items0;  // prefix tiles, prefix items (tiles0 S[0]); the suffix items come after them
+    int items1;          // suffix items, then (a tree's) draft items
     int image_items, direct0, direct_items;  // items of the image kernel, and those of the direct one from direct0
+    int draft_items;
+    int lim1, causal;    // tail tokens of the suffix that row 0 sees, and whether one of chunk token c sees c more
     int rotate;
     float rot_c;
     int first[kSharedPrefixes + 1];  // first sequence of each group
     int tile0[kSharedPrefixes + 1];  // first tile of each group
 };
-// Fills S, bps, tiles0, items0, tile0 and the kernels' items from the rest.
+// Fills S, bps, parts, limits, tiles0, tile0 and the items from the rest.
 void shared_plan(SharedParams* p, int D, int B, int kernels);
-// Upper bound of (S0 + S1) rows for any lengths and groups and up to C queries.
+// Upper bound of parts times rows for any lengths and groups and up to C queries.
 size_t shared_partials_bound(int B, int H, int D, int C, int G);
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream);
 
@@ -306,8 +311,13 @@ extern "C" int kvq_internal_gather_ops(const int32_t* rows, int B_dst, int B_src
 extern "C" kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
                                                const void* Q, int C, int H_q, float sm_scale, void* O, void* workspace,
                                                size_t ws_bytes, int self, void* stream, int kernels);
+extern "C" kvq_status kvq_internal_tree_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
+                                             const void* Q, int C, int H_q, float sm_scale, const uint32_t* tree, void* O,
+                                             void* workspace, size_t ws_bytes, void* stream, int kernels);
 // The partials that such a call writes (of arguments that it would not refuse).
 extern "C" size_t kvq_internal_shared_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
                                                int H_q, int kernels);
+extern "C" size_t kvq_internal_tree_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
+                                             int H_q, int kernels);
 extern "C" int kvq_internal_prefill_ranges(const kvq_cache* cache, int C, int H_q);
 extern "C" int kvq_internal_prefill_tile_rows(const kvq_cache* cache, int C, int H_q);

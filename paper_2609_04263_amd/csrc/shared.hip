@@ -5,7 +5,9 @@
 
 namespace kvq {
 
-#define KVQ_FAMILY(D, KG) hipError_t launch_shared_##D##_##KG(const SharedParams& p, hipStream_t stream);
+#define KVQ_FAMILY(D, KG)                                                    \
+    hipError_t launch_shared_##D##_##KG(const SharedParams& p, hipStream_t stream); \
+    hipError_t launch_tree_##D##_##KG(const SharedParams& p, hipStream_t stream);
 KVQ_FAMILY(64, 0) KVQ_FAMILY(64, 1) KVQ_FAMILY(64, 2)
 KVQ_FAMILY(128, 0) KVQ_FAMILY(128, 1) KVQ_FAMILY(128, 2) KVQ_FAMILY(128, 4)
 KVQ_FAMILY(256, 0) KVQ_FAMILY(256, 1) KVQ_FAMILY(256, 2) KVQ_FAMILY(256, 4) KVQ_FAMILY(256, 8)
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p, int 
     const int R = SLOTS / J, rl = slot % R, j = slot / R;
     const size_t row = (size_t)blockIdx.x * R + rl;
     const size_t at = row < p.rows ? row : p.rows - 1;
-    const int S = p.S[0] + p.S[1];
+    const int S = p.parts;
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     float M = -INFINITY, L = 0.0f;
     const auto raise = [&](float m) {  // M to at least m
@@ -150,7 +152,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SharedParams p, int 
             L += ml.y * w;
         }
     }
-    acc *= 1.0f / L;  // every row sees a token
+    acc *= L > 0.0f ? 1.0f / L : 0.0f;  // (a row of a tree may see no token)
     if (p.rotate) {
         const float a = acc[0] + acc[1], b = acc[0] - acc[1], c = acc[2] + acc[3], e = acc[2] - acc[3];
         acc = floatx4{a + c, b + e, a - c, b - e} * p.rot_c;
@@ -170,7 +172,7 @@ template <int D>
 void launch_join(const SharedParams& p, hipStream_t stream)
 {
     constexpr int SLOTS = kJoinThreads / (D / 4);
-    const int S = p.S[0] + p.S[1];
+    const int S = p.parts;
     int J = 1;
     while (2 * J <= SLOTS && 4 * J <= S)
         J *= 2;
@@ -192,8 +194,15 @@ void launch_join(const SharedParams& p, hipStream_t stream)
 void shared_plan(SharedParams* p, int D, int B, int kernels)
 {
     const AttnParams &a = p->seg[0], &b = p->seg[1];
-    const auto blocks = [](const AttnParams& s) { return ceil_div(s.n_sink, 32) + ceil_div(s.n > 0 ? s.n : 0, 32); };
-    const int nb[2] = {blocks(a), blocks(b)}, own = p->C * a.G;
+    // blocks of the first n tail tokens (negative: of the sink alone)
+    const auto blocks = [](const AttnParams& s, int n) {
+        const int sink = s.n_sink < n + s.sink ? s.n_sink : n + s.sink;
+        return ceil_div(sink, 32) + ceil_div(n > 0 ? n : 0, 32);
+    };
+    const bool tree = p->tree != nullptr;
+    p->causal = !tree;
+    p->lim1 = b.n - p->C + !tree;
+    const int nb[2] = {blocks(a, a.n), blocks(b, tree ? p->lim1 : b.n)}, own = p->C * a.G;
     int most = 0;
     long long work = (long long)B * a.H * ceil_div(own, kTile) * nb[1];
     for (int g = 0; g < p->P; ++g) {
@@ -221,10 +230,12 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
         p->S[k] = ceil_div(nb[k], p->bps[k]);
     }
     p->items0 = tiles[0] * p->S[0];
-    const int items1 = tiles[1] * p->S[1];
-    p->image_items = (kind[0].direct ? 0 : p->items0) + (kind[1].direct ? 0 : items1);
+    p->items1 = tiles[1] * p->S[1];
+    p->image_items = (kind[0].direct ? 0 : p->items0) + (kind[1].direct ? 0 : p->items1);
     p->direct0 = p->image_items;
-    p->direct_items = p->items0 + items1 - p->image_items;
+    p->direct_items = p->items0 + p->items1 - p->image_items;
+    p->draft_items = tree ? B * a.H * ceil_div(own, few.per) : 0;
+    p->parts = p->S[0] + p->S[1] + tree;
 }
 
 size_t shared_partials_bound(int B, int H, int D, int C, int G)
@@ -241,17 +252,25 @@ size_t shared_partials_bound(int B, int H, int D, int C, int G)
         }
         return most;
     };
-    return segment(H, B * C * G) + segment((size_t)B * H, C * G);
+    // (and one of a tree's drafts)
+    return segment(H, B * C * G) + segment((size_t)B * H, C * G) + (size_t)B * H * C * G;
 }
 
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
+    SharedParams images = p;  // what the kernels without trees do
+    if (p.tree)
+        images.direct_items = 0;
     hipError_t e = hipErrorInvalidValue;
     switch (1000 * D + key_groups(a)) {
-#define KVQ_FAMILY(D, KG)                           \
-    case 1000 * D + KG:                             \
-        e = launch_shared_##D##_##KG(p, stream);        \
+#define KVQ_FAMILY(D, KG)                                    \
+    case 1000 * D + KG:                                      \
+        e = hipSuccess;                                      \
+        if (images.image_items + images.direct_items > 0)    \
+            e = launch_shared_##D##_##KG(images, stream);    \
+        if (e == hipSuccess && p.tree)                       \
+            e = launch_tree_##D##_##KG(p, stream);           \
         break;
         KVQ_FAMILY(64, 0)
         KVQ_FAMILY(64, 1)

@@ -26,6 +26,14 @@
 //                  samples): 16 or 32 rows, four waves, each with blocks of its
 //                  own, whose codes become operands in registers.
 //
+// Drafted trees (kvq_tree_attn_shared).  The newest C tokens of a suffix are seen by
+// the bits of a row, those before by all rows, so they are parts of their own: the
+// suffix' items end before the drafts, and further items, one per tile of rows,
+// take the blocks with drafts and mask them by 32 bits of the row.  Those are
+// items of the direct kernel built with TREE.  (Masked in both kernels, a tree's
+// blocks being the last of the suffix' items, the image kernel spilled 20 to 60
+// registers more in every call.)
+//
 // Operands are in the order in which the cache stores its codes, that of
 // v_mfma_f32_16x16x32_f16 (a 1 KiB fragment is one 16-byte piece per lane).
 // Codes are centred (c - (2^b - 1) / 2, or c - 2^(b-1) when symmetric), exact in
@@ -814,7 +822,8 @@ __device__ __forceinline__ constexpr float to_one()
 // group size / 32 (0: per-channel scales).  ROT: rotated queries, hi + lo.
 // DIRECT: direct_kernel's, which takes value offsets apart.  (The scores l of a block
 // include the tokens' starts; nl: where a block's starts and weights are.)
-template <int D, int KG, bool ROT, int CT, bool DIRECT>
+// TREE: lim0 on are drafts, lim[c] is where the column's bits start in the tree.
+template <int D, int KG, bool ROT, int CT, bool DIRECT, bool TREE = false>
 struct Rows {
     static constexpr int NKB = D / 32, NMB = D / 16;
     static constexpr bool KH = KG == 0;
@@ -832,6 +841,18 @@ struct Rows {
     bool apart;              // a token is so large that the sums are taken apart (uniform)
     int lim[CT];             // tail tokens that this lane's column sees (may be negative: only sink tokens)
     int lim0, lim1;          // the least and the most of the wave's rows (uniform)
+    const uint32_t* tree;    // TREE, drafts: the bits, [rows][words]; null: all columns see lim0 tokens (uniform)
+    int words;
+
+    // Which of 32 tokens from draft j on (j > -32) column c sees; none before draft 0.
+    // (The bits behind the last word's are of tokens that do not live: any will do.)
+    __device__ __forceinline__ uint32_t tree_bits(int c, int j) const
+    {
+        const uint32_t* row = tree + lim[c];
+        const int w = j >> 5;
+        const uint32_t lo = w < 0 ? 0u : row[min(w, words - 1)], hi = row[min(w + 1, words - 1)];
+        return __builtin_amdgcn_alignbit(hi, lo, j & 31);
+    }
 
     // Query rows of tile c, this lane's at src (channels 32 kb + 8 qg .. + 7 of it),
     // each times a power of two of its own that brings its largest element to 2^7 ..
@@ -963,10 +984,18 @@ struct Rows {
     __device__ __forceinline__ void settle(float (*l)[8], const float* nl, int t0, int off, int live, int lane, float* shift)
     {
         const int qg = lane >> 4;
-        if (live < 32 || t0 + 32 > lim0 + off) {
+        if (TREE && tree) {
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
-                const int valid = min(live, lim[c] + off - t0);
+                const uint32_t see = tree_bits(c, t0 - lim0 - off) >> (8 * qg);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    l[c][k] = see >> k & 1 && 8 * qg + k < live ? l[c][k] : kNegInf;
+            }
+        } else if (live < 32 || t0 + 32 > lim0 + off) {
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const int valid = min(live, (TREE ? lim0 : lim[c]) + off - t0);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     l[c][k] = 8 * qg + k < valid ? l[c][k] : kNegInf;
@@ -1421,12 +1450,15 @@ struct Item {
     int r0, rows;        // first row of the item, rows of the unit
     int split, part;     // range of blocks, and its place among a row's partials
     int lim, causal;     // limit of row 0, and whether a row of chunk token c sees c more
+    bool drafts;         // the tokens from lim on, by the rows' bits
 };
 
 // Item x of a kernel that takes `per` rows per item.
+template <bool TREE = false>
 __device__ __forceinline__ Item find_item(const SharedParams& p, int x, int per)
 {
     Item it;
+    it.drafts = false;
     if (x < p.items0) {
         // prefix: ranges of a tile apart, tiles of a unit next to each other
         const AttnParams& a = p.seg[0];
@@ -1456,15 +1488,23 @@ __device__ __forceinline__ Item find_item(const SharedParams& p, int x, int per)
         it.seg = 1;
         it.rows = p.C * a.G;
         const int n = (it.rows + per - 1) / per;
-        const int t = x / p.S[1];
-        it.split = x - t * p.S[1];
-        it.part = p.S[0] + it.split;
+        int t;
+        if (TREE && x >= p.items1) {
+            t = x - p.items1;
+            it.drafts = true;
+            it.split = 0;
+            it.part = p.S[0] + p.S[1];
+        } else {
+            t = x / p.S[1];
+            it.split = x - t * p.S[1];
+            it.part = p.S[0] + it.split;
+        }
         it.unit = t / n;
         it.r0 = (t - it.unit * n) * per;
         it.seq0 = it.unit / a.H;
         it.j = it.unit - it.seq0 * a.H;
-        it.lim = a.n - p.C + 1;
-        it.causal = 1;
+        it.lim = p.lim1;
+        it.causal = p.causal;
     }
     return it;
 }
@@ -1483,10 +1523,15 @@ struct Blocks {
     int nsb;     // sink blocks come first; block v is tail block v - nsb after them
     int ncb;     // coded blocks of the tail
 
-    __device__ __forceinline__ Blocks(const SharedParams& sp, const AttnParams& p, const Item& it, int left)
+    __device__ __forceinline__ Blocks(const SharedParams& sp, const AttnParams& p, const Item& it, int left, bool drafts = false)
     {
         nsb = (p.n_sink + 31) >> 5;
         ncb = (p.nq + 31) >> 5;
+        if (drafts) {  // from the block of token lim (of the sink's lim + sink) to the last
+            v0 = it.lim < 0 ? (it.lim + p.sink) >> 5 : nsb + (it.lim >> 5);
+            v1 = nsb + (p.n > 0 ? (p.n + 31) >> 5 : 0);
+            return;
+        }
         const int top = it.lim + (it.causal ? (it.r0 + left - 1) / p.G : 0);  // the most that a row sees
         const int nv = min(nsb, (top + p.sink + 31) >> 5) + (top > 0 ? (top + 31) >> 5 : 0);
         v0 = min(nv, it.split * sp.bps[it.seg]);
@@ -1717,7 +1762,7 @@ __host__ __device__ constexpr int direct_waves(int D)
     return D == 64 ? 3 : 2;
 }
 
-template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS>
+template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool ROWS, bool TREE>
 __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel(SharedParams sp)
 {
     constexpr int NMB = D / 16, NKB = D / 32, W = kDirectWaves, CT = direct_tiles(D, KG, KB, ROT, ROWS), PER = 16 * CT;
@@ -1727,10 +1772,10 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, hh = lane & 15, qg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const Item it = find_item(sp, blockIdx.x + sp.direct0, PER);
+    const Item it = find_item<TREE>(sp, blockIdx.x + sp.direct0, PER);
     const AttnParams& p = sp.seg[it.seg];
     const int G = p.G, left = min(it.rows - it.r0, PER);
-    const Blocks bl(sp, p, it, left);
+    const Blocks bl(sp, p, it, left, TREE && it.drafts);
 
     typedef Builder<D, KG == 0, KB, VB, M16, 1> Build;
     const Build B(p, it.unit, 0, lane);
@@ -1746,12 +1791,16 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     typename Build::Loads raw;
     if constexpr (kAhead || !ROWS)
         raw = prefetch(vc);
-    Rows<D, KG, ROT, CT, true> T;
+    Rows<D, KG, ROT, CT, true, TREE> T;
     T.lim0 = it.lim + (it.causal ? it.r0 / G : 0);
+    if constexpr (TREE) {
+        T.tree = it.drafts ? sp.tree : nullptr;
+        T.words = (sp.C + 31) >> 5;
+    }
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
         const int rc = min(16 * c + hh, left - 1);
-        T.lim[c] = it.lim + (it.causal ? (it.r0 + rc) / G : 0);
+        T.lim[c] = TREE ? (it.seq0 * sp.C + (it.r0 + rc) / G) * T.words : it.lim + (it.causal ? (it.r0 + rc) / G : 0);
         T.load_query(c, sp.q + global_row(sp, it, G, it.r0 + rc) * D, p.rot_c, lane);
     }
     T.init();
@@ -1912,42 +1961,52 @@ __global__ __launch_bounds__(kDirectThreads, direct_waves(D)) void direct_kernel
     }
 }
 
-// Items [0, image_items) by the image kernel, then direct_items by the direct one.
-template <int D, int KG, int KB, int VB, bool M16, bool ROT>
+// Items [0, image_items) by the image kernel, then direct_items by the direct one;
+// TREE: direct_items and draft_items by the direct one of trees.
+template <int D, int KG, int KB, int VB, bool M16, bool ROT, bool TREE>
 hipError_t launch_instance(const SharedParams& p, hipStream_t stream)
 {
     const bool rows = p.seg[0].ring > 0 || p.seg[0].sink > 0;
     constexpr bool kWindow = KG == 0;  // (per-channel keys come with a window)
+    if constexpr (TREE) {
+        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true, true>
+                           : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow, true>,
+                      dim3(p.direct_items + p.draft_items), dim3(kDirectThreads), (size_t)direct_lds(D, rows), stream, p);
+        return hipGetLastError();
+    } else {
     if (p.image_items > 0)
         launch_kernel(rows ? image_kernel<D, KG, KB, VB, M16, ROT, true> : image_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
                       dim3(p.image_items), dim3(64 * waves(D)), (size_t)image_lds(D, KG == 0), stream, p);
     if (p.direct_items > 0)
-        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true>
-                           : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow>,
+        launch_kernel(rows ? direct_kernel<D, KG, KB, VB, M16, ROT, true, false>
+                           : direct_kernel<D, KG, KB, VB, M16, ROT, kWindow, false>,
                       dim3(p.direct_items), dim3(kDirectThreads), (size_t)direct_lds(D, rows), stream, p);
     return hipGetLastError();
+    }
 }
 
-template <int D, int KG, bool M16, bool ROT>
+template <int D, int KG, bool M16, bool ROT, bool TREE>
 hipError_t launch_widths(const SharedParams& p, hipStream_t stream)
 {
     const AttnParams& a = p.seg[0];
     if (a.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
-        return launch_instance<D, KG, 8, 8, M16, ROT>(p, stream);
+        return launch_instance<D, KG, 8, 8, M16, ROT, TREE>(p, stream);
     if (a.k_bits == 4)
-        return a.v_bits == 4 ? launch_instance<D, KG, 4, 4, M16, ROT>(p, stream)
-                             : launch_instance<D, KG, 4, 2, M16, ROT>(p, stream);
-    return a.v_bits == 4 ? launch_instance<D, KG, 2, 4, M16, ROT>(p, stream)
-                         : launch_instance<D, KG, 2, 2, M16, ROT>(p, stream);
+        return a.v_bits == 4 ? launch_instance<D, KG, 4, 4, M16, ROT, TREE>(p, stream)
+                             : launch_instance<D, KG, 4, 2, M16, ROT, TREE>(p, stream);
+    return a.v_bits == 4 ? launch_instance<D, KG, 2, 4, M16, ROT, TREE>(p, stream)
+                         : launch_instance<D, KG, 2, 2, M16, ROT, TREE>(p, stream);
 }
 
 // The kernels of one head size and key grouping.
-template <int D, int KG>
+template <int D, int KG, bool TREE>
 hipError_t launch_family(const SharedParams& p, hipStream_t stream)
 {
     if (p.rotate)
-        return p.seg[0].meta16 ? launch_widths<D, KG, true, true>(p, stream) : launch_widths<D, KG, false, true>(p, stream);
-    return p.seg[0].meta16 ? launch_widths<D, KG, true, false>(p, stream) : launch_widths<D, KG, false, false>(p, stream);
+        return p.seg[0].meta16 ? launch_widths<D, KG, true, true, TREE>(p, stream)
+                               : launch_widths<D, KG, false, true, TREE>(p, stream);
+    return p.seg[0].meta16 ? launch_widths<D, KG, true, false, TREE>(p, stream)
+                           : launch_widths<D, KG, false, false, TREE>(p, stream);
 }
 
 }  // namespace shr

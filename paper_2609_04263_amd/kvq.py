@@ -83,6 +83,7 @@ def _load() -> C.CDLL:
     L.kvq_shared_workspace_bytes.argtypes = [P, P, I, I, C.POINTER(S)]
     L.kvq_decode_attn_shared.argtypes = [P, P, Ip, P, I, C.c_float, P, P, S, P]
     L.kvq_prefill_attn_shared.argtypes = [P, P, Ip, P, I, I, C.c_float, P, P, S, P]
+    L.kvq_tree_attn_shared.argtypes = [P, P, Ip, P, I, I, C.c_float, P, P, P, S, P]
     L.kvq_time_launches.argtypes = [P, P]
     for name in ("kvq_cache_bytes", "kvq_cache_init", "kvq_cache_section", "kvq_cache_reset",
                  "kvq_cache_len", "kvq_cache_rewind", "kvq_cache_restore", "kvq_project_workspace_bytes",
@@ -90,7 +91,7 @@ def _load() -> C.CDLL:
                  "kvq_rope_init", "kvq_rope_qk", "kvq_append_rope",
                  "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
                  "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
-                 "kvq_prefill_attn_shared", "kvq_time_launches"):
+                 "kvq_prefill_attn_shared", "kvq_tree_attn_shared", "kvq_time_launches"):
         getattr(L, name).restype = I
     return L
 
@@ -101,7 +102,7 @@ EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_sect
             "kvq_project_workspace_bytes", "kvq_project_qkv", "kvq_project_append", "kvq_merge_adapter", "kvq_append",
             "kvq_rope_init", "kvq_rope_qk", "kvq_append_rope", "kvq_cache_gather", "kvq_decode_workspace_bytes", "kvq_decode_attn", "kvq_decode_attn_noalloc",
             "kvq_prefill_attn", "kvq_prefill_workspace_bytes", "kvq_shared_workspace_bytes", "kvq_decode_attn_shared",
-            "kvq_prefill_attn_shared", "kvq_time_launches")
+            "kvq_prefill_attn_shared", "kvq_tree_attn_shared", "kvq_time_launches")
 
 
 def lib() -> C.CDLL:
@@ -373,6 +374,40 @@ class Cache:
                                           O.data_ptr(), workspace.data_ptr(), nbytes, _stream(stream))
         if st:
             _check(st, "prefill_attn_shared")
+
+    def tree_attn_shared(self, prefix: "Cache", Q, C_len: int, H_q: int, sm_scale: float, tree, O, workspace,
+                         first=None, stream=None) -> None:
+        """O[B, C, H_q, D] (fp32) <- attention of the newest C_len tokens' bf16 queries over each sequence's prefix,
+        the tokens here before those, and those of them whose bits are set in tree (device int32
+        [B, C, ceil(C / 32)], see tree_words)."""
+        keep, ptr = (None, None) if first is None else _ints(first, prefix.B + 1, "first")
+        _positions(tree, self.B * C_len * (-(-C_len // 32)), "tree")
+        nbytes = workspace.numel() * workspace.element_size()
+        st = _lib.kvq_tree_attn_shared(prefix.handle, self.handle, ptr, Q.data_ptr(), C_len, H_q, sm_scale,
+                                       tree.data_ptr(), O.data_ptr(), workspace.data_ptr(), nbytes, _stream(stream))
+        if st:
+            _check(st, "tree_attn_shared")
+
+
+def tree_words(parents):
+    """The bits of drafted trees for tree_attn_shared, int32 [B, C, ceil(C / 32)] on the parents' device: parents
+    [B, C] holds the index of every draft's parent among the drafts before it, -1 for one that follows the context
+    itself, or anything below for a row that is no draft and sees none."""
+    p = torch.as_tensor(parents)
+    host = p.cpu().tolist()
+    C_len = p.shape[1]
+    words = -(-C_len // 32)
+    flat = array("I")
+    for row in host:
+        seen = []
+        for i, parent in enumerate(row):
+            if parent >= i:
+                raise ValueError(f"draft {i} comes before its parent {parent}")
+            seen.append(0 if parent < -1 else (seen[parent] if parent >= 0 else 0) | 1 << i)
+        for bits in seen:
+            flat.extend(bits >> 32 * w & 0xFFFFFFFF for w in range(words))
+    out = torch.from_numpy(np.frombuffer(flat, np.int32).copy()) if flat else torch.zeros(0, dtype=torch.int32)
+    return out.view(len(host), C_len, words).to(p.device)
 
 
 # ------------------------------------------------------------- projection
