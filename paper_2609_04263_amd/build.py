@@ -39,7 +39,7 @@ _NO_NANS = ["-fno-honor-nans"]
 # prefill kernels once per head size, the shared-prefix kernels once per (head
 # size, key group / 32, 0 for per-channel keys), and those of drafted trees too.
 UNITS = [("kvq_api.cpp", "kvq_api", []), ("append.hip", "append", ["-ffp-contract=off"]),
-         ("append.hip", "append_rope", ["-ffp-contract=off", "-DKVQ_APPEND_ROPE"]), ("rope.hip", "rope", ["-ffp-contract=off"]),
+         ("append.hip", "append_rope", ["-ffp-contract=off", "-DKVQ_APPEND_ROPE"] + _NO_NANS), ("rope.hip", "rope", ["-ffp-contract=off"]),
          ("attn.hip", "attn", _VGPR_MFMA), ("project.hip", "project", []), ("merge.hip", "merge", []),
          ("gather.hip", "gather", []), ("shared.hip", "shared", [])]
 UNITS += [("prefill.hip", f"prefill_{d}", [f"-DKVQ_PREFILL_D={d}"]) for d in (64, 128, 256)]

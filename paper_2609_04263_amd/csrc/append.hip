@@ -34,8 +34,8 @@
 namespace kvq {
 namespace {
 
-// The kernels are built for two kinds of parameters P: AppendParams, and
-// AppendRopeParams, whose keys are normed and rotated (rope.h) and rounded to
+// The file is built for two kinds of parameters P: AppendParams, and (with
+// KVQ_APPEND_ROPE) AppendRopeParams, whose keys are normed and rotated (rope.h) and rounded to
 // bf16 as they are loaded, so that the coder sees what kvq_rope_qk would have
 // written, and whose rows may be chosen by an index.
 template <typename P>
@@ -59,53 +59,108 @@ __device__ __forceinline__ int input_position(const AppendRopeParams& p, int b, 
     return p.rope.pos ? p.rope.pos[(size_t)b * p.n_new + i] : p.rope.pos0 + i;
 }
 
-// A key row held by D / 8 consecutive lanes, eight channels each (piece P of the
-// row): normed, rotated and rounded to bf16.  Every lane computes the angles of
-// four pairs; in the half layout a piece and its partner rot / 16 pieces on need
-// the same eight, and each other's channels (16 exchanges).
-template <int D>
-__device__ __forceinline__ void rope_row8(const RopeArgs& r, int t, int P, float* v)
-{
-#pragma clang fp contract(off)
-    if (r.wk) {
-        const float f = norm_factor(row_sum<D / 8>(squares8(v)), D, r.eps);
-        float g[8];
-        widen8(*(const u32x4*)(r.wk + 8 * P), g);
-        norm8(v, f, g);
+// The angles of K rows held by D / 8 consecutive lanes, eight channels each (piece P
+// of the row).  In the half layout a piece and its partner rot / 16 pieces on need
+// the same eight: each computes four, and they exchange them.  s has the sign of
+// the partner's part: y = c x + s x_partner.
+struct Angles {
+    float c[8], s[8];
+
+    __device__ __forceinline__ Angles() {}
+    __device__ __forceinline__ Angles(const RopeArgs& r, int t, int P)
+    {
+        if (r.layout == KVQ_ROPE_HALF) {
+            const int hp = r.rot / 16;
+            const bool in = P < 2 * hp, up = in && P >= hp;
+            const int base = up ? 8 * (P - hp) + 4 : 8 * P, other = partner(r, P);
+            float2 mine[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                mine[j] = in ? rope_cos_sin(t, r.turns[base + j], r.scale) : make_float2(1.0f, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float oc = __shfl(mine[j].x, other), os = __shfl(mine[j].y, other);
+                c[j] = up ? oc : mine[j].x, s[j] = up ? os : -mine[j].y;
+                c[j + 4] = up ? mine[j].x : oc, s[j + 4] = up ? mine[j].y : -os;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 cs = 8 * P < r.rot ? rope_cos_sin(t, r.turns[4 * P + j], r.scale) : make_float2(1.0f, 0.0f);
+                c[j] = cs.x, s[j] = cs.y;
+            }
+        }
     }
-    if (r.layout == KVQ_ROPE_HALF) {
+
+    // The lane of a piece's partner in the half layout, its own where it has none.
+    static __device__ __forceinline__ int partner(const RopeArgs& r, int P)
+    {
         const int hp = r.rot / 16, lane = threadIdx.x & 63;
-        const bool in = P < 2 * hp, up = in && P >= hp;
-        const int base = up ? 8 * (P - hp) + 4 : 8 * P, other = in ? (up ? lane - hp : lane + hp) : lane;
-        float2 mine[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            mine[j] = in ? rope_cos_sin(t, r.turns[base + j], r.scale) : make_float2(1.0f, 0.0f);
-        float c[8], s[8], y[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float oc = __shfl(mine[j].x, other), os = __shfl(mine[j].y, other);
-            c[j] = up ? oc : mine[j].x, s[j] = up ? os : mine[j].y;
-            c[j + 4] = up ? mine[j].x : oc, s[j + 4] = up ? mine[j].y : os;
+        return P < hp ? lane + hp : P < 2 * hp ? lane - hp : lane;
+    }
+
+    // The row normed (by weights `norm`), turned and rounded to bf16.
+    template <int D>
+    __device__ __forceinline__ void turn(const RopeArgs& r, const u32x4& norm, int P, float* v) const
+    {
+#pragma clang fp contract(off)
+        if (r.wk) {
+            const float f = norm_factor(row_sum<D / 8>(squares8(v)), D, r.eps);
+            float g[8];
+            widen8(norm, g);
+            norm8(v, f, g);
         }
+        if (r.layout == KVQ_ROPE_HALF) {
+            float y[8];
+            exchange<D>(r, P, v, y);
+            if (8 * P < r.rot) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            y[e] = __shfl(v[e], other);
+                for (int e = 0; e < 8; ++e)
+                    v[e] = v[e] * c[e] + y[e] * s[e];
+            }
+        } else if (8 * P < r.rot) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float a = v[e] * c[e], b = y[e] * s[e];
-            v[e] = in ? (up ? a + b : a - b) : v[e];
+            for (int j = 0; j < 4; ++j)
+                turn_pair(v[2 * j], v[2 * j + 1], c[j], s[j]);
         }
-    } else if (8 * P < r.rot) {
+        const u32x4 w = narrow8(v);
+        widen8(w, v);
+    }
+
+    template <int D>
+    __device__ __forceinline__ void turn(const RopeArgs& r, int P, float* v) const
+    {
+        turn<D>(r, r.wk ? *(const u32x4*)(r.wk + 8 * P) : u32x4{0u, 0u, 0u, 0u}, P, v);
+    }
+
+    // The partner's channels: half a row away when all of the head is rotated (a
+    // vector operation each; LDS exchanges otherwise).
+    template <int D>
+    static __device__ __forceinline__ void exchange(const RopeArgs& r, int P, const float* v, float* y)
+    {
+        if (r.rot == D) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 cs = rope_cos_sin(t, r.turns[4 * P + j], r.scale);
-            turn_pair(v[2 * j], v[2 * j + 1], cs.x, cs.y);
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t x = __float_as_uint(v[e]);
+                if constexpr (D == 64) {  // lane ^ 4: lane ^ 7, then ^ 3
+                    const uint32_t m = __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true);
+                    y[e] = __uint_as_float(__builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true));
+                } else if constexpr (D == 128) {  // lane ^ 8
+                    y[e] = __uint_as_float(__builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, true));
+                } else {  // lane ^ 16
+                    const auto rows = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+                    y[e] = __uint_as_float(P & 16 ? rows[0] : rows[1]);
+                }
+            }
+        } else {
+            const int other = partner(r, P);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                y[e] = __shfl(v[e], other);
         }
     }
-    const u32x4 w = narrow8(v);
-    widen8(w, v);
-}
+};
+struct NoAngles {};
 
 constexpr int kThreads = 256;
 constexpr int kBlockTok = 32;
@@ -172,6 +227,19 @@ struct RowStage {
     __device__ static int row(int k) { return ((int)threadIdx.x + kThreads * k) / (D / 8); }
     __device__ static int chan(int k) { return 8 * (((int)threadIdx.x + kThreads * k) % (D / 8)); }
 
+    // The angles of step k's row.
+    template <typename P>
+    __device__ static __forceinline__ auto angles(const P& p, int b, int tb, int k)
+    {
+        if constexpr (kRope<P>) {
+            const int t = tb + row(k);
+            const bool input = t >= p.q0 && t < p.q1 && t >= p.n0;  // (all lanes of a row or none)
+            return input ? Angles(p.rope, input_position(p, b, t - p.n0), chan(k) >> 3) : Angles();
+        } else {
+            return NoAngles();
+        }
+    }
+
     // Issue the loads (bf16 input for tokens of this call, fp16 window slots
     // for tokens appended earlier).
     template <typename P>
@@ -190,10 +258,10 @@ struct RowStage {
     }
 
     // The eight values of step k as the coder sees them: widened to fp32; for
-    // tokens of this call (keys: turned to their positions) rotated, and rounded
+    // tokens of this call (keys: turned by the angles `turn`) rotated, and rounded
     // to fp16 when a window exists.
-    template <bool KEYS, typename P>
-    __device__ __forceinline__ void widen(const P& p, int b, int tb, int k, float* v) const
+    template <typename P, typename A>
+    __device__ __forceinline__ void widen(const P& p, int tb, int k, float* v, const A& turn) const
     {
         const int t = tb + row(k);
         const bool fresh = !(t >= p.q0 && t < p.q1) || t >= p.n0;  // bf16 (zero rows: zero words)
@@ -209,9 +277,9 @@ struct RowStage {
             }
         }
         const bool input = t >= p.q0 && t < p.q1 && t >= p.n0;
-        if constexpr (KEYS && kRope<P>) {
+        if constexpr (std::is_same<A, Angles>::value) {
             if (input)  // (all lanes of a row or none)
-                rope_row8<D>(p.rope, input_position(p, b, t - p.n0), chan(k) >> 3, v);
+                turn.template turn<D>(p.rope, chan(k) >> 3, v);
         }
         if (p.rotate) {
             float r[8];
@@ -263,7 +331,7 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
         for (int k = 0; k < RowStage<D>::kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8, t = tb + i;
             float x[8];
-            kst.template widen<true>(p, b, tb, k, x);
+            kst.widen(p, tb, k, x, RowStage<D>::angles(p, b, tb, k));
             float s, z;
             piece_group_stats(x, lanes, p.k_mode, kb, &s, &z);
             round_meta(p.meta16, &s, &z);
@@ -292,7 +360,7 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
     for (int k = 0; k < RowStage<D>::kSteps; ++k) {
         const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8, t = tb + i;
         float x[8];
-        vst.template widen<false>(p, b, tb, k, x);
+        vst.widen(p, tb, k, x, NoAngles());
         float s, z;
         piece_group_stats(x, vlanes, p.v_mode, vb, &s, &z);
         round_meta(p.meta16, &s, &z);
@@ -345,6 +413,11 @@ __device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, 
 #pragma clang fp contract(off)
     const float top = (float)((1 << BITS) - 1), qmax = (float)((1 << (BITS - 1)) - 1), half = (float)(1 << (BITS - 1));
     const bool aff = mode == KVQ_AFFINE;
+    // The product q is within 2^-22 |d / s| of fl(d / s): 2^-23 of the reciprocal
+    // and two roundings.  Below 2^BITS that is 2^(BITS - 22), beyond it both clamp;
+    // so the codes can differ only where q is as near to a half-integer.  (Four
+    // times that; 2^-10 at any width sent 6 of 10 waves to the divisions.)
+    constexpr float kNear = BITS == 8 ? 0x1p-12f : BITS == 4 ? 0x1p-16f : 0x1p-18f;
     float c[8], worst = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -352,7 +425,7 @@ __device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, 
         c[e] = __builtin_rintf(q);
         worst = fmaxf(worst, fabsf(q - c[e]));
     }
-    if (worst >= 0.5f - 0x1p-10f) {
+    if (worst >= 0.5f - kNear) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             c[e] = __builtin_rintf((aff ? x[e] - z[e] : x[e]) / s[e]);
@@ -395,7 +468,7 @@ __device__ __forceinline__ float row_ror8(float v)
 // 348 MB) took 164 us with rows staged in LDS, one thread per channel for the
 // statistics, codes as bytes and 64-bit shifts; 115 now, window rows included.
 template <int D, bool PERCH, int KB, int VB, typename Params>
-__global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
+__device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
 {
     constexpr int PPT = D / 8, kOut = 4 * D * (KB > VB ? KB : VB);
     // a section's pieces, and the value codes by token (edge_block: all of it)
@@ -408,15 +481,13 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
     __shared__ __attribute__((aligned(16))) float cs[PERCH ? 3 : 1][PERCH ? D : 4];  // channel scales, reciprocals, offsets
     constexpr int kSteps = RowStage<D>::kSteps;
 
-    const int unit = blockIdx.y;
-    const int b = unit / p.H, h = unit % p.H;
-    const int tb = (p.q0 / kBlockTok + (int)blockIdx.x) * kBlockTok;
     if constexpr (!PERCH) {
         if (tb < p.q0 || tb + kBlockTok > p.q1) {
             edge_block<D>(p, unit, tb, pool);
             return;
         }
     }
+    const int b = unit / p.H, h = unit % p.H;
     const int msz = p.meta16 ? 2 : 4;
     const size_t blk = (size_t)unit * (size_t)(p.T / kBlockTok) + (size_t)(tb / kBlockTok);
     RowStage<D> kst, vst;
@@ -432,7 +503,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
         for (int k = 0; k < kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8;
             float x[8], s, z;
-            kst.template widen<true>(p, b, tb, k, x);
+            kst.widen(p, tb, k, x, RowStage<D>::angles(p, b, tb, k));
             piece_group_stats(x, lanes, p.k_mode, KB, &s, &z);
             round_meta(p.meta16, &s, &z);
             if (P % lanes == 0) {
@@ -449,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
         float x[kSteps][8], mn[8], mx[8];
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
-            kst.template widen<true>(p, b, tb, k, x[k]);
+            kst.widen(p, tb, k, x[k], RowStage<D>::angles(p, b, tb, k));
         const bool aff = p.k_mode == KVQ_AFFINE;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -521,7 +592,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
     for (int k = 0; k < kSteps; ++k) {
         const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8;
         float x[8], s, z;
-        vst.template widen<false>(p, b, tb, k, x);
+        vst.widen(p, tb, k, x, NoAngles());
         piece_group_stats(x, vlanes, p.v_mode, VB, &s, &z);
         round_meta(p.meta16, &s, &z);
         if (P % vlanes == 0) {
@@ -564,6 +635,14 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(Params p)
     if (p.v_mode == KVQ_AFFINE)
         copy_out((const uint8_t*)mb[1], (uint8_t*)p.vz + blk * (size_t)(vmeta * msz), vmeta * msz);
 }
+
+#ifndef KVQ_APPEND_ROPE
+template <int D, bool PERCH, int KB, int VB>
+__global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
+{
+    code_block<D, PERCH, KB, VB>(p, blockIdx.y, (p.q0 / kBlockTok + (int)blockIdx.x) * kBlockTok);
+}
+#endif
 
 // One decoded token per (sequence, KV head) without a window: a workgroup of
 // D threads, thread d owning channel d of the token's K and V.  Every load
@@ -638,6 +717,16 @@ __global__ __launch_bounds__(D) void append_token_kernel(Params p)
     __shared__ float xs[2][D];
     __shared__ float red[8 * 4];
     const int unit = blockIdx.x, b = unit / p.H, h = unit % p.H, d = threadIdx.x;
+    if constexpr (kRope<Params>) {
+        if (unit >= p.B * p.H) {  // a row of queries
+            const RopeQkParams& q = p.queries;
+            const size_t row = unit - p.B * p.H;
+            const float x = rope_channel<D>(p.rope, input_position(p, (int)(row / q.H_q), 0), bf16_to_f32(q.q[row * D + d]),
+                                            p.rope.wq, xs[0]);
+            q.qo[row * D + d] = f32_to_bf16(x);
+            return;
+        }
+    }
     const int t = p.n0, tau = t & 31, j = t & 7;
     const size_t blk = (size_t)unit * (p.T / kBlockTok) + (size_t)(t / kBlockTok);
     const size_t vpi = value_piece<D>(blk, tau >> 3, d);
@@ -722,12 +811,11 @@ template <int D>
 constexpr int kRingRows = kThreads / (D / 8);
 
 template <int D, typename Params>
-__global__ __launch_bounds__(kThreads) void append_ring_kernel(Params p, int hi)
+__device__ __forceinline__ void write_rows(const Params& p, int hi, int unit, int first)
 {
-    const int unit = blockIdx.y;
     const int b = unit / p.H, h = unit % p.H;
     const int c8 = 8 * ((int)threadIdx.x % (D / 8));
-    const int t = p.ring_lo + kRingRows<D> * (int)blockIdx.x + (int)threadIdx.x / (D / 8);
+    const int t = first + (int)threadIdx.x / (D / 8);
     u32x4 w[2] = {u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}};
     if (t < hi) {
         const size_t at = (input_row(p, b, t - p.n0) * p.H + h) * D + c8;
@@ -743,7 +831,7 @@ __global__ __launch_bounds__(kThreads) void append_ring_kernel(Params p, int hi)
             v[e] = __uint_as_float((e & 1) ? ww[e >> 1] & 0xFFFF0000u : ww[e >> 1] << 16);
         if constexpr (kRope<Params>) {
             if (q == 0 && t < hi)
-                rope_row8<D>(p.rope, input_position(p, b, t - p.n0), c8 >> 3, v);
+                Angles(p.rope, input_position(p, b, t - p.n0), c8 >> 3).template turn<D>(p.rope, c8 >> 3, v);
         }
         if (p.rotate)  // (every lane of a row takes part)
             rotate8<D>(v, c8 >> 3, p.rot_c);
@@ -757,60 +845,403 @@ __global__ __launch_bounds__(kThreads) void append_ring_kernel(Params p, int hi)
     }
 }
 
-template <int D, bool PERCH, typename P>
-void launch_blocks(const P& p, int blocks, int units, hipStream_t stream)
+template <int D, typename Params>
+__global__ __launch_bounds__(kThreads) void append_ring_kernel(Params p, int hi)
 {
-    const dim3 g(blocks, units), t(kThreads);
-    if (p.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
-        launch_kernel((append_block_kernel<D, PERCH, 8, 8, P>), g, t, 0, stream, p);
-    else if (p.k_bits == 4 && p.v_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 4, 4, P>), g, t, 0, stream, p);
-    else if (p.k_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 4, 2, P>), g, t, 0, stream, p);
-    else if (p.v_bits == 4)
-        launch_kernel((append_block_kernel<D, PERCH, 2, 4, P>), g, t, 0, stream, p);
-    else
-        launch_kernel((append_block_kernel<D, PERCH, 2, 2, P>), g, t, 0, stream, p);
+    write_rows<D>(p, hi, blockIdx.y, p.ring_lo + kRingRows<D> * (int)blockIdx.x);
 }
 
 template <int D, typename P>
-hipError_t launch_append_d(const P& p, hipStream_t stream)
+void launch_ring(const P& p, int hi, hipStream_t stream)
+{
+    launch_kernel((append_ring_kernel<D, P>), dim3((hi - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, p.B * p.H), dim3(kThreads),
+                  0, stream, p, hi);
+}
+
+#ifdef KVQ_APPEND_ROPE
+// The coder of code_heads: the codes, scales and offsets of piece_group_stats,
+// round_meta and piece_codes in fewer operations.  A symmetric group is one with
+// offset zero and other limits (`bias` makes its codes unsigned); the sums of a
+// group meet by DPP, and a group's range is divided by 2^b - 1 as
+//     q = fl(d fl(1 / n)),  s = fl(q + fl(d - q n) fl(1 / n)),
+// the correctly rounded quotient (checked for every mantissa and n = 1, 3, 7, 15,
+// 127, 255; where it would be subnormal the scale is 1e-8).
+template <int BITS, bool PLAIN>
+struct Coder {
+    float n, inv, lo, hi, bias;  // bias: of 16 / BITS codes in their places
+    bool affine;
+
+    __device__ __forceinline__ explicit Coder(int mode) : affine(PLAIN || mode == KVQ_AFFINE)
+    {
+        constexpr float top = (float)((1 << BITS) - 1), qmax = (float)((1 << (BITS - 1)) - 1);
+        constexpr float half = (float)(1 << (BITS - 1));
+        n = affine ? top : qmax;
+        inv = affine ? 1.0f / top : 1.0f / qmax;
+        lo = affine ? 0.0f : -qmax;
+        hi = n;
+        bias = affine ? 0.0f : half * (65535.0f / top);
+    }
+
+    template <int CTRL>
+    static __device__ __forceinline__ float dpp(float x)
+    {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true));
+    }
+
+    // Over `lanes` (4, 8, 16 or 32) lanes.
+    template <typename F>
+    static __device__ __forceinline__ float reduce(float x, int lanes, F f)
+    {
+        x = f(x, dpp<0xB1>(x));
+        x = f(x, dpp<0x4E>(x));
+        if (lanes > 4)
+            x = f(x, dpp<0x141>(x));
+        if (lanes > 8)
+            x = f(x, dpp<0x140>(x));
+        if (lanes > 16)
+            x = f(x, __shfl_xor(x, 16));
+        return x;
+    }
+
+    __device__ __forceinline__ void scale(const float* x, int lanes, int meta16, float* s, float* z) const
+    {
+#pragma clang fp contract(off)
+        const auto least = [](float a, float b) { return fminf(a, b); };
+        const auto most = [](float a, float b) { return fmaxf(a, b); };
+        float d;
+        if (affine) {
+            float mn = x[0], mx = x[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) {
+                mn = fminf(mn, x[e]);
+                mx = fmaxf(mx, x[e]);
+            }
+            mn = reduce(mn, lanes, least);
+            mx = reduce(mx, lanes, most);
+            d = mx - mn;
+            *z = mn + 0.0f;  // canonical +0 for a signed-zero minimum
+        } else {
+            float ma = fabsf(x[0]);
+#pragma unroll
+            for (int e = 1; e < 8; ++e)
+                ma = fmaxf(ma, fabsf(x[e]));
+            d = reduce(ma, lanes, most);
+            *z = 0.0f;
+        }
+        const float q = d * inv;
+        *s = fmaxf(__builtin_fmaf(__builtin_fmaf(-q, n, d), inv, q), 1e-8f);
+        round_meta(meta16, s, z);
+    }
+
+    // (kNear: as in piece_codes)
+    __device__ __forceinline__ uint64_t piece(const float* x, float s, float z) const
+    {
+#pragma clang fp contract(off)
+        constexpr float kNear = BITS == 8 ? 0x1p-12f : BITS == 4 ? 0x1p-16f : 0x1p-18f;
+        const float r = __builtin_amdgcn_rcpf(s);
+        float c[8], worst = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float q = (x[e] - z) * r;
+            c[e] = __builtin_rintf(q);
+            worst = fmaxf(worst, fabsf(q - c[e]));
+        }
+        if (worst >= 0.5f - kNear) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                c[e] = __builtin_rintf((x[e] - z) / s);
+        }
+        constexpr int N = 16 / BITS;  // codes per 16 bits
+        uint64_t word = 0;
+#pragma unroll
+        for (int k = 0; k < 8 / N; ++k) {
+            float v = 0.0f;
+#pragma unroll
+            for (int e = N - 1; e >= 0; --e)
+                v = __builtin_fmaf(v, (float)(1 << BITS), __builtin_amdgcn_fmed3f(c[N * k + e], lo, hi));
+            const uint32_t w = (uint32_t)(v + bias);
+            if constexpr (BITS == 8)
+                word |= (uint64_t)w << (16 * k);
+            else
+                word = (uint32_t)word | (w << (16 * k));
+        }
+        return word;
+    }
+};
+
+// Tokens t0 .. t0 + 2048 / D - 1 of one sequence's heads h0 .., all of them coded by
+// this call, per-token groups: a thread owns eight channels of one token, so that
+// its keys turn by the same eight angles in every head, which cost as much as a
+// third of a head's coding.  (With a 32-token block of one head per workgroup, as
+// code_block, a thread has the angles of up to four rows: 64 registers where heads
+// are to share them.)
+// The codes of a head meet in one of two LDS buffers, so one barrier a head is
+// enough: key pieces in their final order (eight runs of 32 pieces), value words by
+// token, of which each thread then makes one piece of eight tokens, and the scales
+// and offsets.  The next head's rows are loaded meanwhile.
+// PLAIN: affine codes of tokens that are all this call's, without a transform or a
+// window; what the call decides at run time otherwise costs a fifth of the work.
+template <int D, int KB, int VB, bool PLAIN>
+__device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int h0, int heads, int t0)
+{
+    constexpr int PPT = D / 8, T = kThreads / PPT;
+    struct Buffer {
+        uint8_t k[kThreads * KB], v[kThreads * VB];
+        float meta[4][64];  // key scales, offsets, value scales, offsets: [groups][T]
+    };
+    __shared__ __attribute__((aligned(16))) Buffer buffers[2];
+    const int tid = threadIdx.x, i = tid / PPT, P = tid % PPT, t = t0 + i;
+    const bool fresh = PLAIN || t >= p.n0;
+    const size_t row = fresh ? input_row(p, b, t - p.n0) * p.H : ((size_t)b * p.H) * p.ring + t % p.ring;
+    const size_t step = fresh ? D : (size_t)p.ring * D;  // from head to head
+    const uint16_t* ksrc = (fresh ? p.kin : p.kr) + row * D + h0 * step + 8 * P;
+    const uint16_t* vsrc = (fresh ? p.vin : p.vr) + row * D + h0 * step + 8 * P;
+    u32x4 kw = *(const u32x4*)ksrc, vw = *(const u32x4*)vsrc, norm = {0u, 0u, 0u, 0u};
+    if (p.rope.wk)
+        norm = *(const u32x4*)(p.rope.wk + 8 * P);
+    const Angles turn = fresh ? Angles(p.rope, input_position(p, b, t - p.n0), P) : Angles();
+
+    const Coder<KB, PLAIN> kcode(p.k_mode);
+    const Coder<VB, PLAIN> vcode(p.v_mode);
+    const int tau = t % kBlockTok, o0 = t0 % kBlockTok / 8;
+    const int klanes = p.k_group / 8, vlanes = p.v_group / 8;
+    // this thread's key piece in its buffer: run (half, P % 4), row of the run, P / 4
+    const int kp = (((tau >> 2 & 1) * 4 + (P & 3)) * (T / 2) + 4 * ((tau >> 3) - o0) + (tau & 3)) * (D / 32) + (P >> 2);
+    // the value piece it makes (octet, channel) of words vfirst, vfirst + PPT, ..
+    const int vd = 16 * (tid % (D / 16)) + tid / (D / 16) % 16, vfirst = 8 * (tid / D) * PPT + vd / 8;
+    // the metadata element it stores: of array tid / 64, group and token
+    const int ma = tid >> 6, mg = (tid & 63) / T, ng = D / (ma < 2 ? p.k_group : p.v_group);
+    const bool stores = mg < ng && (!(ma & 1) || (ma == 1 ? p.k_mode : p.v_mode) == KVQ_AFFINE);
+    float* meta = ma == 0 ? p.ks : ma == 1 ? p.kz : ma == 2 ? p.vs : p.vz;
+    // of head h0; every head is `blocks` blocks on
+    const size_t blk = (size_t)(b * p.H + h0) * (size_t)(p.T / kBlockTok) + (size_t)(t0 / kBlockTok), blocks = p.T / kBlockTok;
+    const int run = tid / (2 * KB);
+    uint8_t* kdst = (uint8_t*)p.kc + (blk * (size_t)(4 * D) + (size_t)(((run >> 2) * 64 + 16 * (run & 3) + 4 * o0) * (D / 32))) * KB +
+                    16 * (tid % (2 * KB));
+    uint8_t* vdst = (uint8_t*)p.vc + (blk * (size_t)(4 * D) + (size_t)(16 * o0 * (D / 16)) + tid) * VB;
+    size_t mdst = (blk * ng + mg) * kBlockTok + 8 * o0 + (tid & 63) % T;
+    const auto widen = [&](const u32x4& w, float* x) {
+        if (fresh) {
+            widen8(w, x);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                x[2 * q] = f16_bits_to_f32((uint16_t)w[q]);
+                x[2 * q + 1] = f16_bits_to_f32((uint16_t)(w[q] >> 16));
+            }
+        }
+    };
+    const auto to_cache = [&](float* x) {  // as the coder sees it (a window's slots hold rows that are)
+        if (!PLAIN && p.rotate && fresh)  // (all lanes of a row or none)
+            rotate8<D>(x, P, p.rot_c);
+        if (!PLAIN && p.ring && fresh) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[e] = f16_bits_to_f32(f32_to_f16_bits(x[e]));
+        }
+    };
+    for (int j = 0; j < heads; ++j) {
+        Buffer& buf = buffers[j & 1];
+        float x[8], s, z;
+        widen(kw, x);
+        ksrc += step;
+        if (j + 1 < heads)
+            kw = *(const u32x4*)ksrc;
+        if (fresh)
+            turn.template turn<D>(p.rope, norm, P, x);
+        to_cache(x);
+        kcode.scale(x, klanes, p.meta16, &s, &z);
+        if (P % klanes == 0) {
+            buf.meta[0][P / klanes * T + i] = s;
+            buf.meta[1][P / klanes * T + i] = z;
+        }
+        store_piece(buf.k, kp, KB, kcode.piece(x, s, z));
+        widen(vw, x);
+        vsrc += step;
+        if (j + 1 < heads)
+            vw = *(const u32x4*)vsrc;
+        to_cache(x);
+        vcode.scale(x, vlanes, p.meta16, &s, &z);
+        if (P % vlanes == 0) {
+            buf.meta[2][P / vlanes * T + i] = s;
+            buf.meta[3][P / vlanes * T + i] = z;
+        }
+        store_piece(buf.v, i * PPT + P, VB, vcode.piece(x, s, z));
+        __syncthreads();
+        if (tid < 16 * KB)  // 16 bytes of the key pieces
+            *(u32x4*)kdst = *(const u32x4*)(buf.k + 16 * tid);
+        uint64_t word = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const uint64_t w = load_piece(buf.v, vfirst + q * PPT, VB);
+            if constexpr (VB == 8)
+                word |= (w >> (8 * (vd & 7)) & 0xFFu) << (8 * q);
+            else
+                word |= (uint32_t)((uint32_t)w >> (VB * (vd & 7)) & ((1u << VB) - 1u)) << (VB * q);
+        }
+        store_piece(vdst, 0, VB, word);
+        if (stores)
+            store_meta(meta, mdst, buf.meta[ma][tid & 63], p.meta16);
+        kdst += blocks * (size_t)(4 * D * KB);
+        vdst += blocks * (size_t)(4 * D * VB);
+        mdst += blocks * (size_t)(ng * kBlockTok);
+    }
+}
+
+// One launch for all that an append with positions does: workgroups that code
+// blocks, the longest, come first, then those that write window rows and those that
+// rotate queries (four waves of rope_rows).
+constexpr int kQueryIter = 4;  // iterations of a wave
+
+template <int D, bool PERCH, int KB, int VB, bool PLAIN>
+__global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendRopeParams p)
+{
+    uint32_t x = blockIdx.x;
+    if (x < p.code_wgs) {
+        const uint32_t units = p.B * p.H, singles = units * p.edges;  // blocks of one head
+        if (x < singles) {
+            const int e = (int)(x / units), unit = (int)(x - e * units);
+            const int blk = PERCH ? p.q0 / kBlockTok + e : e == 0 && p.q0 % kBlockTok ? p.q0 / kBlockTok : p.q1 / kBlockTok;
+            code_block<D, PERCH, KB, VB>(p, unit, kBlockTok * blk);
+        } else if constexpr (!PERCH) {
+            constexpr int T = 2048 / D, PARTS = kBlockTok / T;
+            x -= singles;
+            const uint32_t hg = (p.H + p.heads - 1) / p.heads, y = x / hg, h0 = (x - y * hg) * p.heads;
+            const uint32_t b = y / (p.blocks * PARTS), part = y - b * (p.blocks * PARTS);
+            code_heads<D, KB, VB, PLAIN>(p, (int)b, (int)h0, min(p.heads, p.H - (int)h0),
+                                         (p.q0 + kBlockTok - 1) / kBlockTok * kBlockTok + (int)part * T);
+        }
+        return;
+    }
+    x -= p.code_wgs;
+    if (x < p.row_wgs) {
+        const uint32_t per = p.row_wgs / (p.B * p.H), unit = x / per;
+        write_rows<D>(p, p.n0 + p.n_new, (int)unit, p.ring_lo + kRingRows<D> * (int)(x - unit * per));
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) float2 angles[kThreads / 64][D / 2];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const uint32_t item = (x - p.row_wgs) * (kThreads / 64) + wave, token = item / (uint32_t)p.queries.parts;
+    if (token < (uint32_t)p.queries.tokens)
+        rope_rows<D, kQueryIter, false>(p.queries, p.rope, token, (int)(item - token * (uint32_t)p.queries.parts), angles[wave]);
+}
+
+template <int D, bool PERCH, bool PLAIN>
+void launch_blocks(const AppendRopeParams& p, uint32_t grid, hipStream_t stream)
+{
+    const dim3 g(grid), t(kThreads);
+    if (p.k_bits == 8)
+        launch_kernel((append_rope_kernel<D, PERCH, 8, 8, PLAIN>), g, t, 0, stream, p);
+    else if (p.k_bits == 4 && p.v_bits == 4)
+        launch_kernel((append_rope_kernel<D, PERCH, 4, 4, PLAIN>), g, t, 0, stream, p);
+    else if (p.k_bits == 4)
+        launch_kernel((append_rope_kernel<D, PERCH, 4, 2, PLAIN>), g, t, 0, stream, p);
+    else if (p.v_bits == 4)
+        launch_kernel((append_rope_kernel<D, PERCH, 2, 4, PLAIN>), g, t, 0, stream, p);
+    else
+        launch_kernel((append_rope_kernel<D, PERCH, 2, 2, PLAIN>), g, t, 0, stream, p);
+}
+
+template <int D>
+hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
+{
+    const int units = p.B * p.H, n1 = p.n0 + p.n_new;
+    if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
+        launch_kernel((append_token_kernel<D, AppendRopeParams>), dim3(units + p.queries.tokens * p.queries.H_q), dim3(D), 0, stream, p);
+        return hipGetLastError();
+    }
+    // whole blocks by code_heads, those at the ends (and per-channel keys) by code_block
+    const int lo = (p.q0 + kBlockTok - 1) / kBlockTok, hi = p.q1 / kBlockTok;
+    const bool perch = p.k_axis == KVQ_PER_CHANNEL;
+    p.blocks = perch || hi < lo ? 0 : hi - lo;
+    p.edges = perch ? hi - lo : p.q1 <= p.q0 ? 0 : hi < lo ? 1 : (p.q0 % kBlockTok != 0) + (p.q1 % kBlockTok != 0);
+    const long long parts = (long long)p.blocks * p.B * (kBlockTok * D / 2048);
+    p.heads = 1;
+    while (p.heads < 4 && p.heads < p.H && parts * p.H > 4096 * p.heads)
+        p.heads *= 2;
+    p.code_wgs = (uint32_t)(parts * ((p.H + p.heads - 1) / p.heads)) + (uint32_t)(p.edges * units);
+    // the window's rows beside the coder, if none takes the slot of a token that is coded from it
+    const bool ring = p.ring && n1 > p.ring_lo, together = ring && n1 - p.ring <= p.q0;
+    p.row_wgs = together ? (uint32_t)((n1 - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>) * (uint32_t)units : 0;
+    uint32_t others = p.row_wgs;
+    if (p.queries.tokens > 0) {
+        constexpr int RPI = 1024 / D;
+        p.queries.parts = (p.queries.H_q + RPI * kQueryIter - 1) / (RPI * kQueryIter);
+        others += (uint32_t)(((long long)p.queries.tokens * p.queries.parts + kThreads / 64 - 1) / (kThreads / 64));
+    }
+    const uint32_t grid = p.code_wgs + others;
+    if (grid > 0) {
+        if (perch)
+            launch_blocks<D, true, false>(p, grid, stream);
+        else if (p.k_mode == KVQ_AFFINE && p.v_mode == KVQ_AFFINE && !p.rotate && !p.ring)
+            launch_blocks<D, false, true>(p, grid, stream);
+        else
+            launch_blocks<D, false, false>(p, grid, stream);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    if (ring && !together)
+        launch_ring<D>(p, n1, stream);
+    return hipGetLastError();
+}
+
+typedef AppendRopeParams Params;
+#else
+template <int D, bool PERCH>
+void launch_blocks(const AppendParams& p, int blocks, int units, hipStream_t stream)
+{
+    const dim3 g(blocks, units), t(kThreads);
+    if (p.k_bits == 8)  // 8-bit codes come as K and V both 8-bit
+        launch_kernel((append_block_kernel<D, PERCH, 8, 8>), g, t, 0, stream, p);
+    else if (p.k_bits == 4 && p.v_bits == 4)
+        launch_kernel((append_block_kernel<D, PERCH, 4, 4>), g, t, 0, stream, p);
+    else if (p.k_bits == 4)
+        launch_kernel((append_block_kernel<D, PERCH, 4, 2>), g, t, 0, stream, p);
+    else if (p.v_bits == 4)
+        launch_kernel((append_block_kernel<D, PERCH, 2, 4>), g, t, 0, stream, p);
+    else
+        launch_kernel((append_block_kernel<D, PERCH, 2, 2>), g, t, 0, stream, p);
+}
+
+template <int D>
+hipError_t launch_append_d(const AppendParams& p, hipStream_t stream)
 {
     const int units = p.B * p.H;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
-        launch_kernel((append_token_kernel<D, P>), dim3(units), dim3(D), 0, stream, p);
+        launch_kernel((append_token_kernel<D, AppendParams>), dim3(units), dim3(D), 0, stream, p);
         return hipGetLastError();
     }
     if (p.q1 > p.q0) {
         const int blocks = (p.q1 + kBlockTok - 1) / kBlockTok - p.q0 / kBlockTok;
         if (p.k_axis == KVQ_PER_CHANNEL)
-            launch_blocks<D, true, P>(p, blocks, units, stream);
+            launch_blocks<D, true>(p, blocks, units, stream);
         else
-            launch_blocks<D, false, P>(p, blocks, units, stream);
+            launch_blocks<D, false>(p, blocks, units, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
-    int n1 = p.n0 + p.n_new;
-    if (p.ring && n1 > p.ring_lo) {
-        launch_kernel((append_ring_kernel<D, P>), dim3((n1 - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, units), dim3(kThreads), 0,
-                      stream, p, n1);
-        return hipGetLastError();
-    }
-    return hipSuccess;
-}
-
-template <int D, typename P>
-hipError_t launch_rows_d(const P& p, int hi, hipStream_t stream)
-{
-    if (hi > p.ring_lo)
-        launch_kernel((append_ring_kernel<D, P>), dim3((hi - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>, p.B * p.H), dim3(kThreads), 0,
-                      stream, p, hi);
+    const int n1 = p.n0 + p.n_new;
+    if (p.ring && n1 > p.ring_lo)
+        launch_ring<D>(p, n1, stream);
     return hipGetLastError();
 }
 
-template <typename P>
-hipError_t launch_rows(const P& p, int D, int hi, hipStream_t stream)
+typedef AppendParams Params;
+#endif
+
+template <int D>
+hipError_t launch_rows_d(const Params& p, int hi, hipStream_t stream)
+{
+    if (hi > p.ring_lo)
+        launch_ring<D>(p, hi, stream);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_append_rows(const Params& p, int D, int hi, hipStream_t stream)
 {
     switch (D) {
     case 64:
@@ -824,8 +1255,7 @@ hipError_t launch_rows(const P& p, int D, int hi, hipStream_t stream)
     }
 }
 
-template <typename P>
-hipError_t launch(const P& p, int D, hipStream_t stream)
+hipError_t launch_append(const Params& p, int D, hipStream_t stream)
 {
     switch (D) {
     case 64:
@@ -837,25 +1267,6 @@ hipError_t launch(const P& p, int D, hipStream_t stream)
     default:
         return hipErrorInvalidValue;
     }
-}
-
-}  // namespace
-
-// Built for one kind of parameters per object.
-#ifdef KVQ_APPEND_ROPE
-typedef AppendRopeParams Params;
-#else
-typedef AppendParams Params;
-#endif
-
-hipError_t launch_append_rows(const Params& p, int D, int hi, hipStream_t stream)
-{
-    return launch_rows(p, D, hi, stream);
-}
-
-hipError_t launch_append(const Params& p, int D, hipStream_t stream)
-{
-    return launch(p, D, stream);
 }
 
 }  // namespace kvq

@@ -9,6 +9,7 @@
 #include <memory>
 #include <mutex>
 #include <new>
+#include <type_traits>
 
 #include "kvq_internal.h"
 
@@ -601,6 +602,11 @@ kvq_status run_append(kvq_cache* c, const void* K, const void* V, int n_new, P p
     p.rot_c = rotation_constant(c->D);
     p.meta16 = f.meta_fp16;
     const int n0 = c->n, n1 = n0 + n_new, S = f.sink;
+    if constexpr (std::is_same<P, kvq::AppendRopeParams>::value) {
+        // (queries go with the tail's launch)
+        if (n1 <= S && p.queries.tokens > 0 && kvq::launch_rope(p.queries, p.rope, c->D, (hipStream_t)stream) != hipSuccess)
+            return KVQ_ERR_DEVICE;
+    }
     if (n0 < S) {
         // sink tokens [n0, min(S, n1)): fp16 rows t of sections 8 and 9
         P ps = p;
@@ -744,7 +750,8 @@ kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B
     if (tokens > INT32_MAX || heads > INT32_MAX || tokens * heads >= kvq::kRopeRows)
         return KVQ_ERR_ARG;
     kvq::RopeQkParams p = {};
-    const kvq_status st = rope_args(rope, D, Q ? q_norm : nullptr, K ? k_norm : nullptr, pos, pos0, n, &p.rope);
+    kvq::RopeArgs args;
+    const kvq_status st = rope_args(rope, D, Q ? q_norm : nullptr, K ? k_norm : nullptr, pos, pos0, n, &args);
     if (st != KVQ_OK || n == 0)
         return st;
     p.q = (const uint16_t*)Q;
@@ -755,7 +762,7 @@ kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B
     p.n = n;
     p.H_q = H_q;
     p.H = H_kv;
-    return kvq::launch_rope(p, D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
+    return kvq::launch_rope(p, args, D, (hipStream_t)stream) == hipSuccess ? KVQ_OK : KVQ_ERR_DEVICE;
 }
 
 kvq_status kvq_append_rope(kvq_cache* c, const kvq_rope* rope, const void* K, const void* V, int n_in,
@@ -778,18 +785,11 @@ kvq_status kvq_append_rope(kvq_cache* c, const kvq_rope* rope, const void* K, co
         return rs;
     p.rows = rows;
     p.n_in = n_in;
-    if (Q) {
-        kvq::RopeQkParams q = {};
-        q.q = (const uint16_t*)Q;
-        q.qo = (uint16_t*)Qo;
-        q.tokens = (int)tokens;
-        q.n = n_new;
-        q.H_q = H_q;
-        q.rope = p.rope;
-        q.rope.wk = nullptr;
-        if (kvq::launch_rope(q, c->D, (hipStream_t)stream) != hipSuccess)
-            return KVQ_ERR_DEVICE;
-    }
+    p.queries.q = (const uint16_t*)Q;
+    p.queries.qo = (uint16_t*)Qo;
+    p.queries.tokens = Q ? (int)tokens : 0;
+    p.queries.n = n_new;
+    p.queries.H_q = H_q;
     return run_append(c, K, V, n_new, p, stream);
 }
 

@@ -93,11 +93,10 @@ struct RopeQkParams {
     int tokens, n;        // B n
     int H_q, H;
     int parts;            // waves that share a token's heads (set at launch)
-    RopeArgs rope;
 };
 // Upper bound of tokens (H_q + H) for 32-bit indexing of waves.
 constexpr long long kRopeRows = 1ll << 31;
-hipError_t launch_rope(const RopeQkParams& p, int D, hipStream_t stream);
+hipError_t launch_rope(const RopeQkParams& p, const RopeArgs& rope, int D, hipStream_t stream);
 // An append whose keys are normed and rotated on the way (kvq_append_rope);
 // p.n_new tokens of the n_in that kin and vin have of every sequence, chosen by
 // rows [B][n_new] or the first ones.
@@ -105,6 +104,11 @@ struct AppendRopeParams : AppendParams {
     const int32_t* rows;
     int n_in;
     RopeArgs rope;
+    RopeQkParams queries; // tokens = 0: none
+    // the workgroups' shares (set at launch)
+    int blocks, heads;    // whole 32-token blocks of a sequence, heads of a workgroup that codes some of their tokens
+    int edges;            // blocks of a sequence that are coded by head
+    uint32_t code_wgs, row_wgs;
 };
 hipError_t launch_append(const AppendRopeParams& p, int D, hipStream_t stream);
 hipError_t launch_append_rows(const AppendRopeParams& p, int D, int hi, hipStream_t stream);

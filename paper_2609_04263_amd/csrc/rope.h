@@ -47,7 +47,10 @@ __device__ __forceinline__ float2 rope_cos_sin(int t, double turn, float scale)
     return make_float2((float)((k + 1) & 2 ? -(a * m) : a * m), (float)(k & 2 ? -(b * m) : b * m));
 }
 
-// bf16 pairs -> fp32, and back (round to nearest even).
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// bf16 pairs -> fp32, and back (round to nearest even: one conversion a pair).
 __device__ __forceinline__ void widen8(const u32x4& w, float* v)
 {
 #pragma unroll
@@ -62,7 +65,7 @@ __device__ __forceinline__ u32x4 narrow8(const float* v)
     u32x4 w;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        w[j] = f32_to_bf16(v[2 * j]) | ((uint32_t)f32_to_bf16(v[2 * j + 1]) << 16);
+        w[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * j], v[2 * j + 1]}), bf16x2));
     return w;
 }
 
@@ -72,8 +75,8 @@ template <int CTRL>
 __device__ __forceinline__ double dpp_f64(double x)
 {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, 0xF, 0xF, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 
@@ -103,11 +106,16 @@ __device__ __forceinline__ double squares8(const float* v)
     return s;
 }
 
-// The factor of a row with sum of squares `sum`.
+// The factor of a row with sum of squares `sum`: 1 / sqrt(v) by the hardware's
+// estimate y (2^-23 or better) and one step of third order, y (1 + e / 2 + 3 e^2 / 8)
+// with e = 1 - v y^2 (binary64: off by 2^-51, so the binary32 result is the nearest
+// in all but 1 of 10^8 cases).
 __device__ __forceinline__ float norm_factor(double sum, int D, float eps)
 {
 #pragma clang fp contract(off)
-    return (float)(1.0 / __builtin_sqrt(sum / (double)D + (double)eps));
+    const double v = sum * (1.0 / D) + (double)eps, y = __builtin_amdgcn_rsq(v);
+    const double e = __builtin_fma(-(v * y), y, 1.0);
+    return (float)__builtin_fma(y * e, __builtin_fma(0.375, e, 0.5), y);
 }
 
 __device__ __forceinline__ void norm8(float* v, float r, const float* w)
@@ -125,6 +133,101 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s)
     const float x = a * c - b * s, y = b * c + a * s;
     a = x;
     b = y;
+}
+
+// One wave's share of rotating queries and keys: ITER iterations of 1024 / D heads of
+// one token, all loaded before the angles are computed; lds: D / 2 of the wave.
+//
+// A lane holds sixteen channels of a row, such that both members of each of its
+// eight pairs are its own and the pairs are 8 l .. 8 l + 7 in either layout:
+//     halves       channels 8 l .. and rot / 2 + 8 l ..  (l < rot / 16)
+//     interleaved  channels 16 l .. 16 l + 15, as are those that are not rotated
+// (two 16-byte loads), so rotating needs no exchange, and lane l's eight cosines
+// and sines are the same for every head of a token: the wave's lanes compute each
+// once, pass them on through LDS and keep their eight in registers.
+// KEYS: there may be keys beside the queries.
+template <int D, int ITER, bool KEYS>
+__device__ __forceinline__ void rope_rows(const RopeQkParams& p, const RopeArgs& r, uint32_t token, int part, float2* lds)
+{
+    constexpr int LPR = D / 16, RPI = 64 / LPR;  // lanes of a row, rows of an iteration
+    const int lane = threadIdx.x & 63, l = lane & (LPR - 1);
+    const bool half = r.layout == KVQ_ROPE_HALF && l < r.rot / 16;
+    const int c0 = half ? 8 * l : 16 * l, c1 = half ? r.rot / 2 + 8 * l : 16 * l + 8;
+    u32x4 w[ITER][2];
+    const int heads = p.H_q + (KEYS ? p.H : 0), h0 = part * ITER * RPI + lane / LPR;
+    const auto row_of = [&](const uint16_t* q, const uint16_t* k, int h) {
+        if constexpr (KEYS)
+            return h < p.H_q ? q + ((size_t)token * p.H_q + h) * D : k + ((size_t)token * p.H + (h - p.H_q)) * D;
+        else
+            return q + ((size_t)token * p.H_q + h) * D;
+    };
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int h = h0 + i * RPI;
+        if (h < heads) {
+            const uint16_t* row = row_of(p.q, p.k, h);
+            w[i][0] = *(const u32x4*)(row + c0);
+            w[i][1] = *(const u32x4*)(row + c1);
+        }
+    }
+    float cs[8], sn[8];
+    if (r.rot > 0) {
+        const int t = r.pos ? r.pos[token] : r.pos0 + (int)(token % (uint32_t)p.n);
+#pragma unroll
+        for (int i = lane; i < D / 2; i += 64)
+            if (i < r.rot / 2)
+                lds[i] = rope_cos_sin(t, r.turns[i], r.scale);
+        asm volatile("" ::: "memory");  // LDS accesses of a wave are performed in order
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const float4 x = *(const float4*)&lds[8 * l + j];
+            cs[j] = x.x, sn[j] = x.y, cs[j + 1] = x.z, sn[j + 1] = x.w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        const int h = h0 + i * RPI;
+        if (i > 0 && (part * ITER + i) * RPI >= heads)
+            break;
+        float v[16];
+        widen8(w[i][0], v);
+        widen8(w[i][1], v + 8);
+        if (r.wq || (KEYS && r.wk)) {  // (every lane of a row takes part in its sum)
+            const bool is_q = !KEYS || h < p.H_q;
+            const uint16_t* any = KEYS && !r.wq ? r.wk : r.wq;
+            const uint16_t* weight = !KEYS || is_q ? r.wq : r.wk;
+            float f = norm_factor(row_sum<LPR>(squares8(v) + squares8(v + 8)), D, r.eps);
+            float g[16];
+            const uint16_t* at = weight ? weight : any;
+            widen8(*(const u32x4*)(at + c0), g);
+            widen8(*(const u32x4*)(at + c1), g + 8);
+            if (KEYS && (!r.wq || !r.wk)) {  // rows of the kind without a norm: times one, twice
+                f = weight ? f : 1.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    g[e] = weight ? g[e] : 1.0f;
+            }
+            norm8(v, f, g);
+            norm8(v + 8, f, g + 8);
+        }
+        if (16 * l < r.rot) {
+            if (half) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    turn_pair(v[j], v[j + 8], cs[j], sn[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    turn_pair(v[2 * j], v[2 * j + 1], cs[j], sn[j]);
+            }
+        }
+        if (h < heads) {
+            uint16_t* row = const_cast<uint16_t*>(row_of(p.qo, p.ko, h));
+            *(u32x4*)(row + c0) = narrow8(v);
+            *(u32x4*)(row + c1) = narrow8(v + 8);
+        }
+    }
 }
 
 }  // namespace kvq
