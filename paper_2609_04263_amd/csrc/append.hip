@@ -455,6 +455,7 @@ __device__ __forceinline__ float row_ror8(float v)
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xF, 0xF, false));
 }
 
+#ifndef KVQ_APPEND_ROPE
 // One workgroup per 32-token block of one (sequence, KV head); a block this
 // call does not write whole takes edge_block (in a launch of its own it cost
 // 5 to 10 us a call).  Per-token groups: each thread takes the eight channels of one piece, the
@@ -467,8 +468,8 @@ __device__ __forceinline__ float row_ror8(float v)
 // Vector work bounds it.  A KIVI chunk of 2048 tokens (B = 32, 8 heads of 128,
 // 348 MB) took 164 us with rows staged in LDS, one thread per channel for the
 // statistics, codes as bytes and 64-bit shifts; 115 now, window rows included.
-template <int D, bool PERCH, int KB, int VB, typename Params>
-__device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
+template <int D, bool PERCH, int KB, int VB>
+__global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
 {
     constexpr int PPT = D / 8, kOut = 4 * D * (KB > VB ? KB : VB);
     // a section's pieces, and the value codes by token (edge_block: all of it)
@@ -481,13 +482,15 @@ __device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
     __shared__ __attribute__((aligned(16))) float cs[PERCH ? 3 : 1][PERCH ? D : 4];  // channel scales, reciprocals, offsets
     constexpr int kSteps = RowStage<D>::kSteps;
 
+    const int unit = blockIdx.y;
+    const int b = unit / p.H, h = unit % p.H;
+    const int tb = (p.q0 / kBlockTok + (int)blockIdx.x) * kBlockTok;
     if constexpr (!PERCH) {
         if (tb < p.q0 || tb + kBlockTok > p.q1) {
             edge_block<D>(p, unit, tb, pool);
             return;
         }
     }
-    const int b = unit / p.H, h = unit % p.H;
     const int msz = p.meta16 ? 2 : 4;
     const size_t blk = (size_t)unit * (size_t)(p.T / kBlockTok) + (size_t)(tb / kBlockTok);
     RowStage<D> kst, vst;
@@ -503,7 +506,7 @@ __device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
         for (int k = 0; k < kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8;
             float x[8], s, z;
-            kst.widen(p, tb, k, x, RowStage<D>::angles(p, b, tb, k));
+            kst.widen(p, tb, k, x, NoAngles());
             piece_group_stats(x, lanes, p.k_mode, KB, &s, &z);
             round_meta(p.meta16, &s, &z);
             if (P % lanes == 0) {
@@ -520,7 +523,7 @@ __device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
         float x[kSteps][8], mn[8], mx[8];
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
-            kst.widen(p, tb, k, x[k], RowStage<D>::angles(p, b, tb, k));
+            kst.widen(p, tb, k, x[k], NoAngles());
         const bool aff = p.k_mode == KVQ_AFFINE;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -636,12 +639,6 @@ __device__ __forceinline__ void code_block(const Params& p, int unit, int tb)
         copy_out((const uint8_t*)mb[1], (uint8_t*)p.vz + blk * (size_t)(vmeta * msz), vmeta * msz);
 }
 
-#ifndef KVQ_APPEND_ROPE
-template <int D, bool PERCH, int KB, int VB>
-__global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
-{
-    code_block<D, PERCH, KB, VB>(p, blockIdx.y, (p.q0 / kBlockTok + (int)blockIdx.x) * kBlockTok);
-}
 #endif
 
 // One decoded token per (sequence, KV head) without a window: a workgroup of
@@ -928,28 +925,39 @@ struct Coder {
             d = reduce(ma, lanes, most);
             *z = 0.0f;
         }
-        const float q = d * inv;
-        *s = fmaxf(__builtin_fmaf(__builtin_fmaf(-q, n, d), inv, q), 1e-8f);
+        *s = over_n(d);
         round_meta(meta16, s, z);
     }
 
-    // (kNear: as in piece_codes)
+    __device__ __forceinline__ float over_n(float d) const
+    {
+        const float q = d * inv;
+        return fmaxf(__builtin_fmaf(__builtin_fmaf(-q, n, d), inv, q), 1e-8f);
+    }
+
     __device__ __forceinline__ uint64_t piece(const float* x, float s, float z) const
+    {
+        const float r = __builtin_amdgcn_rcpf(s);
+        return piece(x, [&](int) { return s; }, [&](int) { return r; }, [&](int) { return z; });
+    }
+
+    // Element e's scale, its reciprocal and its offset.  (kNear: as in piece_codes)
+    template <typename S, typename R, typename Z>
+    __device__ __forceinline__ uint64_t piece(const float* x, S s, R r, Z z) const
     {
 #pragma clang fp contract(off)
         constexpr float kNear = BITS == 8 ? 0x1p-12f : BITS == 4 ? 0x1p-16f : 0x1p-18f;
-        const float r = __builtin_amdgcn_rcpf(s);
         float c[8], worst = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float q = (x[e] - z) * r;
+            const float q = (x[e] - z(e)) * r(e);
             c[e] = __builtin_rintf(q);
             worst = fmaxf(worst, fabsf(q - c[e]));
         }
         if (worst >= 0.5f - kNear) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                c[e] = __builtin_rintf((x[e] - z) / s);
+                c[e] = __builtin_rintf((x[e] - z(e)) / s(e));
         }
         constexpr int N = 16 / BITS;  // codes per 16 bits
         uint64_t word = 0;
@@ -1088,28 +1096,198 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
     }
 }
 
+// Block tb of one sequence's heads h0 .. with per-channel keys: a thread owns eight
+// channels of D / 64 tokens.  The angles of the block's tokens are computed once, for
+// all heads, and kept in LDS (ANGLES: 16 KiB at D = 128; at 256 they would leave one
+// workgroup per CU, so a workgroup takes one head and computes its own); 16-byte
+// pieces of them are swapped by row and lane so that 16 lanes hit 16 different ones.
+template <int D, int KB, int VB>
+__device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, int h0, int heads, int tb)
+{
+    constexpr int PPT = D / 8, kSteps = RowStage<D>::kSteps;
+    constexpr bool kAngles = D <= 128;
+    __shared__ __attribute__((aligned(16))) uint8_t kbuf[4 * D * KB], vbuf[4 * D * VB];
+    __shared__ __attribute__((aligned(16))) float meta[2][kBlockTok * 8];  // value scales, offsets: [groups][32]
+    __shared__ __attribute__((aligned(16))) float red[2][4][D], cs[3][D];  // extremes by wave; scales, reciprocals, offsets
+    __shared__ __attribute__((aligned(16))) float4 angles[kAngles ? kBlockTok : 1][kAngles ? D / 4 : 1];
+    const int tid = threadIdx.x, P = tid % PPT, lane = tid & 63, wave = tid >> 6;
+    const Coder<KB, false> kcode(p.k_mode);
+    const Coder<VB, false> vcode(p.v_mode);
+    const int vlanes = p.v_group / 8, ng = D / p.v_group;
+    const auto fresh = [&](int k) { return tb + RowStage<D>::row(k) >= p.n0; };  // (all lanes of a row or none)
+    RowStage<D> kst, vst;
+    kst.load(p, 0, b, h0, tb);
+    vst.load(p, 1, b, h0, tb);
+    // where row i's angles of pairs 8 u + 2 j, 8 u + 2 j + 1 are
+    const auto place = [&](int i, int u, int j) { return 4 * u + (j ^ ((u + i) & 3)); };
+    if constexpr (kAngles) {
+        for (int x = tid; x < kBlockTok * (D / 4); x += kThreads) {
+            const int i = x / (D / 4), c = x % (D / 4);  // pairs 2 c, 2 c + 1
+            const int t = tb + i;
+            if (t < p.n0 || 4 * c >= p.rope.rot)
+                continue;
+            const int at = input_position(p, b, t - p.n0);
+            const float2 a = rope_cos_sin(at, p.rope.turns[2 * c], p.rope.scale);
+            const float2 d = rope_cos_sin(at, p.rope.turns[2 * c + 1], p.rope.scale);
+            angles[i][place(i, c >> 2, c & 3)] = make_float4(a.x, a.y, d.x, d.y);
+        }
+        __syncthreads();
+    }
+    const auto angles_of = [&](int k) {
+        if constexpr (kAngles) {
+            const int i = RowStage<D>::row(k), hp = p.rope.rot / 16;
+            const bool half = p.rope.layout == KVQ_ROPE_HALF, up = half && P >= hp;
+            Angles a;
+            if (8 * P < p.rope.rot) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (half) {
+                        const float4 x = angles[i][place(i, up ? P - hp : P, j)];
+                        a.c[2 * j] = x.x, a.c[2 * j + 1] = x.z;
+                        a.s[2 * j] = up ? x.y : -x.y, a.s[2 * j + 1] = up ? x.w : -x.w;
+                    } else if (j < 2) {
+                        const float4 x = angles[i][place(i, P >> 1, 2 * (P & 1) + j)];
+                        a.c[2 * j] = x.x, a.c[2 * j + 1] = x.z;
+                        a.s[2 * j] = x.y, a.s[2 * j + 1] = x.w;
+                    }
+                }
+            }
+            return a;
+        } else {
+            return RowStage<D>::angles(p, b, tb, k);
+        }
+    };
+    for (int h = h0; h < h0 + heads; ++h) {
+        const size_t blk = (size_t)(b * p.H + h) * (size_t)(p.T / kBlockTok) + (size_t)(tb / kBlockTok);
+        float x[kSteps][8], mn[8], mx[8];
+        asm volatile("" ::: "memory");  // (angles are read again for every head, not kept in 16 registers a row)
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+            kst.widen(p, tb, k, x[k], fresh(k) ? angles_of(k) : Angles());
+        if (h + 1 < h0 + heads)
+            kst.load(p, 0, b, h + 1, tb);
+        const bool aff = kcode.affine;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            mn[e] = x[0][e];
+            mx[e] = aff ? x[0][e] : fabsf(x[0][e]);
+#pragma unroll
+            for (int k = 1; k < kSteps; ++k) {
+                mn[e] = fminf(mn[e], x[k][e]);
+                mx[e] = fmaxf(mx[e], aff ? x[k][e] : fabsf(x[k][e]));
+            }
+            if constexpr (PPT <= 8) {
+                mn[e] = fminf(mn[e], row_ror8(mn[e]));
+                mx[e] = fmaxf(mx[e], row_ror8(mx[e]));
+            }
+#pragma unroll
+            for (int off = PPT < 16 ? 16 : PPT; off < 64; off <<= 1) {
+                mn[e] = fminf(mn[e], __shfl_xor(mn[e], off));
+                mx[e] = fmaxf(mx[e], __shfl_xor(mx[e], off));
+            }
+        }
+        if (lane < PPT) {
+            *(float4*)&red[0][wave][8 * P] = make_float4(mn[0], mn[1], mn[2], mn[3]);
+            *(float4*)&red[0][wave][8 * P + 4] = make_float4(mn[4], mn[5], mn[6], mn[7]);
+            *(float4*)&red[1][wave][8 * P] = make_float4(mx[0], mx[1], mx[2], mx[3]);
+            *(float4*)&red[1][wave][8 * P + 4] = make_float4(mx[4], mx[5], mx[6], mx[7]);
+        }
+        __syncthreads();
+        if (tid < D) {
+            const float lo = fminf(fminf(red[0][0][tid], red[0][1][tid]), fminf(red[0][2][tid], red[0][3][tid]));
+            const float hi = fmaxf(fmaxf(red[1][0][tid], red[1][1][tid]), fmaxf(red[1][2][tid], red[1][3][tid]));
+            float s = kcode.over_n(aff ? hi - lo : hi), z = aff ? lo + 0.0f : 0.0f;
+            round_meta(p.meta16, &s, &z);
+            cs[0][tid] = s;
+            cs[1][tid] = __builtin_amdgcn_rcpf(s);
+            cs[2][tid] = z;
+            store_meta(p.ks, blk * D + tid, s, p.meta16);
+            if (aff)
+                store_meta(p.kz, blk * D + tid, z, p.meta16);
+        }
+        __syncthreads();
+        float s8[8], r8[8], z8[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            *(float4*)(s8 + e) = *(const float4*)&cs[0][8 * P + e];
+            *(float4*)(r8 + e) = *(const float4*)&cs[1][8 * P + e];
+            *(float4*)(z8 + e) = *(const float4*)&cs[2][8 * P + e];
+        }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+            store_piece(kbuf, key_piece<D>(0, RowStage<D>::row(k), P), KB,
+                        kcode.piece(x[k], [&](int e) { return s8[e]; }, [&](int e) { return r8[e]; }, [&](int e) { return z8[e]; }));
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int i = RowStage<D>::row(k);
+            float v[8], s, z;
+            vst.widen(p, tb, k, v, NoAngles());
+            vcode.scale(v, vlanes, p.meta16, &s, &z);
+            if (P % vlanes == 0) {
+                meta[0][P / vlanes * kBlockTok + i] = s;
+                meta[1][P / vlanes * kBlockTok + i] = z;
+            }
+            store_piece(vbuf, i * PPT + P, VB, vcode.piece(v, s, z));
+        }
+        if (h + 1 < h0 + heads)
+            vst.load(p, 1, b, h + 1, tb);
+        // (what the next head writes before its second barrier, nobody reads behind this one)
+        __syncthreads();
+        for (int at = 16 * tid; at < 4 * D * KB; at += 16 * kThreads)
+            *(u32x4*)((uint8_t*)p.kc + blk * (size_t)(4 * D * KB) + at) = *(const u32x4*)(kbuf + at);
+#pragma unroll
+        for (int x0 = 0; x0 < 4 * D; x0 += kThreads) {  // value piece x: octet, channel
+            const int at = x0 + tid, d = 16 * (at % (D / 16)) + at / (D / 16) % 16, first = 8 * (at / D) * PPT + d / 8;
+            uint64_t word = 0;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint64_t w = load_piece(vbuf, first + q * PPT, VB);
+                if constexpr (VB == 8)
+                    word |= (w >> (8 * (d & 7)) & 0xFFu) << (8 * q);
+                else
+                    word |= (uint32_t)((uint32_t)w >> (VB * (d & 7)) & ((1u << VB) - 1u)) << (VB * q);
+            }
+            store_piece(p.vc, blk * (size_t)(4 * D) + at, VB, word);
+        }
+        for (int at = tid; at < ng * kBlockTok; at += kThreads) {
+            store_meta(p.vs, blk * (size_t)(ng * kBlockTok) + at, meta[0][at], p.meta16);
+            if (vcode.affine)
+                store_meta(p.vz, blk * (size_t)(ng * kBlockTok) + at, meta[1][at], p.meta16);
+        }
+    }
+}
+
 // One launch for all that an append with positions does: workgroups that code
 // blocks, the longest, come first, then those that write window rows and those that
 // rotate queries (four waves of rope_rows).
 constexpr int kQueryIter = 4;  // iterations of a wave
 
+// Waves per SIMD that the registers are held to.
+__host__ __device__ constexpr int append_waves(int D, bool perch)
+{
+    return !perch ? 5 : D == 256 ? 2 : D == 128 ? 3 : 4;
+}
+
 template <int D, bool PERCH, int KB, int VB, bool PLAIN>
-__global__ __launch_bounds__(kThreads) void append_rope_kernel(AppendRopeParams p)
+__global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_kernel(AppendRopeParams p)
 {
     uint32_t x = blockIdx.x;
     if (x < p.code_wgs) {
-        const uint32_t units = p.B * p.H, singles = units * p.edges;  // blocks of one head
-        if (x < singles) {
+        const uint32_t units = p.B * p.H, singles = units * p.edges;  // blocks at the ends, by head
+        if (!PERCH && x < singles) {
+            __shared__ __attribute__((aligned(16))) uint8_t vcode[32 * D];
             const int e = (int)(x / units), unit = (int)(x - e * units);
-            const int blk = PERCH ? p.q0 / kBlockTok + e : e == 0 && p.q0 % kBlockTok ? p.q0 / kBlockTok : p.q1 / kBlockTok;
-            code_block<D, PERCH, KB, VB>(p, unit, kBlockTok * blk);
-        } else if constexpr (!PERCH) {
-            constexpr int T = 2048 / D, PARTS = kBlockTok / T;
+            edge_block<D>(p, unit, kBlockTok * (e == 0 && p.q0 % kBlockTok ? p.q0 / kBlockTok : p.q1 / kBlockTok), vcode);
+        } else {
+            constexpr int T = PERCH ? kBlockTok : 2048 / D, PARTS = kBlockTok / T;
             x -= singles;
             const uint32_t hg = (p.H + p.heads - 1) / p.heads, y = x / hg, h0 = (x - y * hg) * p.heads;
             const uint32_t b = y / (p.blocks * PARTS), part = y - b * (p.blocks * PARTS);
-            code_heads<D, KB, VB, PLAIN>(p, (int)b, (int)h0, min(p.heads, p.H - (int)h0),
-                                         (p.q0 + kBlockTok - 1) / kBlockTok * kBlockTok + (int)part * T);
+            const int heads = min(p.heads, p.H - (int)h0), t0 = (p.q0 + kBlockTok - 1) / kBlockTok * kBlockTok + (int)part * T;
+            if constexpr (PERCH)
+                code_channels<D, KB, VB>(p, (int)b, (int)h0, heads, t0);
+            else
+                code_heads<D, KB, VB, PLAIN>(p, (int)b, (int)h0, heads, t0);
         }
         return;
     }
@@ -1150,14 +1328,14 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
         launch_kernel((append_token_kernel<D, AppendRopeParams>), dim3(units + p.queries.tokens * p.queries.H_q), dim3(D), 0, stream, p);
         return hipGetLastError();
     }
-    // whole blocks by code_heads, those at the ends (and per-channel keys) by code_block
+    // whole blocks by code_heads or code_channels, those at the ends by edge_block
     const int lo = (p.q0 + kBlockTok - 1) / kBlockTok, hi = p.q1 / kBlockTok;
-    const bool perch = p.k_axis == KVQ_PER_CHANNEL;
-    p.blocks = perch || hi < lo ? 0 : hi - lo;
-    p.edges = perch ? hi - lo : p.q1 <= p.q0 ? 0 : hi < lo ? 1 : (p.q0 % kBlockTok != 0) + (p.q1 % kBlockTok != 0);
-    const long long parts = (long long)p.blocks * p.B * (kBlockTok * D / 2048);
+    const bool perch = p.k_axis == KVQ_PER_CHANNEL;  // (whole blocks only)
+    p.blocks = hi < lo ? 0 : hi - lo;
+    p.edges = p.q1 <= p.q0 || perch ? 0 : hi < lo ? 1 : (p.q0 % kBlockTok != 0) + (p.q1 % kBlockTok != 0);
+    const long long parts = (long long)p.blocks * p.B * (perch ? 1 : kBlockTok * D / 2048);
     p.heads = 1;
-    while (p.heads < 4 && p.heads < p.H && parts * p.H > 4096 * p.heads)
+    while (p.heads < (perch && D == 256 ? 1 : 4) && p.heads < p.H && parts * p.H > (perch ? 1024 : 4096) * p.heads)
         p.heads *= 2;
     p.code_wgs = (uint32_t)(parts * ((p.H + p.heads - 1) / p.heads)) + (uint32_t)(p.edges * units);
     // the window's rows beside the coder, if none takes the slot of a token that is coded from it

@@ -290,3 +290,29 @@ def test_a_refused_append_changes_nothing():
         c.append_rope(kvq.Rope(D), dev_bf16(K[:, :11]), dev_bf16(V[:, :11]), Q=q, Qo=out)
     assert e.value.status == kvq.ERR_CAPACITY
     assert c.n == 30 and np.array_equal(image(c), before) and not out.any()
+
+
+@pytest.mark.parametrize("name,B,H,n", [("kivi", 8, 9, 1000), ("gqa12b", 8, 9, 1000), ("tiny_b16", 8, 17, 2030),
+                                        ("hadamard", 8, 17, 1000), ("had_affine_window", 8, 9, 1001),
+                                        ("sym4_window", 8, 17, 2100), ("affine8", 8, 17, 2030), ("kivi", 1, 1, 1000)])
+@pytest.mark.parametrize("norm", [0, 1])
+def test_append_several_heads_of_a_workgroup(name, B, H, n, norm):
+    # calls so large that a workgroup codes several heads, the last ones fewer: the bytes of the two calls
+    from paper_2609_04263_amd import kvq
+    fmt, D = CASES[name]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(50)
+    K, V, Q = (torch.randn((B, n, h, D), generator=g, device="cuda").to(torch.bfloat16) for h in (H, H, 2 * H))
+    w = dev_bf16(weights(50, "k", D)) if norm else None
+    rope = kvq.Rope(D if norm else D // 2, 500000.0)
+    one, two = (kvq.Cache(fmt, B, H, D, n + 40) for _ in range(2))
+    for lo, hi in ((0, 37), (37, n)):
+        k, v, q = (x[:, lo:hi].contiguous() for x in (K, V, Q))
+        kw = dict(k_norm=w, q_norm=w, pos0=lo)
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        kk = torch.empty_like(k)
+        rope.qk(q, k, a, kk, **kw)
+        two.append(kk, v)
+        one.append_rope(rope, k, v, Q=q, Qo=b, **kw)
+        assert torch.equal(a, b)
+    assert torch.equal(one.storage, two.storage)
