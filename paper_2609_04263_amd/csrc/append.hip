@@ -308,6 +308,7 @@ __device__ __forceinline__ void copy_out(const uint8_t* src, uint8_t* dst, int b
         *(u32x4*)(dst + off) = *(const u32x4*)(src + off);
 }
 
+#ifndef KVQ_APPEND_ROPE
 // A block shared with earlier or later calls (per-token groups: a block of
 // per-channel keys is one whole group), written piece by piece: value pieces
 // keep the bits of tokens appended earlier.  vcode: 32 D bytes of LDS for the
@@ -448,6 +449,8 @@ __device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, 
     }
     return word;
 }
+
+#endif
 
 // The value of lane l ^ 8 (a rotation by half a 16-lane row).
 __device__ __forceinline__ float row_ror8(float v)
@@ -1096,6 +1099,69 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
     }
 }
 
+// The part of block tb that this call codes, tokens lo .. hi - 1 of one head (per-token
+// groups; never of a window, which is coded by whole blocks).  Value pieces keep the
+// bits of tokens appended earlier and clear later ones; those of the first octet are
+// loaded first, with the rows.  Bound by latency: five tokens of 128 heads took 11.0 us
+// as edge_block, which takes all 32 rows and loads old pieces when it needs them.
+template <int D, int KB, int VB, bool PLAIN>
+__device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, int tb)
+{
+    constexpr int PPT = D / 8, T = kThreads / PPT;
+    __shared__ __attribute__((aligned(16))) uint8_t words[4 * D * VB];  // [token][PPT]
+    const int tid = threadIdx.x, P = tid % PPT, b = unit / p.H, h = unit % p.H;
+    const int lo = max(p.q0, tb), hi = min(p.q1, tb + kBlockTok), o0 = (lo - tb) >> 3, o1 = (hi - 1 - tb) >> 3;
+    const size_t blk = (size_t)unit * (size_t)(p.T / kBlockTok) + (size_t)(tb / kBlockTok);
+    uint64_t old = 0;
+    if ((lo & 7) && tid < D)
+        old = load_piece(p.vc, value_piece<D>(blk, o0, tid), VB) & low_codes(VB, lo & 7);
+    const Coder<KB, PLAIN> kcode(p.k_mode);
+    const Coder<VB, PLAIN> vcode(p.v_mode);
+    const int klanes = p.k_group / 8, vlanes = p.v_group / 8;
+    for (int t = lo + tid / PPT; t < hi; t += T) {  // (all lanes of a row or none)
+        const int i = t - tb;
+        const size_t at = (input_row(p, b, t - p.n0) * p.H + h) * D + 8 * P;
+        const u32x4 kw = *(const u32x4*)(p.kin + at), vw = *(const u32x4*)(p.vin + at);
+        float x[8], s, z;
+        const Angles turn(p.rope, input_position(p, b, t - p.n0), P);
+        widen8(kw, x);
+        turn.template turn<D>(p.rope, P, x);
+        if (!PLAIN && p.rotate)
+            rotate8<D>(x, P, p.rot_c);
+        kcode.scale(x, klanes, p.meta16, &s, &z);
+        if (P % klanes == 0) {
+            const size_t mi = (blk * (D / p.k_group) + P / klanes) * kBlockTok + i;
+            store_meta(p.ks, mi, s, p.meta16);
+            if (kcode.affine)
+                store_meta(p.kz, mi, z, p.meta16);
+        }
+        store_piece(p.kc, key_piece<D>(blk, i, P), KB, kcode.piece(x, s, z));
+        widen8(vw, x);
+        if (!PLAIN && p.rotate)
+            rotate8<D>(x, P, p.rot_c);
+        vcode.scale(x, vlanes, p.meta16, &s, &z);
+        if (P % vlanes == 0) {
+            const size_t mi = (blk * (D / p.v_group) + P / vlanes) * kBlockTok + i;
+            store_meta(p.vs, mi, s, p.meta16);
+            if (vcode.affine)
+                store_meta(p.vz, mi, z, p.meta16);
+        }
+        store_piece(words, i * PPT + P, VB, vcode.piece(x, s, z));
+    }
+    __syncthreads();
+    for (int idx = tid; idx < (o1 - o0 + 1) * D; idx += kThreads) {
+        const int o = o0 + idx / D, d = idx % D;
+        uint64_t word = idx < D ? old : 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int t = tb + 8 * o + q;
+            const uint64_t c = load_piece(words, (8 * o + q) * PPT + d / 8, VB) >> (VB * (d & 7)) & ((1u << VB) - 1u);
+            word |= t >= lo && t < hi ? c << (VB * q) : 0;
+        }
+        store_piece(p.vc, value_piece<D>(blk, o, d), VB, word);
+    }
+}
+
 // Block tb of one sequence's heads h0 .. with per-channel keys: a thread owns eight
 // channels of D / 64 tokens.  The angles of the block's tokens are computed once, for
 // all heads, and kept in LDS (ANGLES: 16 KiB at D = 128; at 256 they would leave one
@@ -1275,9 +1341,8 @@ __global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_
     if (x < p.code_wgs) {
         const uint32_t units = p.B * p.H, singles = units * p.edges;  // blocks at the ends, by head
         if (!PERCH && x < singles) {
-            __shared__ __attribute__((aligned(16))) uint8_t vcode[32 * D];
             const int e = (int)(x / units), unit = (int)(x - e * units);
-            edge_block<D>(p, unit, kBlockTok * (e == 0 && p.q0 % kBlockTok ? p.q0 / kBlockTok : p.q1 / kBlockTok), vcode);
+            code_edge<D, KB, VB, PLAIN>(p, unit, kBlockTok * (e == 0 && p.q0 % kBlockTok ? p.q0 / kBlockTok : p.q1 / kBlockTok));
         } else {
             constexpr int T = PERCH ? kBlockTok : 2048 / D, PARTS = kBlockTok / T;
             x -= singles;
@@ -1328,7 +1393,7 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
         launch_kernel((append_token_kernel<D, AppendRopeParams>), dim3(units + p.queries.tokens * p.queries.H_q), dim3(D), 0, stream, p);
         return hipGetLastError();
     }
-    // whole blocks by code_heads or code_channels, those at the ends by edge_block
+    // whole blocks by code_heads or code_channels, those at the ends by code_edge
     const int lo = (p.q0 + kBlockTok - 1) / kBlockTok, hi = p.q1 / kBlockTok;
     const bool perch = p.k_axis == KVQ_PER_CHANNEL;  // (whole blocks only)
     p.blocks = hi < lo ? 0 : hi - lo;
