@@ -105,6 +105,9 @@ EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_sect
             "kvq_prefill_attn_shared", "kvq_tree_attn_shared", "kvq_time_launches")
 
 
+_rope_qk, _append_rope = _lib.kvq_rope_qk, _lib.kvq_append_rope
+
+
 def lib() -> C.CDLL:
     return _lib
 
@@ -175,9 +178,10 @@ class Rope:
                  factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0, scale=None,
                  eps: float = 1e-6, turns=None):
         self.c = _Rope()
+        self._ref = C.byref(self.c)
         if scaling not in ROPE_SCALINGS:
             raise ValueError(f"scaling: one of {', '.join(ROPE_SCALINGS)} expected")
-        _check(_lib.kvq_rope_init(C.byref(self.c), rot, int(bool(interleaved)), base, ROPE_SCALINGS.index(scaling),
+        _check(_lib.kvq_rope_init(self._ref, rot, int(bool(interleaved)), base, ROPE_SCALINGS.index(scaling),
                                   factor, original, low, high), "rope_init")
         if turns is not None:
             if len(turns) != rot // 2:
@@ -191,15 +195,24 @@ class Rope:
         """Qo, Ko (Q and K themselves where not given) <- bf16 Q [B, n, H_q, D] and K [B, n, H_kv, D] (either may be
         None), normed by bf16 weights [D] where given and rotated to positions pos (device int32 [B, n], or None for
         pos0, pos0 + 1, ..)."""
-        x = K if Q is None else Q
-        B, n, _, D = x.shape
-        if Q is not None and K is not None and K.shape[:2] + K.shape[3:] != (B, n, D):
-            raise ValueError("Q and K are of different tokens or head sizes")
-        _positions(pos, B * n, "pos")
-        Qo, Ko = Q if Qo is None else Qo, K if Ko is None else Ko
-        st = _lib.kvq_rope_qk(C.byref(self.c), _ptr(Q), _ptr(K), B, n, 0 if Q is None else Q.shape[2],
-                              0 if K is None else K.shape[2], D, _ptr(q_norm), _ptr(k_norm), _ptr(pos), pos0,
-                              _ptr(Qo), _ptr(Ko), _stream(stream))
+        q = k = qo = ko = None
+        H_q = H = 0
+        if Q is not None:
+            B, n, H_q, D = Q.shape
+            q = Q.data_ptr()
+            qo = q if Qo is None else Qo.data_ptr()
+        if K is not None:
+            b, m, H, d = K.shape
+            if Q is not None and (b != B or m != n or d != D):
+                raise ValueError("Q and K are of different tokens or head sizes")
+            B, n, D = b, m, d
+            k = K.data_ptr()
+            ko = k if Ko is None else Ko.data_ptr()
+        if pos is not None:
+            _positions(pos, B * n, "pos")
+            pos = pos.data_ptr()
+        st = _rope_qk(self._ref, q, k, B, n, H_q, H, D, q_norm if q_norm is None else q_norm.data_ptr(),
+                      k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0, qo, ko, _stream(stream))
         if st:
             _check(st, "rope_qk")
 
@@ -277,12 +290,18 @@ class Cache:
         n_in = K.shape[1]
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
-        _positions(rows, self.B * n_new, "rows")
-        _positions(pos, self.B * n_new, "pos")
+        if rows is not None:
+            _positions(rows, self.B * n_new, "rows")
+            rows = rows.data_ptr()
+        if pos is not None:
+            _positions(pos, self.B * n_new, "pos")
+            pos = pos.data_ptr()
         f = self._fmt_ref if fmt is None else C.byref(Format.of(fmt))
-        st = _lib.kvq_append_rope(self.handle, C.byref(rope.c), K.data_ptr(), V.data_ptr(), n_in, _ptr(rows), n_new,
-                                  _ptr(Q), 0 if Q is None else Q.shape[-2], _ptr(q_norm), _ptr(k_norm), _ptr(pos),
-                                  pos0, _ptr(Qo), f, _stream(stream))
+        q, H_q = (None, 0) if Q is None else (Q.data_ptr(), Q.shape[-2])
+        st = _append_rope(self.handle, rope._ref, K.data_ptr(), V.data_ptr(), n_in, rows, n_new, q, H_q,
+                          q_norm if q_norm is None else q_norm.data_ptr(),
+                          k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0,
+                          Qo if Qo is None else Qo.data_ptr(), f, _stream(stream))
         if st:
             _check(st, "append_rope")
 
