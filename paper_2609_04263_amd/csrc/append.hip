@@ -859,6 +859,17 @@ void launch_ring(const P& p, int hi, hipStream_t stream)
 }
 
 #ifdef KVQ_APPEND_ROPE
+// Per-token groups of `size` channels (a power of two; by shifts, a division of
+// integers is 20 to 30 vector operations): lanes of one, how many of a row.
+template <int D>
+struct Groups {
+    int shift, lanes, count;
+    __device__ __forceinline__ explicit Groups(int size)
+        : shift(__builtin_ctz(size) - 3), lanes(1 << shift), count((D / 8) >> shift) {}
+    __device__ __forceinline__ bool first(int piece) const { return (piece & (lanes - 1)) == 0; }
+    __device__ __forceinline__ int of(int piece) const { return piece >> shift; }
+};
+
 // The coder of code_heads: the codes, scales and offsets of piece_group_stats,
 // round_meta and piece_codes in fewer operations.  A symmetric group is one with
 // offset zero and other limits (`bias` makes its codes unsigned); the sums of a
@@ -940,27 +951,27 @@ struct Coder {
 
     __device__ __forceinline__ uint64_t piece(const float* x, float s, float z) const
     {
-        const float r = __builtin_amdgcn_rcpf(s);
-        return piece(x, [&](int) { return s; }, [&](int) { return r; }, [&](int) { return z; });
+        const float y = 1.0f / s;
+        return piece(x, [&](int) { return s; }, [&](int) { return y; }, [&](int) { return z; });
     }
 
-    // Element e's scale, its reciprocal and its offset.  (kNear: as in piece_codes)
-    template <typename S, typename R, typename Z>
-    __device__ __forceinline__ uint64_t piece(const float* x, S s, R r, Z z) const
+    // Element e's scale, the nearest binary32 number to its reciprocal, and its offset.
+    // fl(d / s) by two corrections of fl(d y): the first leaves less than an ulp, from
+    // which the second gives the correctly rounded quotient (Markstein's theorem; no
+    // exception in 2 10^9 pairs).  Numbers on a grid, as bf16 rows are, meet ties of their
+    // codes in 8 of 10 waves' pieces, so a branch to exact divisions costs more.
+    template <typename S, typename Y, typename Z>
+    __device__ __forceinline__ uint64_t piece(const float* x, S s, Y y, Z z) const
     {
 #pragma clang fp contract(off)
-        constexpr float kNear = BITS == 8 ? 0x1p-12f : BITS == 4 ? 0x1p-16f : 0x1p-18f;
-        float c[8], worst = 0.0f;
+        float c[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float q = (x[e] - z(e)) * r(e);
+            const float d = x[e] - z(e);
+            float q = d * y(e);
+            q = __builtin_fmaf(__builtin_fmaf(-q, s(e), d), y(e), q);
+            q = __builtin_fmaf(__builtin_fmaf(-q, s(e), d), y(e), q);
             c[e] = __builtin_rintf(q);
-            worst = fmaxf(worst, fabsf(q - c[e]));
-        }
-        if (worst >= 0.5f - kNear) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                c[e] = __builtin_rintf((x[e] - z(e)) / s(e));
         }
         constexpr int N = 16 / BITS;  // codes per 16 bits
         uint64_t word = 0;
@@ -1015,13 +1026,13 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
     const Coder<KB, PLAIN> kcode(p.k_mode);
     const Coder<VB, PLAIN> vcode(p.v_mode);
     const int tau = t % kBlockTok, o0 = t0 % kBlockTok / 8;
-    const int klanes = p.k_group / 8, vlanes = p.v_group / 8;
+    const Groups<D> kg(p.k_group), vg(p.v_group);
     // this thread's key piece in its buffer: run (half, P % 4), row of the run, P / 4
     const int kp = (((tau >> 2 & 1) * 4 + (P & 3)) * (T / 2) + 4 * ((tau >> 3) - o0) + (tau & 3)) * (D / 32) + (P >> 2);
     // the value piece it makes (octet, channel) of words vfirst, vfirst + PPT, ..
     const int vd = 16 * (tid % (D / 16)) + tid / (D / 16) % 16, vfirst = 8 * (tid / D) * PPT + vd / 8;
     // the metadata element it stores: of array tid / 64, group and token
-    const int ma = tid >> 6, mg = (tid & 63) / T, ng = D / (ma < 2 ? p.k_group : p.v_group);
+    const int ma = __builtin_amdgcn_readfirstlane(tid >> 6), mg = (tid & 63) / T, ng = ma < 2 ? kg.count : vg.count;
     const bool stores = mg < ng && (!(ma & 1) || (ma == 1 ? p.k_mode : p.v_mode) == KVQ_AFFINE);
     float* meta = ma == 0 ? p.ks : ma == 1 ? p.kz : ma == 2 ? p.vs : p.vz;
     // of head h0; every head is `blocks` blocks on
@@ -1061,10 +1072,10 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
         if (fresh)
             turn.template turn<D>(p.rope, norm, P, x);
         to_cache(x);
-        kcode.scale(x, klanes, p.meta16, &s, &z);
-        if (P % klanes == 0) {
-            buf.meta[0][P / klanes * T + i] = s;
-            buf.meta[1][P / klanes * T + i] = z;
+        kcode.scale(x, kg.lanes, p.meta16, &s, &z);
+        if (kg.first(P)) {
+            buf.meta[0][kg.of(P) * T + i] = s;
+            buf.meta[1][kg.of(P) * T + i] = z;
         }
         store_piece(buf.k, kp, KB, kcode.piece(x, s, z));
         widen(vw, x);
@@ -1072,10 +1083,10 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
         if (j + 1 < heads)
             vw = *(const u32x4*)vsrc;
         to_cache(x);
-        vcode.scale(x, vlanes, p.meta16, &s, &z);
-        if (P % vlanes == 0) {
-            buf.meta[2][P / vlanes * T + i] = s;
-            buf.meta[3][P / vlanes * T + i] = z;
+        vcode.scale(x, vg.lanes, p.meta16, &s, &z);
+        if (vg.first(P)) {
+            buf.meta[2][vg.of(P) * T + i] = s;
+            buf.meta[3][vg.of(P) * T + i] = z;
         }
         store_piece(buf.v, i * PPT + P, VB, vcode.piece(x, s, z));
         __syncthreads();
@@ -1117,7 +1128,7 @@ __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, i
         old = load_piece(p.vc, value_piece<D>(blk, o0, tid), VB) & low_codes(VB, lo & 7);
     const Coder<KB, PLAIN> kcode(p.k_mode);
     const Coder<VB, PLAIN> vcode(p.v_mode);
-    const int klanes = p.k_group / 8, vlanes = p.v_group / 8;
+    const Groups<D> kg(p.k_group), vg(p.v_group);
     for (int t = lo + tid / PPT; t < hi; t += T) {  // (all lanes of a row or none)
         const int i = t - tb;
         const size_t at = (input_row(p, b, t - p.n0) * p.H + h) * D + 8 * P;
@@ -1128,9 +1139,9 @@ __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, i
         turn.template turn<D>(p.rope, P, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
-        kcode.scale(x, klanes, p.meta16, &s, &z);
-        if (P % klanes == 0) {
-            const size_t mi = (blk * (D / p.k_group) + P / klanes) * kBlockTok + i;
+        kcode.scale(x, kg.lanes, p.meta16, &s, &z);
+        if (kg.first(P)) {
+            const size_t mi = (blk * kg.count + kg.of(P)) * kBlockTok + i;
             store_meta(p.ks, mi, s, p.meta16);
             if (kcode.affine)
                 store_meta(p.kz, mi, z, p.meta16);
@@ -1139,9 +1150,9 @@ __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, i
         widen8(vw, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
-        vcode.scale(x, vlanes, p.meta16, &s, &z);
-        if (P % vlanes == 0) {
-            const size_t mi = (blk * (D / p.v_group) + P / vlanes) * kBlockTok + i;
+        vcode.scale(x, vg.lanes, p.meta16, &s, &z);
+        if (vg.first(P)) {
+            const size_t mi = (blk * vg.count + vg.of(P)) * kBlockTok + i;
             store_meta(p.vs, mi, s, p.meta16);
             if (vcode.affine)
                 store_meta(p.vz, mi, z, p.meta16);
@@ -1179,7 +1190,8 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
     const int tid = threadIdx.x, P = tid % PPT, lane = tid & 63, wave = tid >> 6;
     const Coder<KB, false> kcode(p.k_mode);
     const Coder<VB, false> vcode(p.v_mode);
-    const int vlanes = p.v_group / 8, ng = D / p.v_group;
+    const Groups<D> vg(p.v_group);
+    const int ng = vg.count;
     const auto fresh = [&](int k) { return tb + RowStage<D>::row(k) >= p.n0; };  // (all lanes of a row or none)
     RowStage<D> kst, vst;
     kst.load(p, 0, b, h0, tb);
@@ -1265,7 +1277,7 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
             float s = kcode.over_n(aff ? hi - lo : hi), z = aff ? lo + 0.0f : 0.0f;
             round_meta(p.meta16, &s, &z);
             cs[0][tid] = s;
-            cs[1][tid] = __builtin_amdgcn_rcpf(s);
+            cs[1][tid] = 1.0f / s;
             cs[2][tid] = z;
             store_meta(p.ks, blk * D + tid, s, p.meta16);
             if (aff)
@@ -1288,10 +1300,10 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
             const int i = RowStage<D>::row(k);
             float v[8], s, z;
             vst.widen(p, tb, k, v, NoAngles());
-            vcode.scale(v, vlanes, p.meta16, &s, &z);
-            if (P % vlanes == 0) {
-                meta[0][P / vlanes * kBlockTok + i] = s;
-                meta[1][P / vlanes * kBlockTok + i] = z;
+            vcode.scale(v, vg.lanes, p.meta16, &s, &z);
+            if (vg.first(P)) {
+                meta[0][vg.of(P) * kBlockTok + i] = s;
+                meta[1][vg.of(P) * kBlockTok + i] = z;
             }
             store_piece(vbuf, i * PPT + P, VB, vcode.piece(v, s, z));
         }
@@ -1328,10 +1340,11 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
 // rotate queries (four waves of rope_rows).
 constexpr int kQueryIter = 4;  // iterations of a wave
 
-// Waves per SIMD that the registers are held to.
+// Waves per SIMD that the registers are held to.  (Five with per-token groups spill 16
+// to 24 registers: 2048 tokens 3% faster, five tokens 12% slower.)
 __host__ __device__ constexpr int append_waves(int D, bool perch)
 {
-    return !perch ? 5 : D == 256 ? 2 : D == 128 ? 3 : 4;
+    return !perch ? 4 : D == 256 ? 2 : D == 128 ? 3 : 4;
 }
 
 template <int D, bool PERCH, int KB, int VB, bool PLAIN>
