@@ -417,7 +417,8 @@ __device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, 
     // The product q is within 2^-22 |d / s| of fl(d / s): 2^-23 of the reciprocal
     // and two roundings.  Below 2^BITS that is 2^(BITS - 22), beyond it both clamp;
     // so the codes can differ only where q is as near to a half-integer.  (Four
-    // times that; 2^-10 at any width sent 6 of 10 waves to the divisions.)
+    // times that.  2048 tokens of 8 x 8 heads of 256, 4 bits: 61 us, 64 with 2^-10 at
+    // any width.)
     constexpr float kNear = BITS == 8 ? 0x1p-12f : BITS == 4 ? 0x1p-16f : 0x1p-18f;
     float c[8], worst = 0.0f;
 #pragma unroll
