@@ -1351,7 +1351,7 @@ __host__ __device__ constexpr int append_waves(int D, bool perch)
 template <int D, bool PERCH, int KB, int VB, bool PLAIN>
 __global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_kernel(AppendRopeParams p)
 {
-    uint32_t x = blockIdx.x;
+    uint32_t x = wg_index();
     if (x < p.code_wgs) {
         const uint32_t units = p.B * p.H, singles = units * p.edges;  // blocks at the ends, by head
         if (!PERCH && x < singles) {
@@ -1386,7 +1386,7 @@ __global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_
 template <int D, bool PERCH, bool PLAIN>
 void launch_blocks(const AppendRopeParams& p, uint32_t grid, hipStream_t stream)
 {
-    const dim3 g(grid), t(kThreads);
+    const dim3 g = grid_of(grid), t(kThreads);
     if (p.k_bits == 8)
         launch_kernel((append_rope_kernel<D, PERCH, 8, 8, PLAIN>), g, t, 0, stream, p);
     else if (p.k_bits == 4 && p.v_bits == 4)

@@ -41,6 +41,18 @@ inline void launch_kernel(F kernel, dim3 grid, dim3 block, size_t lds, hipStream
         t.start = nullptr;
 }
 
+// `count` workgroups in rows of at most 2^20 (a launch has fewer than 2^32 threads in
+// a dimension); wg_index() of the last row's surplus is count or more.
+inline dim3 grid_of(uint32_t count)
+{
+    constexpr uint32_t kRow = 1u << 20;
+    return count <= kRow ? dim3(count) : dim3(kRow, (count + kRow - 1) / kRow);
+}
+__device__ __forceinline__ uint32_t wg_index()
+{
+    return blockIdx.y * gridDim.x + blockIdx.x;
+}
+
 // Tail tokens (past the sink) at length n.
 int num_tail(const kvq_format& f, int n);
 // Tokens held as codes at length n: the tail count m, or floor(max(0, m -
@@ -282,13 +294,13 @@ struct SharedParams {
     const uint32_t* tree;  // [B][C][ceil(C / 32)]: which of the newest C tokens a query sees, null: causal
     size_t rows;         // B C H_q
     int C, H_q, P;
+    int lim1, causal;    // tail tokens of the suffix that row 0 sees, and whether one of chunk token c sees c more
     int S[2], bps[2];    // ranges of a tile, 32-token blocks per range
     int parts;           // partials of a row: S[0] + S[1], and one of the drafts
     int tiles0, items0;  // prefix tiles, prefix items (tiles0 S[0]); the suffix items come after them
     int items1;          // suffix items, then (a tree's) draft items
     int image_items, direct0, direct_items;  // items of the image kernel, and those of the direct one from direct0
     int draft_items;
-    int lim1, causal;    // tail tokens of the suffix that row 0 sees, and whether one of chunk token c sees c more
     int rotate;
     float rot_c;
     int first[kSharedPrefixes + 1];  // first sequence of each group

@@ -13,7 +13,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeQkParams p, RopeArgs
 {
     __shared__ __attribute__((aligned(16))) float2 lds[kWaves][D / 2];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const uint32_t item = blockIdx.x * kWaves + wave, token = item / (uint32_t)p.parts;
+    const uint32_t item = wg_index() * kWaves + wave, token = item / (uint32_t)p.parts;
     if (token < (uint32_t)p.tokens)  // (waves of a workgroup do not wait for each other)
         rope_rows<D, ITER, true>(p, r, token, (int)(item - token * (uint32_t)p.parts), lds[wave]);
 }
@@ -24,9 +24,9 @@ hipError_t launch_d(RopeQkParams p, const RopeArgs& rope, hipStream_t stream)
     constexpr int RPI = 1024 / D;
     const int iters = (p.H_q + p.H + RPI - 1) / RPI;
     // few tokens: a wave per RPI rows; else up to four iterations of a wave
-    const int iter = p.tokens * iters <= 1024 ? 1 : (iters + (iters + 3) / 4 - 1) / ((iters + 3) / 4);
+    const int iter = (long long)p.tokens * iters <= 1024 ? 1 : (iters + (iters + 3) / 4 - 1) / ((iters + 3) / 4);
     p.parts = (iters + iter - 1) / iter;
-    const dim3 g((unsigned)((p.tokens * p.parts + kWaves - 1) / kWaves)), t(kThreads);
+    const dim3 g = grid_of((uint32_t)(((long long)p.tokens * p.parts + kWaves - 1) / kWaves)), t(kThreads);
     if (iter == 1)
         launch_kernel((rope_kernel<D, 1>), g, t, 0, stream, p, rope);
     else if (iter == 2)

@@ -284,10 +284,11 @@ class Cache:
     def append_rope(self, rope: "Rope", K, V, n_new: int | None = None, rows=None, Q=None, Qo=None, q_norm=None,
                     k_norm=None, pos=None, pos0: int = 0, fmt=None, stream=None) -> None:
         """append of keys that `rope` norms and rotates on the way.  bf16 K, V [B, n_in, H_kv, D]; with rows (device
-        int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default).  Q, Qo
+        int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]:
+        one token).  Q, Qo
         [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32 [B, n_new], or
         None for pos0, pos0 + 1, .."""
-        n_in = K.shape[1]
+        n_in = K.shape[1] if K.dim() == 4 else 1
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
         if rows is not None:

@@ -316,3 +316,29 @@ def test_append_several_heads_of_a_workgroup(name, B, H, n, norm):
         one.append_rope(rope, k, v, Q=q, Qo=b, **kw)
         assert torch.equal(a, b)
     assert torch.equal(one.storage, two.storage)
+
+
+def test_append_of_one_token_without_its_axis():
+    from paper_2609_04263_amd import kvq
+    fmt, D = CASES["tiny_b16"]
+    K, V = synth.kv_tokens(51, 3, 1, 2, D)
+    a, b = (kvq.Cache(fmt, 3, 2, D, 100) for _ in range(2))
+    a.append_rope(kvq.Rope(D), dev_bf16(K), dev_bf16(V), pos0=9)
+    b.append_rope(kvq.Rope(D), dev_bf16(K[:, 0]), dev_bf16(V[:, 0]), pos0=9)
+    assert a.n == b.n == 1 and np.array_equal(image(a), image(b))
+
+
+def test_more_workgroups_than_a_row_of_the_grid():
+    # 2^22 + 5 tokens of one head: 2^20 + 2 workgroups of four waves
+    from paper_2609_04263_amd import kvq
+    n = (1 << 22) + 5
+    x = torch.ones((1, n, 1, 64), dtype=torch.bfloat16, device="cuda")
+    rope = kvq.Rope(64)
+    rope.qk(x, None, pos0=1)
+    at = [0, 1 << 21, (1 << 22) - 1, 1 << 22, n - 1]
+    y = torch.ones((1, len(at), 1, 64), dtype=torch.bfloat16, device="cuda")
+    rope.qk(y, None, pos=torch.tensor([[i + 1 for i in at]], dtype=torch.int32, device="cuda"))
+    assert torch.equal(x[0, at], y[0])
+    # every row has the length of its two halves' pairs
+    z = x.float().square()
+    assert ((z[..., :32] + z[..., 32:] - 2).abs() <= 4 * 2.0 ** -8).all()

@@ -96,6 +96,9 @@ class Shaped(FakeStorage):
         super().__init__(0, addr)
         self.shape = shape
 
+    def dim(self):
+        return len(self.shape)
+
 
 def ints(*shape):
     return torch.zeros(shape, dtype=torch.int32)
