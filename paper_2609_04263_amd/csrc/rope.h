@@ -11,7 +11,7 @@
 //     sin x = x - x^3/3! + .. - x^15/15!,  cos x = 1 - x^2/2! + .. + x^16/16!
 // leave less than 5e-17, so the binary32 cosine is the nearest one in all but
 // 1 of 10^8 cases.  Binary64 operations run at the rate of (unpacked) binary32
-// ones on this chip: 35 of them per pair.
+// ones on this chip: about 35 of them per pair.
 #pragma once
 
 #include "kvq_device.h"
