@@ -164,10 +164,13 @@ def _ints(values, count: int, what: str):
 ROPE_SCALINGS = ("plain", "linear", "base", "bands", "yarn")
 
 
-def _positions(t, count: int, what: str) -> None:
-    """Refuses what is not `count` int32 numbers in one piece (the library sees an address alone)."""
-    if t is not None and (t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous()):
+def _positions(t, count: int, what: str, beside) -> None:
+    """Refuses what is not `count` int32 numbers in one piece on the device of `beside` (the library sees an address
+    alone)."""
+    if t.dtype != torch.int32 or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{what}: {count} contiguous int32 numbers expected")
+    if t.get_device() != beside.get_device():
+        raise ValueError(f"{what}: on another device than the tensors beside it")
 
 
 class Rope:
@@ -208,8 +211,10 @@ class Rope:
             B, n, D = b, m, d
             k = K.data_ptr()
             ko = k if Ko is None else Ko.data_ptr()
+        elif Q is None:
+            raise ValueError("neither Q nor K")
         if pos is not None:
-            _positions(pos, B * n, "pos")
+            _positions(pos, B * n, "pos", K if Q is None else Q)
             pos = pos.data_ptr()
         st = _rope_qk(self._ref, q, k, B, n, H_q, H, D, q_norm if q_norm is None else q_norm.data_ptr(),
                       k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0, qo, ko, _stream(stream))
@@ -285,20 +290,23 @@ class Cache:
                     k_norm=None, pos=None, pos0: int = 0, fmt=None, stream=None) -> None:
         """append of keys that `rope` norms and rotates on the way.  bf16 K, V [B, n_in, H_kv, D]; with rows (device
         int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]:
-        one token).  Q, Qo
-        [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32 [B, n_new], or
-        None for pos0, pos0 + 1, .."""
+        one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32
+        [B, n_new], or None for pos0, pos0 + 1, .."""
         n_in = K.shape[1] if K.dim() == 4 else 1
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
         if rows is not None:
-            _positions(rows, self.B * n_new, "rows")
+            _positions(rows, self.B * n_new, "rows", K)
             rows = rows.data_ptr()
         if pos is not None:
-            _positions(pos, self.B * n_new, "pos")
+            _positions(pos, self.B * n_new, "pos", K)
             pos = pos.data_ptr()
         f = self._fmt_ref if fmt is None else C.byref(Format.of(fmt))
-        q, H_q = (None, 0) if Q is None else (Q.data_ptr(), Q.shape[-2])
+        q, H_q = None, 0
+        if Q is not None:
+            if (Q.shape[1] if len(Q.shape) == 4 else 1) != n_new:
+                raise ValueError(f"Q: rows of {n_new} tokens expected")
+            q, H_q = Q.data_ptr(), Q.shape[-2]
         st = _append_rope(self.handle, rope._ref, K.data_ptr(), V.data_ptr(), n_in, rows, n_new, q, H_q,
                           q_norm if q_norm is None else q_norm.data_ptr(),
                           k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0,
@@ -401,7 +409,7 @@ class Cache:
         the tokens here before those, and those of them whose bits are set in tree (device int32
         [B, C, ceil(C / 32)], see tree_words)."""
         keep, ptr = (None, None) if first is None else _ints(first, prefix.B + 1, "first")
-        _positions(tree, self.B * C_len * (-(-C_len // 32)), "tree")
+        _positions(tree, self.B * C_len * (-(-C_len // 32)), "tree", Q)
         nbytes = workspace.numel() * workspace.element_size()
         st = _lib.kvq_tree_attn_shared(prefix.handle, self.handle, ptr, Q.data_ptr(), C_len, H_q, sm_scale,
                                        tree.data_ptr(), O.data_ptr(), workspace.data_ptr(), nbytes, _stream(stream))

@@ -99,6 +99,11 @@ class Shaped(FakeStorage):
     def dim(self):
         return len(self.shape)
 
+    def get_device(self):
+        return self.device_index
+
+    device_index = -1
+
 
 def ints(*shape):
     return torch.zeros(shape, dtype=torch.int32)
@@ -151,6 +156,8 @@ def test_rope_shapes(kvq):
         with pytest.raises(ValueError):
             rope.qk(Shaped(2, 3, 4, 64), Shaped(2, 3, 2, 64), pos=bad, stream=0)
     with pytest.raises(ValueError):
+        rope.qk(None, None, stream=0)
+    with pytest.raises(ValueError):
         rope.qk(Shaped(2, 3, 4, 64), Shaped(2, 4, 2, 64), stream=0)
 
 
@@ -186,3 +193,30 @@ def test_append_refusals(kvq):
     bad = lib.kvq_append_rope(c.handle, None, FAKE, FAKE, 4, None, 4, None, 0, None, None, None, 0, None, c._fmt_ref, 0)
     assert bad == kvq.ERR_ARG
     assert c.n == 95
+
+
+class OnDevice(Shaped):
+    device_index = 0
+
+
+def test_host_indices_beside_device_tensors(kvq):
+    # (an address of host memory would be read on the GPU)
+    c = cache(kvq, configs.make_format(), 3, 2, 64, 100, n=4)
+    k, q = OnDevice(3, 8, 2, 64), OnDevice(3, 2, 8, 64, addr=3 * FAKE)
+    for call in (lambda: kvq.Rope(64).qk(q, None, pos=ints(3, 2), stream=0),
+                 lambda: kvq.Rope(64).qk(None, k, pos=ints(3, 8), stream=0),
+                 lambda: c.append_rope(kvq.Rope(64), k, k, pos=ints(3, 8), stream=0),
+                 lambda: c.append_rope(kvq.Rope(64), k, k, rows=ints(3, 2), stream=0),
+                 lambda: c.tree_attn_shared(c, q, 2, 8, 0.125, ints(3, 2, 1), q, q, stream=0)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    assert c.n == 4
+
+
+def test_queries_of_other_tokens(kvq):
+    c = cache(kvq, configs.make_format(), 3, 2, 64, 100, n=4)
+    k = Shaped(3, 8, 2, 64)
+    for q, kw in ((Shaped(3, 8, 8, 64), dict(n_new=4)), (Shaped(3, 8, 64), {}), (Shaped(3, 4, 8, 64), {})):
+        with pytest.raises(ValueError, match="tokens"):
+            c.append_rope(kvq.Rope(64), k, k, Q=q, Qo=q, stream=0, **kw)
+    assert c.n == 4
