@@ -717,11 +717,13 @@ __global__ __launch_bounds__(D) void append_token_kernel(Params p)
 {
     __shared__ float xs[2][D];
     __shared__ float red[8 * 4];
-    const int unit = blockIdx.x, b = unit / p.H, h = unit % p.H, d = threadIdx.x;
+    const int unit = kRope<Params> ? (int)wg_index() : (int)blockIdx.x, b = unit / p.H, h = unit % p.H, d = threadIdx.x;
     if constexpr (kRope<Params>) {
         if (unit >= p.B * p.H) {  // a row of queries
             const RopeQkParams& q = p.queries;
             const size_t row = unit - p.B * p.H;
+            if (row >= (size_t)q.tokens * q.H_q)
+                return;
             const float x = rope_channel<D>(p.rope, input_position(p, (int)(row / q.H_q), 0), bf16_to_f32(q.q[row * D + d]),
                                             p.rope.wq, xs[0]);
             q.qo[row * D + d] = f32_to_bf16(x);
@@ -1404,7 +1406,8 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
 {
     const int units = p.B * p.H, n1 = p.n0 + p.n_new;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
-        launch_kernel((append_token_kernel<D, AppendRopeParams>), dim3(units + p.queries.tokens * p.queries.H_q), dim3(D), 0, stream, p);
+        const dim3 g = grid_of((uint32_t)units + (uint32_t)p.queries.tokens * (uint32_t)p.queries.H_q);
+        launch_kernel((append_token_kernel<D, AppendRopeParams>), g, dim3(D), 0, stream, p);
         return hipGetLastError();
     }
     // whole blocks by code_heads or code_channels, those at the ends by code_edge

@@ -342,3 +342,20 @@ def test_more_workgroups_than_a_row_of_the_grid():
     # every row has the length of its two halves' pairs
     z = x.float().square()
     assert ((z[..., :32] + z[..., 32:] - 2).abs() <= 4 * 2.0 ** -8).all()
+
+
+def test_one_token_of_more_workgroups_than_a_row_of_the_grid():
+    # 2^14 keys and 2^20 rows of queries, a workgroup each
+    from paper_2609_04263_amd import kvq
+    fmt, B, H_q, D = configs.make_format(k_group=32, v_group=32), 1 << 14, 64, 64
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn((B, 1, h, D), device="cuda", generator=gen).bfloat16() for h in (H_q, 1, 1))
+    rope, w = kvq.Rope(D), torch.rand(D, device="cuda", generator=gen).bfloat16()
+    one, two = (kvq.Cache(fmt, B, 1, D, 32) for _ in range(2))
+    guard = torch.full((q.numel() + 4096,), 7.0, dtype=torch.bfloat16, device="cuda")
+    qo, want, kk = guard[:q.numel()].view_as(q), torch.empty_like(q), torch.empty_like(k)
+    one.append_rope(rope, k, v, Q=q, Qo=qo, q_norm=w, k_norm=w, pos0=77)
+    rope.qk(q, k, want, kk, q_norm=w, k_norm=w, pos0=77)
+    two.append(kk, v)
+    assert torch.equal(qo, want) and torch.equal(one.storage, two.storage)
+    assert (guard[q.numel():] == 7.0).all()
