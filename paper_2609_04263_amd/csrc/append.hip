@@ -645,6 +645,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
 
 #endif
 
+#ifndef KVQ_APPEND_ROPE
 // One decoded token per (sequence, KV head) without a window: a workgroup of
 // D threads, thread d owning channel d of the token's K and V.  Every load
 // (the token's K and V, and the value piece it shares with earlier tokens)
@@ -675,69 +676,18 @@ __device__ __forceinline__ float group_reduce(float v, int g, bool is_max, float
     return v;
 }
 
-// Channel d = threadIdx.x of a row of D threads (value x), normed by weights w
-// (null: not), rotated and rounded to bf16; the row passes through xs [D].
 template <int D>
-__device__ __forceinline__ float rope_channel(const RopeArgs& r, int t, float x, const uint16_t* w, float* xs)
-{
-#pragma clang fp contract(off)
-    __shared__ double sums[D / 64];
-    const int d = threadIdx.x;
-    float2 cs = make_float2(1.0f, 0.0f);
-    const bool half = r.layout == KVQ_ROPE_HALF;
-    const int other = half ? (d < r.rot / 2 ? d + r.rot / 2 : d - r.rot / 2) : d ^ 1;
-    if (d < r.rot)
-        cs = rope_cos_sin(t, r.turns[half ? min(d, other) : d >> 1], r.scale);
-    if (w) {
-        double sum = row_sum<32>((double)x * (double)x);
-        sum += __shfl_xor(sum, 32);
-        if constexpr (D > 64) {
-            if ((d & 63) == 0)
-                sums[d >> 6] = sum;
-            __syncthreads();
-            sum = 0.0;
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i)
-                sum += sums[i];
-        }
-        x = (x * norm_factor(sum, D, r.eps)) * bf16_to_f32(w[d]);
-    }
-    xs[d] = x;
-    __syncthreads();
-    if (d < r.rot) {
-        const float a = x * cs.x, b = xs[other] * cs.y;
-        x = d > other ? a + b : a - b;
-    }
-    __syncthreads();  // xs may be written again
-    return bf16_to_f32(f32_to_bf16(x));
-}
-
-template <int D, typename Params>
-__global__ __launch_bounds__(D) void append_token_kernel(Params p)
+__global__ __launch_bounds__(D) void append_token_kernel(AppendParams p)
 {
     __shared__ float xs[2][D];
     __shared__ float red[8 * 4];
-    const int unit = kRope<Params> ? (int)wg_index() : (int)blockIdx.x, b = unit / p.H, h = unit % p.H, d = threadIdx.x;
-    if constexpr (kRope<Params>) {
-        if (unit >= p.B * p.H) {  // a row of queries
-            const RopeQkParams& q = p.queries;
-            const size_t row = unit - p.B * p.H;
-            if (row >= (size_t)q.tokens * q.H_q)
-                return;
-            const float x = rope_channel<D>(p.rope, input_position(p, (int)(row / q.H_q), 0), bf16_to_f32(q.q[row * D + d]),
-                                            p.rope.wq, xs[0]);
-            q.qo[row * D + d] = f32_to_bf16(x);
-            return;
-        }
-    }
+    const int unit = blockIdx.x, b = unit / p.H, h = unit % p.H, d = threadIdx.x;
     const int t = p.n0, tau = t & 31, j = t & 7;
     const size_t blk = (size_t)unit * (p.T / kBlockTok) + (size_t)(t / kBlockTok);
     const size_t vpi = value_piece<D>(blk, tau >> 3, d);
-    const size_t in = (input_row(p, b, 0) * p.H + h) * D + d;  // n_new == 1
+    const size_t in = ((size_t)b * p.H + h) * D + d;  // n_new == 1
     float x[2] = {bf16_to_f32(p.kin[in]), bf16_to_f32(p.vin[in])};
     const uint64_t old = load_piece(p.vc, vpi, p.v_bits);
-    if constexpr (kRope<Params>)
-        x[0] = rope_channel<D>(p.rope, input_position(p, b, 0), x[0], p.rope.wk, xs[0]);
     if (p.rotate) {
         xs[0][d] = x[0];
         xs[1][d] = x[1];
@@ -802,6 +752,8 @@ __global__ __launch_bounds__(D) void append_token_kernel(Params p)
         }
     }
 }
+
+#endif
 
 // fp16 window: slot t mod (R + F) <- fp16 of token t (rotated first when
 // the format rotates), for t in [ring_lo, n0 + n_new).  Runs after the coder
@@ -1338,6 +1290,113 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
     }
 }
 
+// One token per sequence without a window (a decode step), a wave per (sequence, KV
+// head): lanes 0 .. D / 8 - 1 hold eight channels each of its key, those from lane 32 on
+// of its value, so nothing waits for another wave; further waves rotate queries.  The
+// value pieces that it shares with earlier tokens are loaded first.  Bound by one chain
+// of latencies, its own instructions' fetch among them: 4 heads of 64 take 3.9 us, 8 of
+// 256 of 8 sequences 4.2.  With a thread per channel and reductions through LDS 4.5 and
+// 5.4; as this, but widths decided at run time (169 branches), 4.5 and 4.8.
+template <int D, int KB, int VB>
+__global__ __launch_bounds__(64) void append_token_rope_kernel(AppendRopeParams p)
+{
+#pragma clang fp contract(off)
+    constexpr int PPT = D / 8;
+    __shared__ __attribute__((aligned(16))) float2 angles[D / 2];
+    const uint32_t x = wg_index();
+    if (x >= p.code_wgs) {
+        const uint32_t item = x - p.code_wgs, parts = (uint32_t)p.queries.parts, token = item / parts;
+        if (token < (uint32_t)p.queries.tokens)
+            rope_rows<D, 1, false>(p.queries, p.rope, token, (int)(item - token * parts), angles);
+        return;
+    }
+    const int unit = (int)x, b = unit / p.H, h = unit - b * p.H, lane = threadIdx.x, P = lane & 31;
+    const bool value = lane >= 32, live = P < PPT;
+    const int t = p.n0, tau = t & 31, j = t & 7;
+    const size_t blk = (size_t)unit * (size_t)(p.T / kBlockTok) + (size_t)(t / kBlockTok);
+    const int bits = value ? VB : KB, group = value ? p.v_group : p.k_group;
+    const int log2 = value ? __builtin_ctz(p.v_group) : __builtin_ctz(p.k_group);
+    const bool affine = (value ? p.v_mode : p.k_mode) == KVQ_AFFINE;
+    const size_t at = (input_row(p, b, 0) * p.H + h) * D + 8 * P;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    uint64_t old[8];
+    if (live)
+        w = *(const u32x4*)((value ? p.vin : p.kin) + at);
+    if (live && value && j) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            old[e] = load_piece(p.vc, value_piece<D>(blk, tau >> 3, 8 * P + e), VB);
+    }
+    float v[8];
+    if (live && !value) {
+        const Angles turn(p.rope, input_position(p, b, 0), P);
+        widen8(w, v);
+        turn.template turn<D>(p.rope, P, v);
+    } else {
+        widen8(w, v);
+    }
+    if (p.rotate)  // (every lane of a row takes part)
+        rotate8<D>(v, P, p.rot_c);
+    // the group's extremes, over group / 8 lanes
+    float mn = v[0], mx = v[0], ma;
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+        mn = fminf(mn, v[e]);
+        mx = fmaxf(mx, v[e]);
+    }
+    const auto step = [&](float a, float c) {
+        mn = fminf(mn, a);
+        mx = fmaxf(mx, c);
+    };
+    typedef Coder<4, true> Dpp;
+    step(Dpp::dpp<0xB1>(mn), Dpp::dpp<0xB1>(mx));
+    step(Dpp::dpp<0x4E>(mn), Dpp::dpp<0x4E>(mx));
+    float a = Dpp::dpp<0x141>(mn), c = Dpp::dpp<0x141>(mx);
+    if (group > 32)
+        step(a, c);
+    a = Dpp::dpp<0x140>(mn), c = Dpp::dpp<0x140>(mx);
+    if (group > 64)
+        step(a, c);
+    a = __shfl_xor(mn, 16), c = __shfl_xor(mx, 16);
+    if (group > 128)
+        step(a, c);
+    ma = fmaxf(fabsf(mn), fabsf(mx));
+    const float top = (float)((1 << bits) - 1), qmax = (float)((1 << (bits - 1)) - 1);
+    float s = fmaxf((affine ? mx - mn : ma) / (affine ? top : qmax), 1e-8f), z = affine ? mn + 0.0f : 0.0f;
+    round_meta(p.meta16, &s, &z);
+    const float y = 1.0f / s, lo = affine ? 0.0f : -qmax, hi = affine ? top : qmax, half = affine ? 0.0f : (float)(1 << (bits - 1));
+    uint32_t code[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // (Coder::piece)
+        const float d = v[e] - z;
+        float q = d * y;
+        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), y, q);
+        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), y, q);
+        code[e] = (uint32_t)(__builtin_amdgcn_fmed3f(__builtin_rintf(q), lo, hi) + half);
+    }
+    if (!live)
+        return;
+    if ((8 * P & (group - 1)) == 0) {
+        const size_t mi = (blk * (size_t)(D >> log2) + (size_t)(8 * P >> log2)) * kBlockTok + tau;
+        store_meta(value ? p.vs : p.ks, mi, s, p.meta16);
+        if (affine)
+            store_meta(value ? p.vz : p.kz, mi, z, p.meta16);
+    }
+    if (value) {
+        const uint64_t keep = low_codes(VB, j);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            store_piece(p.vc, value_piece<D>(blk, tau >> 3, 8 * P + e), VB,
+                        (j ? old[e] & keep : 0) | ((uint64_t)code[e] << (VB * j)));
+    } else {
+        uint64_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            word |= (uint64_t)code[e] << (KB * e);
+        store_piece(p.kc, key_piece<D>(blk, tau, P), KB, word);
+    }
+}
+
 // One launch for all that an append with positions does: workgroups that code
 // blocks, the longest, come first, then those that write window rows and those that
 // rotate queries (four waves of rope_rows).
@@ -1385,6 +1444,21 @@ __global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_
         rope_rows<D, kQueryIter, false>(p.queries, p.rope, token, (int)(item - token * (uint32_t)p.queries.parts), angles[wave]);
 }
 
+template <int D>
+void launch_token(const AppendRopeParams& p, dim3 g, hipStream_t stream)
+{
+    if (p.k_bits == 8)
+        launch_kernel(append_token_rope_kernel<D, 8, 8>, g, dim3(64), 0, stream, p);
+    else if (p.k_bits == 4 && p.v_bits == 4)
+        launch_kernel(append_token_rope_kernel<D, 4, 4>, g, dim3(64), 0, stream, p);
+    else if (p.k_bits == 4)
+        launch_kernel(append_token_rope_kernel<D, 4, 2>, g, dim3(64), 0, stream, p);
+    else if (p.v_bits == 4)
+        launch_kernel(append_token_rope_kernel<D, 2, 4>, g, dim3(64), 0, stream, p);
+    else
+        launch_kernel(append_token_rope_kernel<D, 2, 2>, g, dim3(64), 0, stream, p);
+}
+
 template <int D, bool PERCH, bool PLAIN>
 void launch_blocks(const AppendRopeParams& p, uint32_t grid, hipStream_t stream)
 {
@@ -1406,8 +1480,10 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
 {
     const int units = p.B * p.H, n1 = p.n0 + p.n_new;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
-        const dim3 g = grid_of((uint32_t)units + (uint32_t)p.queries.tokens * (uint32_t)p.queries.H_q);
-        launch_kernel((append_token_kernel<D, AppendRopeParams>), g, dim3(D), 0, stream, p);
+        constexpr int RPI = 1024 / D;
+        p.queries.parts = (p.queries.H_q + RPI - 1) / RPI;
+        p.code_wgs = (uint32_t)units;
+        launch_token<D>(p, grid_of(p.code_wgs + (uint32_t)(p.queries.tokens * p.queries.parts)), stream);
         return hipGetLastError();
     }
     // whole blocks by code_heads or code_channels, those at the ends by code_edge
@@ -1469,7 +1545,7 @@ hipError_t launch_append_d(const AppendParams& p, hipStream_t stream)
 {
     const int units = p.B * p.H;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
-        launch_kernel((append_token_kernel<D, AppendParams>), dim3(units), dim3(D), 0, stream, p);
+        launch_kernel(append_token_kernel<D>, dim3(units), dim3(D), 0, stream, p);
         return hipGetLastError();
     }
     if (p.q1 > p.q0) {
