@@ -1068,8 +1068,10 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
 // The part of block tb that this call codes, tokens lo .. hi - 1 of one head (per-token
 // groups; never of a window, which is coded by whole blocks).  Value pieces keep the
 // bits of tokens appended earlier and clear later ones; those of the first octet are
-// loaded first, with the rows.  Bound by latency: five tokens of 128 heads took 11.0 us
-// as edge_block, which takes all 32 rows and loads old pieces when it needs them.
+// loaded first, with the rows.  Bound by latency: five tokens of 16 x 8 heads of 128 take
+// 5.2 us; 7.0 where a thread codes a key and then a value, which more tokens than T / 2
+// do (31 of 8 x 8 heads of 256: 10.4, 12.7 with keys and values apart); 11.0 as edge_block,
+// which takes all 32 rows and loads old pieces when it needs them.
 template <int D, int KB, int VB, bool PLAIN>
 __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, int tb)
 {
@@ -1084,35 +1086,56 @@ __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, i
     const Coder<KB, PLAIN> kcode(p.k_mode);
     const Coder<VB, PLAIN> vcode(p.v_mode);
     const Groups<D> kg(p.k_group), vg(p.v_group);
-    for (int t = lo + tid / PPT; t < hi; t += T) {  // (all lanes of a row or none)
-        const int i = t - tb;
-        const size_t at = (input_row(p, b, t - p.n0) * p.H + h) * D + 8 * P;
-        const u32x4 kw = *(const u32x4*)(p.kin + at), vw = *(const u32x4*)(p.vin + at);
+    const auto load = [&](const uint16_t* in, int t) {
+        return *(const u32x4*)(in + (input_row(p, b, t - p.n0) * p.H + h) * D + 8 * P);
+    };
+    const auto key = [&](int t, const u32x4& w) {
         float x[8], s, z;
         const Angles turn(p.rope, input_position(p, b, t - p.n0), P);
-        widen8(kw, x);
+        widen8(w, x);
         turn.template turn<D>(p.rope, P, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
         kcode.scale(x, kg.lanes, p.meta16, &s, &z);
         if (kg.first(P)) {
-            const size_t mi = (blk * kg.count + kg.of(P)) * kBlockTok + i;
+            const size_t mi = (blk * kg.count + kg.of(P)) * kBlockTok + (t - tb);
             store_meta(p.ks, mi, s, p.meta16);
             if (kcode.affine)
                 store_meta(p.kz, mi, z, p.meta16);
         }
-        store_piece(p.kc, key_piece<D>(blk, i, P), KB, kcode.piece(x, s, z));
-        widen8(vw, x);
+        store_piece(p.kc, key_piece<D>(blk, t - tb, P), KB, kcode.piece(x, s, z));
+    };
+    const auto value = [&](int t, const u32x4& w) {
+        float x[8], s, z;
+        widen8(w, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
         vcode.scale(x, vg.lanes, p.meta16, &s, &z);
         if (vg.first(P)) {
-            const size_t mi = (blk * vg.count + vg.of(P)) * kBlockTok + i;
+            const size_t mi = (blk * vg.count + vg.of(P)) * kBlockTok + (t - tb);
             store_meta(p.vs, mi, s, p.meta16);
             if (vcode.affine)
                 store_meta(p.vz, mi, z, p.meta16);
         }
-        store_piece(words, i * PPT + P, VB, vcode.piece(x, s, z));
+        store_piece(words, (t - tb) * PPT + P, VB, vcode.piece(x, s, z));
+    };
+    const int row = tid / PPT;  // (all lanes of a row or none)
+    if (hi - lo <= T / 2) {  // keys by two waves, values by the others
+        const bool keys = row < T / 2;
+        const int t = lo + row % (T / 2);
+        if (t < hi) {
+            const u32x4 w = load(keys ? p.kin : p.vin, t);
+            if (keys)
+                key(t, w);
+            else
+                value(t, w);
+        }
+    } else {
+        for (int t = lo + row; t < hi; t += T) {
+            const u32x4 kw = load(p.kin, t), vw = load(p.vin, t);
+            key(t, kw);
+            value(t, vw);
+        }
     }
     __syncthreads();
     for (int idx = tid; idx < (o1 - o0 + 1) * D; idx += kThreads) {

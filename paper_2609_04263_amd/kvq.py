@@ -292,7 +292,8 @@ class Cache:
         int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]:
         one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32
         [B, n_new], or None for pos0, pos0 + 1, .."""
-        n_in = K.shape[1] if K.dim() == 4 else 1
+        shape = K.shape
+        n_in = shape[1] if len(shape) == 4 else 1
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
         if rows is not None:
@@ -304,9 +305,10 @@ class Cache:
         f = self._fmt_ref if fmt is None else C.byref(Format.of(fmt))
         q, H_q = None, 0
         if Q is not None:
-            if (Q.shape[1] if len(Q.shape) == 4 else 1) != n_new:
+            shape = Q.shape
+            if (shape[1] if len(shape) == 4 else 1) != n_new:
                 raise ValueError(f"Q: rows of {n_new} tokens expected")
-            q, H_q = Q.data_ptr(), Q.shape[-2]
+            q, H_q = Q.data_ptr(), shape[-2]
         st = _append_rope(self.handle, rope._ref, K.data_ptr(), V.data_ptr(), n_in, rows, n_new, q, H_q,
                           q_norm if q_norm is None else q_norm.data_ptr(),
                           k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0,
