@@ -1504,7 +1504,7 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
     const int units = p.B * p.H, n1 = p.n0 + p.n_new;
     if (p.n_new == 1 && p.ring == 0 && p.k_axis == KVQ_PER_TOKEN) {
         constexpr int RPI = 1024 / D;
-        p.queries.parts = (p.queries.H_q + RPI - 1) / RPI;
+        p.queries.parts = p.queries.tokens > 0 ? (p.queries.H_q + RPI - 1) / RPI : 1;
         p.code_wgs = (uint32_t)units;
         launch_token<D>(p, grid_of(p.code_wgs + (uint32_t)(p.queries.tokens * p.queries.parts)), stream);
         return hipGetLastError();
@@ -1523,6 +1523,7 @@ hipError_t launch_append_d(AppendRopeParams p, hipStream_t stream)
     const bool ring = p.ring && n1 > p.ring_lo, together = ring && n1 - p.ring <= p.q0;
     p.row_wgs = together ? (uint32_t)((n1 - p.ring_lo + kRingRows<D> - 1) / kRingRows<D>) * (uint32_t)units : 0;
     uint32_t others = p.row_wgs;
+    p.queries.parts = 1;  // (a divisor, without queries too)
     if (p.queries.tokens > 0) {
         constexpr int RPI = 1024 / D;
         p.queries.parts = (p.queries.H_q + RPI * kQueryIter - 1) / (RPI * kQueryIter);

@@ -359,3 +359,17 @@ def test_one_token_of_more_workgroups_than_a_row_of_the_grid():
     two.append(kk, v)
     assert torch.equal(qo, want) and torch.equal(one.storage, two.storage)
     assert (guard[q.numel():] == 7.0).all()
+
+
+@pytest.mark.parametrize("n", (1, 3))
+def test_more_heads_than_a_row_of_the_grid_without_queries(n):
+    from paper_2609_04263_amd import kvq
+    fmt, B, D = configs.make_format(k_group=32, v_group=32), (1 << 20) + 5, 64
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    k, v = (torch.randn((B, n, 1, D), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    rope, kk = kvq.Rope(D), torch.empty_like(k)
+    one, two = (kvq.Cache(fmt, B, 1, D, 32) for _ in range(2))
+    one.append_rope(rope, k, v, pos0=77)
+    rope.qk(None, k, None, kk, pos0=77)
+    two.append(kk, v)
+    assert torch.equal(one.storage, two.storage)
