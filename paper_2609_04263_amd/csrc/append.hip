@@ -344,7 +344,7 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
                 if (p.k_mode == KVQ_AFFINE)
                     store_meta(p.kz, mi, z, p.meta16);
             }
-            const float r = __builtin_amdgcn_rcpf(s);
+            const float r = code_reciprocal(s);
             uint64_t word = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -371,7 +371,7 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
             if (p.v_mode == KVQ_AFFINE)
                 store_meta(p.vz, mi, z, p.meta16);
         }
-        const float r = __builtin_amdgcn_rcpf(s);
+        const float r = code_reciprocal(s);
         uint32_t c[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -402,14 +402,24 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
 
 // ---- blocks
 
+// Whether finite numbers can leave a group of BITS-bit codes a scale s without a
+// hardware reciprocal: with more bits a range is divided by 7 at least.
+template <int BITS>
+__device__ __forceinline__ bool no_reciprocal(float s)
+{
+    return BITS == 2 && s > kMostReciprocal;
+}
+
 // The eight codes of a piece.  The quotient is the product with the hardware
 // reciprocal wherever that provably rounds to the same code (rint_quotient);
 // the eight distances to the rounded values are folded into one test, and a
 // piece with a near tie takes the exact divisions.  Codes are packed by fp32
 // sums (below 2^24, exact), one conversion per 16 bits: conversions, shifts
-// and the per-element branch took half of the instructions before.
+// and the per-element branch took half of the instructions before.  `divide`: a
+// scale has no reciprocal (no_reciprocal), so all take the divisions.
 template <int BITS>
-__device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, const float* r, const float* z, int mode)
+__device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, const float* r, const float* z, int mode,
+                                                bool divide)
 {
 #pragma clang fp contract(off)
     const float top = (float)((1 << BITS) - 1), qmax = (float)((1 << (BITS - 1)) - 1), half = (float)(1 << (BITS - 1));
@@ -427,7 +437,7 @@ __device__ __forceinline__ uint64_t piece_codes(const float* x, const float* s, 
         c[e] = __builtin_rintf(q);
         worst = fmaxf(worst, fabsf(q - c[e]));
     }
-    if (worst >= 0.5f - kNear) {
+    if (worst >= 0.5f - kNear || divide) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             c[e] = __builtin_rintf((aff ? x[e] - z[e] : x[e]) / s[e]);
@@ -520,7 +530,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
             }
             const float r = __builtin_amdgcn_rcpf(s);
             const float s8[8] = {s, s, s, s, s, s, s, s}, r8[8] = {r, r, r, r, r, r, r, r}, z8[8] = {z, z, z, z, z, z, z, z};
-            store_piece(ob, key_piece<D>(0, i, P), KB, piece_codes<KB>(x, s8, r8, z8, p.k_mode));
+            store_piece(ob, key_piece<D>(0, i, P), KB, piece_codes<KB>(x, s8, r8, z8, p.k_mode, no_reciprocal<KB>(s)));
         }
     } else {
         kmeta = D;
@@ -582,9 +592,10 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
             *(float4*)(r8 + e) = *(const float4*)&cs[1][c8 + e];
             *(float4*)(z8 + e) = *(const float4*)&cs[2][c8 + e];
         }
+        // (a window's numbers, and so the scales, are below 2^17)
 #pragma unroll
         for (int k = 0; k < kSteps; ++k)
-            store_piece(ob, key_piece<D>(0, RowStage<D>::row(k), c8 / 8), KB, piece_codes<KB>(x[k], s8, r8, z8, p.k_mode));
+            store_piece(ob, key_piece<D>(0, RowStage<D>::row(k), c8 / 8), KB, piece_codes<KB>(x[k], s8, r8, z8, p.k_mode, false));
     }
     __syncthreads();
     copy_out(ob, (uint8_t*)p.kc + blk * (size_t)(4 * D * KB), 4 * D * KB);
@@ -609,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void append_block_kernel(AppendParams p)
         }
         const float r = __builtin_amdgcn_rcpf(s);
         const float s8[8] = {s, s, s, s, s, s, s, s}, r8[8] = {r, r, r, r, r, r, r, r}, z8[8] = {z, z, z, z, z, z, z, z};
-        store_piece(vw, i * PPT + P, VB, piece_codes<VB>(x, s8, r8, z8, p.v_mode));
+        store_piece(vw, i * PPT + P, VB, piece_codes<VB>(x, s8, r8, z8, p.v_mode, no_reciprocal<VB>(s)));
     }
     __syncthreads();
     // (octet o, channels 8 P .. 8 P + 7): the eight tokens' words transposed
@@ -727,7 +738,7 @@ __global__ __launch_bounds__(D) void append_token_kernel(AppendParams p)
             z = 0.0f;
         }
         round_meta(p.meta16, &s, &z);
-        const uint32_t c = code_one(x[w], s, __builtin_amdgcn_rcpf(s), z, mode, bits);
+        const uint32_t c = code_one(x[w], s, code_reciprocal(s), z, mode, bits);
         if (d % g == 0) {
             const size_t mi = (blk * ng + gi) * kBlockTok + tau;
             store_meta(w ? p.vs : p.ks, mi, s, p.meta16);

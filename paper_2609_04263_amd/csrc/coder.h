@@ -39,19 +39,30 @@ __device__ __forceinline__ uint64_t low_codes(int bits, int n)
     return (1ull << (bits * n)) - 1ull;
 }
 
+// A scale above which the hardware's reciprocal, subnormal, is flushed to zero
+// (2-bit codes of numbers above 2^126).
+constexpr float kMostReciprocal = 0x1p126f;
+
+// The hardware reciprocal of a scale, or NaN where there is none.
+__device__ __forceinline__ float code_reciprocal(float s)
+{
+    const float r = __builtin_amdgcn_rcpf(s);
+    return s > kMostReciprocal ? __builtin_nanf("") : r;
+}
+
 // rint(fl(d / s)), the correctly rounded quotient rounded half to even,
-// with r the hardware reciprocal of s (within 1 ulp).  d r is within about
+// with r the code_reciprocal of s (within 1 ulp).  d r is within about
 // 1.5 2^-23 relative of d / s, so for |d / s| <= 256 (every code here) it
 // is within 2^-14 of fl(d / s); rint can differ only if that interval
 // contains a half-integer, so the exact division runs only where d r lies
-// within 2^-10 of one.
+// within 2^-10 of one, or is no number.
 __device__ __forceinline__ float rint_quotient(float d, float s, float r)
 {
 #pragma clang fp contract(off)
     const float q = d * r;
     float c = __builtin_rintf(q);
     const float f = q - floorf(q);
-    if (fabsf(f - 0.5f) < 0x1p-10f)
+    if (!(fabsf(f - 0.5f) >= 0x1p-10f))
         c = __builtin_rintf(d / s);
     return c;
 }
@@ -127,7 +138,7 @@ __device__ __forceinline__ void store_meta(float* base, size_t i, float v, int m
         base[i] = v;
 }
 
-// Code of x in a group with scale s (r = its hardware reciprocal) and offset z.
+// Code of x in a group with scale s (r = its code_reciprocal) and offset z.
 __device__ __forceinline__ uint32_t code_one(float x, float s, float r, float z, int mode, int bits)
 {
 #pragma clang fp contract(off)

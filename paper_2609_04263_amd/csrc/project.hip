@@ -740,7 +740,7 @@ __device__ void fused_code_slices(const ProjParams& p, uint8_t* glds, int m0, in
             if (mode == KVQ_AFFINE)
                 store_meta(mzs + (p.meta16 ? q * mcount / 2 : q * mcount), mi_, z, p.meta16);
         }
-        const float r = __builtin_amdgcn_rcpf(s);
+        const float r = code_reciprocal(s);
         uint32_t c[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
