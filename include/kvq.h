@@ -19,7 +19,9 @@
  *     KVQ_ERR_DEVICE reports a HIP launch error (state is then undefined).
  *   - Device pointers must be 16-byte aligned.  bf16 and fp16 tensors are
  *     16-bit IEEE-style storage (bfloat16 / binary16).
- *   - Non-finite inputs are outside the contract (results are undefined).
+ *   - Non-finite inputs are outside the contract (results are undefined), as
+ *     are those that become so on the way: in a transform's sums, a norm or a
+ *     rotation, or as fp16 rows of a window or a sink (above 65504).
  */
 #ifndef KVQ_H
 #define KVQ_H

@@ -836,13 +836,31 @@ struct Groups {
     __device__ __forceinline__ int of(int piece) const { return piece >> shift; }
 };
 
+// What a group's codes are made with: its scale, that one's reciprocal and its offset, of
+// numbers times 2^-8, so that no finite number's difference from the offset overflows and no
+// reciprocal is subnormal below an infinite scale (2^127 here: every code is 0, or the
+// middle).  Between numbers of magnitude up to `most` of which one is the offset the scale is
+// no less than most 2^-32, so raising it to most 2^-120 changes nothing; where fp16 holds the
+// offset of a larger constant, it keeps the quotients finite and beyond every code's.
+struct Divisor {
+    float s, y, z;
+    __device__ __forceinline__ Divisor(float scale, float offset, float most)
+        : s(__builtin_amdgcn_fmed3f(scale * 0x1p-8f, most * 0x1p-128f, 0x1p127f)), y(1.0f / s), z(offset * 0x1p-8f) {}
+};
+
+// fl(x - offset) 2^-8.
+__device__ __forceinline__ float from_offset(float x, float z)
+{
+    return __builtin_fmaf(x, 0x1p-8f, -z);
+}
+
 // The coder of code_heads: the codes, scales and offsets of piece_group_stats,
 // round_meta and piece_codes in fewer operations.  A symmetric group is one with
 // offset zero and other limits (`bias` makes its codes unsigned); the sums of a
 // group meet by DPP, and a group's range is divided by 2^b - 1 as
 //     q = fl(d fl(1 / n)),  s = fl(q + fl(d - q n) fl(1 / n)),
 // the correctly rounded quotient (checked for every mantissa and n = 1, 3, 7, 15,
-// 127, 255; where it would be subnormal the scale is 1e-8).
+// 127, 255; where it would be subnormal the scale is 1e-8), infinite where d is.
 template <int BITS, bool PLAIN>
 struct Coder {
     float n, inv, lo, hi, bias;  // bias: of 16 / BITS codes in their places
@@ -880,12 +898,12 @@ struct Coder {
         return x;
     }
 
-    __device__ __forceinline__ void scale(const float* x, int lanes, int meta16, float* s, float* z) const
+    __device__ __forceinline__ Divisor scale(const float* x, int lanes, int meta16, float* s, float* z) const
     {
 #pragma clang fp contract(off)
         const auto least = [](float a, float b) { return fminf(a, b); };
         const auto most = [](float a, float b) { return fmaxf(a, b); };
-        float d;
+        float d, large = 0.0f;
         if (affine) {
             float mn = x[0], mx = x[0];
 #pragma unroll
@@ -896,6 +914,7 @@ struct Coder {
             mn = reduce(mn, lanes, least);
             mx = reduce(mx, lanes, most);
             d = mx - mn;
+            large = fmaxf(fabsf(mn), fabsf(mx));
             *z = mn + 0.0f;  // canonical +0 for a signed-zero minimum
         } else {
             float ma = fabsf(x[0]);
@@ -907,21 +926,21 @@ struct Coder {
         }
         *s = over_n(d);
         round_meta(meta16, s, z);
+        return Divisor(*s, *z, large);
     }
 
     __device__ __forceinline__ float over_n(float d) const
     {
-        const float q = d * inv;
+        const float q = fminf(d * inv, 0x1.fffffep127f);
         return fmaxf(__builtin_fmaf(__builtin_fmaf(-q, n, d), inv, q), 1e-8f);
     }
 
-    __device__ __forceinline__ uint64_t piece(const float* x, float s, float z) const
+    __device__ __forceinline__ uint64_t piece(const float* x, const Divisor& by) const
     {
-        const float y = 1.0f / s;
-        return piece(x, [&](int) { return s; }, [&](int) { return y; }, [&](int) { return z; });
+        return piece(x, [&](int) { return by.s; }, [&](int) { return by.y; }, [&](int) { return by.z; });
     }
 
-    // Element e's scale, the nearest binary32 number to its reciprocal, and its offset.
+    // Element e's Divisor.
     // fl(d / s) by two corrections of fl(d y): the first leaves less than an ulp, from
     // which the second gives the correctly rounded quotient (Markstein's theorem; no
     // exception in 2 10^9 pairs).  Numbers on a grid, as bf16 rows are, meet ties of their
@@ -933,7 +952,7 @@ struct Coder {
         float c[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float d = x[e] - z(e);
+            const float d = from_offset(x[e], z(e));
             float q = d * y(e);
             q = __builtin_fmaf(__builtin_fmaf(-q, s(e), d), y(e), q);
             q = __builtin_fmaf(__builtin_fmaf(-q, s(e), d), y(e), q);
@@ -1038,23 +1057,23 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
         if (fresh)
             turn.template turn<D>(p.rope, norm, P, x);
         to_cache(x);
-        kcode.scale(x, kg.lanes, p.meta16, &s, &z);
+        const Divisor kdiv = kcode.scale(x, kg.lanes, p.meta16, &s, &z);
         if (kg.first(P)) {
             buf.meta[0][kg.of(P) * T + i] = s;
             buf.meta[1][kg.of(P) * T + i] = z;
         }
-        store_piece(buf.k, kp, KB, kcode.piece(x, s, z));
+        store_piece(buf.k, kp, KB, kcode.piece(x, kdiv));
         widen(vw, x);
         vsrc += step;
         if (j + 1 < heads)
             vw = *(const u32x4*)vsrc;
         to_cache(x);
-        vcode.scale(x, vg.lanes, p.meta16, &s, &z);
+        const Divisor vdiv = vcode.scale(x, vg.lanes, p.meta16, &s, &z);
         if (vg.first(P)) {
             buf.meta[2][vg.of(P) * T + i] = s;
             buf.meta[3][vg.of(P) * T + i] = z;
         }
-        store_piece(buf.v, i * PPT + P, VB, vcode.piece(x, s, z));
+        store_piece(buf.v, i * PPT + P, VB, vcode.piece(x, vdiv));
         __syncthreads();
         if (tid < 16 * KB)  // 16 bytes of the key pieces
             *(u32x4*)kdst = *(const u32x4*)(buf.k + 16 * tid);
@@ -1107,28 +1126,28 @@ __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, i
         turn.template turn<D>(p.rope, P, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
-        kcode.scale(x, kg.lanes, p.meta16, &s, &z);
+        const Divisor by = kcode.scale(x, kg.lanes, p.meta16, &s, &z);
         if (kg.first(P)) {
             const size_t mi = (blk * kg.count + kg.of(P)) * kBlockTok + (t - tb);
             store_meta(p.ks, mi, s, p.meta16);
             if (kcode.affine)
                 store_meta(p.kz, mi, z, p.meta16);
         }
-        store_piece(p.kc, key_piece<D>(blk, t - tb, P), KB, kcode.piece(x, s, z));
+        store_piece(p.kc, key_piece<D>(blk, t - tb, P), KB, kcode.piece(x, by));
     };
     const auto value = [&](int t, const u32x4& w) {
         float x[8], s, z;
         widen8(w, x);
         if (!PLAIN && p.rotate)
             rotate8<D>(x, P, p.rot_c);
-        vcode.scale(x, vg.lanes, p.meta16, &s, &z);
+        const Divisor by = vcode.scale(x, vg.lanes, p.meta16, &s, &z);
         if (vg.first(P)) {
             const size_t mi = (blk * vg.count + vg.of(P)) * kBlockTok + (t - tb);
             store_meta(p.vs, mi, s, p.meta16);
             if (vcode.affine)
                 store_meta(p.vz, mi, z, p.meta16);
         }
-        store_piece(words, (t - tb) * PPT + P, VB, vcode.piece(x, s, z));
+        store_piece(words, (t - tb) * PPT + P, VB, vcode.piece(x, by));
     };
     const int row = tid / PPT;  // (all lanes of a row or none)
     if (hi - lo <= T / 2) {  // keys by two waves, values by the others
@@ -1174,7 +1193,7 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
     constexpr bool kAngles = D <= 128;
     __shared__ __attribute__((aligned(16))) uint8_t kbuf[4 * D * KB], vbuf[4 * D * VB];
     __shared__ __attribute__((aligned(16))) float meta[2][kBlockTok * 8];  // value scales, offsets: [groups][32]
-    __shared__ __attribute__((aligned(16))) float red[2][4][D], cs[3][D];  // extremes by wave; scales, reciprocals, offsets
+    __shared__ __attribute__((aligned(16))) float red[2][4][D], cs[3][D];  // extremes by wave; each channel's Divisor
     __shared__ __attribute__((aligned(16))) float4 angles[kAngles ? kBlockTok : 1][kAngles ? D / 4 : 1];
     const int tid = threadIdx.x, P = tid % PPT, lane = tid & 63, wave = tid >> 6;
     const Coder<KB, false> kcode(p.k_mode);
@@ -1265,9 +1284,10 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
             const float hi = fmaxf(fmaxf(red[1][0][tid], red[1][1][tid]), fmaxf(red[1][2][tid], red[1][3][tid]));
             float s = kcode.over_n(aff ? hi - lo : hi), z = aff ? lo + 0.0f : 0.0f;
             round_meta(p.meta16, &s, &z);
-            cs[0][tid] = s;
-            cs[1][tid] = 1.0f / s;
-            cs[2][tid] = z;
+            const Divisor by(s, z, aff ? fmaxf(fabsf(lo), fabsf(hi)) : 0.0f);
+            cs[0][tid] = by.s;
+            cs[1][tid] = by.y;
+            cs[2][tid] = by.z;
             store_meta(p.ks, blk * D + tid, s, p.meta16);
             if (aff)
                 store_meta(p.kz, blk * D + tid, z, p.meta16);
@@ -1289,12 +1309,12 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
             const int i = RowStage<D>::row(k);
             float v[8], s, z;
             vst.widen(p, tb, k, v, NoAngles());
-            vcode.scale(v, vg.lanes, p.meta16, &s, &z);
+            const Divisor by = vcode.scale(v, vg.lanes, p.meta16, &s, &z);
             if (vg.first(P)) {
                 meta[0][vg.of(P) * kBlockTok + i] = s;
                 meta[1][vg.of(P) * kBlockTok + i] = z;
             }
-            store_piece(vbuf, i * PPT + P, VB, vcode.piece(v, s, z));
+            store_piece(vbuf, i * PPT + P, VB, vcode.piece(v, by));
         }
         if (h + 1 < h0 + heads)
             vst.load(p, 1, b, h + 1, tb);
@@ -1398,14 +1418,15 @@ __global__ __launch_bounds__(64) void append_token_rope_kernel(AppendRopeParams 
     const float top = (float)((1 << bits) - 1), qmax = (float)((1 << (bits - 1)) - 1);
     float s = fmaxf((affine ? mx - mn : ma) / (affine ? top : qmax), 1e-8f), z = affine ? mn + 0.0f : 0.0f;
     round_meta(p.meta16, &s, &z);
-    const float y = 1.0f / s, lo = affine ? 0.0f : -qmax, hi = affine ? top : qmax, half = affine ? 0.0f : (float)(1 << (bits - 1));
+    const Divisor by(s, z, affine ? ma : 0.0f);
+    const float lo = affine ? 0.0f : -qmax, hi = affine ? top : qmax, half = affine ? 0.0f : (float)(1 << (bits - 1));
     uint32_t code[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {  // (Coder::piece)
-        const float d = v[e] - z;
-        float q = d * y;
-        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), y, q);
-        q = __builtin_fmaf(__builtin_fmaf(-q, s, d), y, q);
+        const float d = from_offset(v[e], by.z);
+        float q = d * by.y;
+        q = __builtin_fmaf(__builtin_fmaf(-q, by.s, d), by.y, q);
+        q = __builtin_fmaf(__builtin_fmaf(-q, by.s, d), by.y, q);
         code[e] = (uint32_t)(__builtin_amdgcn_fmed3f(__builtin_rintf(q), lo, hi) + half);
     }
     if (!live)
