@@ -105,7 +105,7 @@ struct Angles {
     {
 #pragma clang fp contract(off)
         if (r.wk) {
-            const float f = norm_factor(row_sum<D / 8>(squares8(v)), D, r.eps);
+            const float f = norm_factor(row_squares<D>(r, P, squares8(v)), D, r.eps);
             float g[8];
             widen8(norm, g);
             norm8(v, f, g);
@@ -1344,6 +1344,16 @@ __device__ __forceinline__ void code_channels(const AppendRopeParams& p, int b, 
     }
 }
 
+// A wave's share of a call's queries.
+template <int D, int ITER>
+__device__ __forceinline__ void rope_queries(const AppendRopeParams& p, uint32_t token, int part, float2* lds)
+{
+    if (part_in_halves(p.rope, D))
+        rope_rows<D, ITER, false, true>(p.queries, p.rope, token, part, lds);
+    else
+        rope_rows<D, ITER, false, false>(p.queries, p.rope, token, part, lds);
+}
+
 // One token per sequence without a window (a decode step), a wave per (sequence, KV
 // head): lanes 0 .. D / 8 - 1 hold eight channels each of its key, those from lane 32 on
 // of its value, so nothing waits for another wave; further waves rotate queries.  The
@@ -1361,7 +1371,7 @@ __global__ __launch_bounds__(64) void append_token_rope_kernel(AppendRopeParams 
     if (x >= p.code_wgs) {
         const uint32_t item = x - p.code_wgs, parts = (uint32_t)p.queries.parts, token = item / parts;
         if (token < (uint32_t)p.queries.tokens)
-            rope_rows<D, 1, false>(p.queries, p.rope, token, (int)(item - token * parts), angles);
+            rope_queries<D, 1>(p, token, (int)(item - token * parts), angles);
         return;
     }
     const int unit = (int)x, b = unit / p.H, h = unit - b * p.H, lane = threadIdx.x, P = lane & 31;
@@ -1496,7 +1506,7 @@ __global__ __launch_bounds__(kThreads, append_waves(D, PERCH)) void append_rope_
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t item = (x - p.row_wgs) * (kThreads / 64) + wave, token = item / (uint32_t)p.queries.parts;
     if (token < (uint32_t)p.queries.tokens)
-        rope_rows<D, kQueryIter, false>(p.queries, p.rope, token, (int)(item - token * (uint32_t)p.queries.parts), angles[wave]);
+        rope_queries<D, kQueryIter>(p, token, (int)(item - token * (uint32_t)p.queries.parts), angles[wave]);
 }
 
 template <int D>

@@ -14,6 +14,8 @@
 // ones on this chip: about 35 of them per pair.
 #pragma once
 
+#include <type_traits>
+
 #include "kvq_device.h"
 #include "kvq_internal.h"
 
@@ -106,6 +108,79 @@ __device__ __forceinline__ double squares8(const float* v)
     return s;
 }
 
+// The sum of squares of a row from those of its pieces of eight channels: one order, to
+// the bit, for kvq_rope_qk and for appends.  Pairs in halves of a whole head: the two pieces
+// with a pair's members first, then neighbours of these sums.  Else: neighbours first.
+//
+// Whether pairs in halves are of a part of the head.
+__host__ __device__ __forceinline__ bool part_in_halves(const RopeArgs& r, int D)
+{
+    return r.layout == KVQ_ROPE_HALF && r.rot < D && r.rot > 16;
+}
+
+// Lane l of D / 16 holds two pieces' sums, a and b (rope_rows), which come together in
+// that order.  PART (part_in_halves): those of the rotated part are l and hp + l instead, so
+// they are added up side by side up to the hp lanes that hold them, or, where hp is no power of
+// two, exchanged (3 x 999 tokens of 40 normed heads of 128: 13.7 us in a's and b's own order, 14.1
+// and 14.3 so; an instance of its own, so that the others' registers stay).
+template <int D, bool PART>
+__device__ __forceinline__ double row_squares(const RopeArgs& r, int l, double a, double b)
+{
+    constexpr int LPR = D / 16;
+    if constexpr (!PART) {
+        return row_sum<LPR>(a + b);
+    } else {
+        const int hp = r.rot / 16;
+        if ((hp & (hp - 1)) == 0) {
+            double x = l < hp ? a : a + b, y = l < hp ? b : 0.0;
+            const auto step = [&](auto ctrl, int n) {
+                if (n == hp)
+                    x += y;
+                x += dpp_f64<ctrl.value>(x);
+                if (n < hp)
+                    y += dpp_f64<ctrl.value>(y);
+            };
+            step(std::integral_constant<int, 0xB1>{}, 1);
+            step(std::integral_constant<int, 0x4E>{}, 2);
+            if constexpr (LPR >= 8)
+                step(std::integral_constant<int, 0x141>{}, 4);
+            if constexpr (LPR >= 16)
+                step(std::integral_constant<int, 0x140>{}, 8);
+            return x;
+        }
+        const int row = (threadIdx.x & 63) - l;
+        const auto piece = [&](int P) {  // where it is: lane, and which of its two
+            const int lane = P < hp ? P : P < 2 * hp ? P - hp : P >> 1;
+            const double x = __shfl(a, row + lane), y = __shfl(b, row + lane);
+            return P < hp || (P >= 2 * hp && P % 2 == 0) ? x : y;
+        };
+        const double even = piece(2 * l), odd = piece(2 * l + 1);
+        return row_sum<LPR>(even + odd);
+    }
+}
+
+// The same where lane P of D / 8 holds piece P's (appends).
+template <int D>
+__device__ __forceinline__ double row_squares(const RopeArgs& r, int P, double s)
+{
+    if (r.layout != KVQ_ROPE_HALF || r.rot != D)
+        return row_sum<D / 8>(s);
+    const uint64_t u = __builtin_bit_cast(uint64_t, s);
+    const auto other = [&](uint32_t x) -> uint32_t {  // of lane P ^ (D / 16)
+        if constexpr (D == 64) {
+            const uint32_t m = __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true);
+            return __builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true);
+        } else if constexpr (D == 128) {
+            return __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, true);
+        } else {
+            const auto rows = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+            return P & 16 ? rows[0] : rows[1];
+        }
+    };
+    const uint64_t v = ((uint64_t)other((uint32_t)(u >> 32)) << 32) | other((uint32_t)u);
+    return row_sum<D / 16>(s + __builtin_bit_cast(double, v));
+}
+
 // The factor of a row with sum of squares `sum`: 1 / sqrt(v) by the hardware's
 // estimate y (2^-23 or better) and one step of third order, y (1 + e / 2 + 3 e^2 / 8)
 // with e = 1 - v y^2 (binary64: off by 2^-51, so the binary32 result is the nearest
@@ -145,8 +220,8 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s)
 // (two 16-byte loads), so rotating needs no exchange, and lane l's eight cosines
 // and sines are the same for every head of a token: the wave's lanes compute each
 // once, pass them on through LDS and keep their eight in registers.
-// KEYS: there may be keys beside the queries.
-template <int D, int ITER, bool KEYS>
+// KEYS: there may be keys beside the queries.  PART: part_in_halves.
+template <int D, int ITER, bool KEYS, bool PART>
 __device__ __forceinline__ void rope_rows(const RopeQkParams& p, const RopeArgs& r, uint32_t token, int part, float2* lds)
 {
     constexpr int LPR = D / 16, RPI = 64 / LPR;  // lanes of a row, rows of an iteration
@@ -197,7 +272,7 @@ __device__ __forceinline__ void rope_rows(const RopeQkParams& p, const RopeArgs&
             const bool is_q = !KEYS || h < p.H_q;
             const uint16_t* any = KEYS && !r.wq ? r.wk : r.wq;
             const uint16_t* weight = !KEYS || is_q ? r.wq : r.wk;
-            float f = norm_factor(row_sum<LPR>(squares8(v) + squares8(v + 8)), D, r.eps);
+            float f = norm_factor(row_squares<D, PART>(r, l, squares8(v), squares8(v + 8)), D, r.eps);
             float g[16];
             const uint16_t* at = weight ? weight : any;
             widen8(*(const u32x4*)(at + c0), g);

@@ -9,17 +9,17 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-template <int D, int ITER>
+template <int D, int ITER, bool PART>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeQkParams p, RopeArgs r)
 {
     __shared__ __attribute__((aligned(16))) float2 lds[kWaves][D / 2];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const uint32_t item = wg_index() * kWaves + wave, token = item / (uint32_t)p.parts;
     if (token < (uint32_t)p.tokens)  // (waves of a workgroup do not wait for each other)
-        rope_rows<D, ITER, true>(p, r, token, (int)(item - token * (uint32_t)p.parts), lds[wave]);
+        rope_rows<D, ITER, true, PART>(p, r, token, (int)(item - token * (uint32_t)p.parts), lds[wave]);
 }
 
-template <int D>
+template <int D, bool PART>
 hipError_t launch_d(RopeQkParams p, const RopeArgs& rope, hipStream_t stream)
 {
     constexpr int RPI = 1024 / D;
@@ -31,13 +31,13 @@ hipError_t launch_d(RopeQkParams p, const RopeArgs& rope, hipStream_t stream)
     p.parts = (iters + iter - 1) / iter;
     const dim3 g = grid_of((uint32_t)(((long long)p.tokens * p.parts + kWaves - 1) / kWaves)), t(kThreads);
     if (iter == 1)
-        launch_kernel((rope_kernel<D, 1>), g, t, 0, stream, p, rope);
+        launch_kernel((rope_kernel<D, 1, PART>), g, t, 0, stream, p, rope);
     else if (iter == 2)
-        launch_kernel((rope_kernel<D, 2>), g, t, 0, stream, p, rope);
+        launch_kernel((rope_kernel<D, 2, PART>), g, t, 0, stream, p, rope);
     else if (iter == 3)
-        launch_kernel((rope_kernel<D, 3>), g, t, 0, stream, p, rope);
+        launch_kernel((rope_kernel<D, 3, PART>), g, t, 0, stream, p, rope);
     else
-        launch_kernel((rope_kernel<D, 4>), g, t, 0, stream, p, rope);
+        launch_kernel((rope_kernel<D, 4, PART>), g, t, 0, stream, p, rope);
     return hipGetLastError();
 }
 
@@ -47,11 +47,11 @@ hipError_t launch_rope(const RopeQkParams& p, const RopeArgs& rope, int D, hipSt
 {
     switch (D) {
     case 64:
-        return launch_d<64>(p, rope, stream);
+        return part_in_halves(rope, D) ? launch_d<64, true>(p, rope, stream) : launch_d<64, false>(p, rope, stream);
     case 128:
-        return launch_d<128>(p, rope, stream);
+        return part_in_halves(rope, D) ? launch_d<128, true>(p, rope, stream) : launch_d<128, false>(p, rope, stream);
     case 256:
-        return launch_d<256>(p, rope, stream);
+        return part_in_halves(rope, D) ? launch_d<256, true>(p, rope, stream) : launch_d<256, false>(p, rope, stream);
     default:
         return hipErrorInvalidValue;
     }
