@@ -112,10 +112,10 @@ __device__ __forceinline__ double squares8(const float* v)
 // the bit, for kvq_rope_qk and for appends.  Pairs in halves of a whole head: the two pieces
 // with a pair's members first, then neighbours of these sums.  Else: neighbours first.
 //
-// Whether pairs in halves are of a part of the head.
+// Whether pairs in halves are of a part of the head, and rows are normed.
 __host__ __device__ __forceinline__ bool part_in_halves(const RopeArgs& r, int D)
 {
-    return r.layout == KVQ_ROPE_HALF && r.rot < D && r.rot > 16;
+    return r.layout == KVQ_ROPE_HALF && r.rot < D && r.rot > 16 && (r.wq || r.wk);
 }
 
 // Lane l of D / 16 holds two pieces' sums, a and b (rope_rows), which come together in
