@@ -797,6 +797,46 @@ kvq_status kvq_append_rope(kvq_cache* c, const kvq_rope* rope, const void* K, co
 
 namespace {
 
+// Whether numbers i, j, .. of `args` are those of an int.
+template <typename... I>
+bool ints(const int64_t* args, I... i)
+{
+    return (... && (args[i] == (int)args[i]));
+}
+
+template <typename T>
+T* address(int64_t x)
+{
+    return (T*)(uintptr_t)x;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvq_status kvq_internal_rope_qk(const int64_t* a)
+{
+    if (!ints(a, 3, 4, 5, 6, 7, 11))
+        return KVQ_ERR_ARG;
+    return kvq_rope_qk(address<kvq_rope>(a[0]), address<void>(a[1]), address<void>(a[2]), (int)a[3], (int)a[4], (int)a[5],
+                       (int)a[6], (int)a[7], address<void>(a[8]), address<void>(a[9]), address<int32_t>(a[10]), (int)a[11],
+                       address<void>(a[12]), address<void>(a[13]), address<void>(a[14]));
+}
+
+kvq_status kvq_internal_append_rope(const int64_t* a)
+{
+    if (!ints(a, 4, 6, 8, 12))
+        return KVQ_ERR_ARG;
+    return kvq_append_rope(address<kvq_cache>(a[0]), address<kvq_rope>(a[1]), address<void>(a[2]), address<void>(a[3]),
+                           (int)a[4], address<int32_t>(a[5]), (int)a[6], address<void>(a[7]), (int)a[8], address<void>(a[9]),
+                           address<void>(a[10]), address<int32_t>(a[11]), (int)a[12], address<void>(a[13]),
+                           address<kvq_format>(a[14]), address<void>(a[15]));
+}
+
+}  // extern "C"
+
+namespace {
+
 // The operations of kvq_cache_gather, in batches of kGatherBatch (`ops`, up to
 // `cap` entries, gaps with dst = -1).  In place, an operation comes after all
 // that read what it overwrites, or in the same batch: first the sequences that

@@ -330,6 +330,10 @@ extern "C" kvq_status kvq_internal_shared_attn(const kvq_cache* prefix, const kv
 extern "C" kvq_status kvq_internal_tree_attn(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first,
                                              const void* Q, int C, int H_q, float sm_scale, const uint32_t* tree, void* O,
                                              void* workspace, size_t ws_bytes, void* stream, int kernels);
+// kvq_rope_qk and kvq_append_rope with their arguments as 64-bit numbers, in their
+// order (the Python binding's calls).
+extern "C" kvq_status kvq_internal_rope_qk(const int64_t* args);
+extern "C" kvq_status kvq_internal_append_rope(const int64_t* args);
 // The partials that such a call writes (of arguments that it would not refuse).
 extern "C" size_t kvq_internal_shared_partials(const kvq_cache* prefix, const kvq_cache* suffix, const int32_t* first, int C,
                                                int H_q, int kernels);

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from array import array
 
 import numpy as np
@@ -105,7 +106,12 @@ EXPORTED = ("kvq_strerror", "kvq_cache_bytes", "kvq_cache_init", "kvq_cache_sect
             "kvq_prefill_attn_shared", "kvq_tree_attn_shared", "kvq_time_launches")
 
 
-_rope_qk, _append_rope = _lib.kvq_rope_qk, _lib.kvq_append_rope
+# Calls whose arguments come as 64-bit numbers, in their order: packing them takes a third of ctypes' conversions (1.0 of
+# 1.4 us of 16), which is what checking the tensors costs.
+_rope_qk, _append_rope = _lib.kvq_internal_rope_qk, _lib.kvq_internal_append_rope
+for _f in (_rope_qk, _append_rope):
+    _f.argtypes, _f.restype = [C.c_char_p], C.c_int
+_pack_qk, _pack_append = struct.Struct("15q").pack, struct.Struct("16q").pack
 
 
 def lib() -> C.CDLL:
@@ -125,8 +131,8 @@ def _ptr(t):
     return t.data_ptr()
 
 
-try:  # raw handle of torch's current stream without building a Stream object
-    _raw_stream = torch._C._cuda_getCurrentRawStream
+try:  # raw handle of torch's current stream without building a Stream object, of the current device
+    _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 except AttributeError:  # pragma: no cover - older torch
     _raw_stream = None
 
@@ -134,7 +140,7 @@ except AttributeError:  # pragma: no cover - older torch
 def _stream(stream) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -173,6 +179,30 @@ def _positions(t, count: int, what: str, beside) -> None:
         raise ValueError(f"{what}: on another device than the tensors beside it")
 
 
+_bf16, _Tensor = torch.bfloat16, torch.Tensor
+
+
+def _rows(x, y, count: int, what: str, device: int) -> None:
+    """Refuses tensors that are not `count` bf16 numbers in one piece each (x by its shape) on that device: the library
+    sees addresses alone.  (What is no tensor is taken at its word.)"""
+    if isinstance(x, _Tensor):
+        if x.dtype is not _bf16 or not x.is_contiguous() or (
+                y is not x and (y.dtype is not _bf16 or y.numel() != count or not y.is_contiguous())):
+            raise ValueError(f"{what}: {count} contiguous bf16 numbers each expected")
+        if x.get_device() != device or y is not x and y.get_device() != device:
+            raise ValueError(f"{what}: on another device than the tensors beside it")
+
+
+def _weights(w, D: int, what: str, device: int) -> int:
+    """The address of a norm's weights."""
+    if isinstance(w, _Tensor):
+        if w.dtype is not _bf16 or w.numel() != D or not w.is_contiguous():
+            raise ValueError(f"{what}: {D} contiguous bf16 numbers expected")
+        if w.get_device() != device:
+            raise ValueError(f"{what}: on another device than the tensors beside it")
+    return w.data_ptr()
+
+
 class Rope:
     """Rotary positions of `rot` channels of a head (kvq_rope): frequencies base^(-2 i / rot), scaled for contexts
     `factor` times `original`, or `turns`, turns per position of each of the rot / 2 pairs; and the norms' eps."""
@@ -181,7 +211,7 @@ class Rope:
                  factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0, scale=None,
                  eps: float = 1e-6, turns=None):
         self.c = _Rope()
-        self._ref = C.byref(self.c)
+        self._ref, self._at = C.byref(self.c), C.addressof(self.c)
         if scaling not in ROPE_SCALINGS:
             raise ValueError(f"scaling: one of {', '.join(ROPE_SCALINGS)} expected")
         _check(_lib.kvq_rope_init(self._ref, rot, int(bool(interleaved)), base, ROPE_SCALINGS.index(scaling),
@@ -198,26 +228,32 @@ class Rope:
         """Qo, Ko (Q and K themselves where not given) <- bf16 Q [B, n, H_q, D] and K [B, n, H_kv, D] (either may be
         None), normed by bf16 weights [D] where given and rotated to positions pos (device int32 [B, n], or None for
         pos0, pos0 + 1, ..)."""
-        q = k = qo = ko = None
-        H_q = H = 0
+        q = k = qo = ko = H_q = H = 0
         if Q is not None:
             B, n, H_q, D = Q.shape
-            q = Q.data_ptr()
-            qo = q if Qo is None else Qo.data_ptr()
+            device = Q.get_device()
+            if Qo is None:
+                Qo = Q
+            _rows(Q, Qo, B * n * H_q * D, "Q, Qo", device)
+            q, qo = Q.data_ptr(), Qo.data_ptr()
         if K is not None:
             b, m, H, d = K.shape
-            if Q is not None and (b != B or m != n or d != D):
+            if Q is None:
+                B, n, D, device = b, m, d, K.get_device()
+            elif b != B or m != n or d != D:
                 raise ValueError("Q and K are of different tokens or head sizes")
-            B, n, D = b, m, d
-            k = K.data_ptr()
-            ko = k if Ko is None else Ko.data_ptr()
+            if Ko is None:
+                Ko = K
+            _rows(K, Ko, B * n * H * D, "K, Ko", device)
+            k, ko = K.data_ptr(), Ko.data_ptr()
         elif Q is None:
             raise ValueError("neither Q nor K")
+        q_norm = 0 if q_norm is None else _weights(q_norm, D, "q_norm", device)
+        k_norm = 0 if k_norm is None else _weights(k_norm, D, "k_norm", device)
         if pos is not None:
             _positions(pos, B * n, "pos", K if Q is None else Q)
-            pos = pos.data_ptr()
-        st = _rope_qk(self._ref, q, k, B, n, H_q, H, D, q_norm if q_norm is None else q_norm.data_ptr(),
-                      k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0, qo, ko, _stream(stream))
+        st = _rope_qk(_pack_qk(self._at, q, k, B, n, H_q, H, D, q_norm, k_norm, 0 if pos is None else pos.data_ptr(), pos0,
+                               qo, ko, _stream(stream)))
         if st:
             _check(st, "rope_qk")
 
@@ -244,8 +280,8 @@ class Cache:
         h = C.c_void_p()
         _check(_lib.kvq_cache_init(C.byref(self.fmt), B, H_kv, D, T_max, C.c_void_p(_ptr(storage)),
                                    storage.numel() * storage.element_size(), C.byref(h)), "cache_init")
-        self.handle = h
-        self._fmt_ref = C.byref(self.fmt)
+        self.handle, self._at = h, h.value
+        self._fmt_ref, self._fmt_at = C.byref(self.fmt), C.addressof(self.fmt)
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -290,29 +326,44 @@ class Cache:
                     k_norm=None, pos=None, pos0: int = 0, fmt=None, stream=None) -> None:
         """append of keys that `rope` norms and rotates on the way.  bf16 K, V [B, n_in, H_kv, D]; with rows (device
         int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]:
-        one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows).  pos: device int32
-        [B, n_new], or None for pos0, pos0 + 1, .."""
+        one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows; Qo may be Q and has to
+        be given).  pos: device int32 [B, n_new], or None for pos0, pos0 + 1, .. (pos0 = self.n where the cache holds
+        all tokens before these)."""
         shape = K.shape
-        n_in = shape[1] if len(shape) == 4 else 1
+        if len(shape) == 4:
+            B, n_in, H, D = shape
+        else:
+            (B, H, D), n_in = shape, 1
+        if B != self.B or H != self.H or D != self.D:
+            raise ValueError(f"K: rows of {self.B} sequences, {self.H} heads of {self.D} expected")
+        device = K.get_device()
+        _rows(K, V, B * n_in * H * D, "K, V", device)
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
         if rows is not None:
-            _positions(rows, self.B * n_new, "rows", K)
-            rows = rows.data_ptr()
+            _positions(rows, B * n_new, "rows", K)
         if pos is not None:
-            _positions(pos, self.B * n_new, "pos", K)
-            pos = pos.data_ptr()
-        f = self._fmt_ref if fmt is None else C.byref(Format.of(fmt))
-        q, H_q = None, 0
+            _positions(pos, B * n_new, "pos", K)
+        q = H_q = 0
         if Q is not None:
             shape = Q.shape
-            if (shape[1] if len(shape) == 4 else 1) != n_new:
+            if len(shape) == 4:
+                b, m, H_q, d = shape
+            else:
+                (b, H_q, d), m = shape, 1
+            if m != n_new:
                 raise ValueError(f"Q: rows of {n_new} tokens expected")
-            q, H_q = Q.data_ptr(), shape[-2]
-        st = _append_rope(self.handle, rope._ref, K.data_ptr(), V.data_ptr(), n_in, rows, n_new, q, H_q,
-                          q_norm if q_norm is None else q_norm.data_ptr(),
-                          k_norm if k_norm is None else k_norm.data_ptr(), pos, pos0,
-                          Qo if Qo is None else Qo.data_ptr(), f, _stream(stream))
+            if b != B or d != D:
+                raise ValueError(f"Q: rows of {B} sequences, heads of {D} expected")
+            _rows(Q, Q if Qo is None else Qo, B * m * H_q * D, "Q, Qo", device)
+            q = Q.data_ptr()
+        if fmt is not None:
+            fmt = Format.of(fmt)
+        st = _append_rope(_pack_append(
+            self._at, rope._at, K.data_ptr(), V.data_ptr(), n_in, 0 if rows is None else rows.data_ptr(), n_new, q, H_q,
+            0 if q_norm is None else _weights(q_norm, D, "q_norm", device), 0 if k_norm is None else _weights(k_norm, D, "k_norm", device),
+            0 if pos is None else pos.data_ptr(), pos0, 0 if Qo is None else Qo.data_ptr(),
+            self._fmt_at if fmt is None else C.addressof(fmt), _stream(stream)))
         if st:
             _check(st, "append_rope")
 
