@@ -437,7 +437,9 @@ kvq_status kvq_prefill_workspace_bytes(const kvq_cache* cache, size_t* bytes);
 
 /* Workspace bytes for calls of up to C queries per sequence at any lengths and
  * groups of these caches (contents need no initialization; calls that share a
- * workspace must not overlap). */
+ * workspace must not overlap).  Decode and chunk attention also take one without
+ * what kvq_tree_attn_shared needs beyond them, 4 (D + 2) bytes less for each of the
+ * B C H_q rows where a row has fewer than 64 partial outputs. */
 kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* suffix, int C, int H_q, size_t* bytes);
 
 /* Decode attention for one new query per sequence over its prefix and suffix.

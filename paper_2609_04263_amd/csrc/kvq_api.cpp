@@ -1218,9 +1218,9 @@ static kvq_status shared_caches(const kvq_cache* prefix, const kvq_cache* suffix
     return same_format(prefix->fmt, suffix->fmt) ? KVQ_OK : KVQ_ERR_FORMAT;
 }
 
-static size_t shared_workspace_layout(const kvq_cache* suffix, int C, int H_q, size_t* off_ml)
+static size_t shared_workspace_layout(const kvq_cache* suffix, int C, int H_q, bool tree, size_t* off_ml)
 {
-    const size_t partials = kvq::shared_partials_bound(suffix->B, suffix->H, suffix->D, C, H_q / suffix->H);
+    const size_t partials = kvq::shared_partials_bound(suffix->B, suffix->H, suffix->D, C, H_q / suffix->H, tree);
     const size_t o_ml = round_up(partials * suffix->D * sizeof(float), 256);
     if (off_ml)
         *off_ml = o_ml;
@@ -1234,7 +1234,7 @@ kvq_status kvq_shared_workspace_bytes(const kvq_cache* prefix, const kvq_cache* 
         return st;
     if (!bytes)
         return KVQ_ERR_ARG;
-    *bytes = shared_workspace_layout(suffix, C, H_q, nullptr);
+    *bytes = shared_workspace_layout(suffix, C, H_q, true, nullptr);
     return KVQ_OK;
 }
 
@@ -1279,7 +1279,7 @@ static kvq_status shared_attn(const kvq_cache* prefix, const kvq_cache* suffix, 
         if (first[g] > first[g + 1])
             return KVQ_ERR_ARG;
     size_t off_ml;
-    if (ws_bytes < shared_workspace_layout(suffix, C, H_q, &off_ml))
+    if (ws_bytes < shared_workspace_layout(suffix, C, H_q, tree != nullptr, &off_ml))
         return KVQ_ERR_WORKSPACE;
     kvq::SharedParams p = shared_params(prefix, suffix, first, C, H_q, sm_scale, kernels, tree);
     p.q = (const uint16_t*)Q;

@@ -308,8 +308,9 @@ struct SharedParams {
 };
 // Fills S, bps, parts, limits, tiles0, tile0 and the items from the rest.
 void shared_plan(SharedParams* p, int D, int B, int kernels);
-// Upper bound of parts times rows for any lengths and groups and up to C queries.
-size_t shared_partials_bound(int B, int H, int D, int C, int G);
+// Upper bound of parts times rows for any lengths and groups and up to C queries,
+// of calls with a tree or of those without.
+size_t shared_partials_bound(int B, int H, int D, int C, int G, bool tree);
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream);
 
 }  // namespace kvq

@@ -79,6 +79,9 @@ bool all_direct(int rows, long long work, const Kind& k)
     return rows <= 2 * kTile || work <= k.most * 1024;
 }
 
+// Partials of a row that are enough for those of a tree's drafts to be one of them.
+constexpr size_t kManyParts = 64;
+
 // Ranges that a segment of `tiles` tiles is cut into, at most.
 int shared_splits(long long tiles, int round)
 {
@@ -229,6 +232,20 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
         p->bps[k] = nb[k] > 0 ? ceil_div(ceil_div(nb[k], want), step) * step : step;
         p->S[k] = ceil_div(nb[k], p->bps[k]);
     }
+    if (tree) {
+        // The drafts' partial, where both segments are cut into all that the workspace holds
+        // (kManyParts): from the one whose ranges grow by less.
+        const size_t most = shared_partials_bound(B, a.H, D, p->C, a.G, true) / p->rows;
+        const auto fewer = [&](int k) {  // blocks per range if there is one range less
+            return p->S[k] < 2 ? INT32_MAX : ceil_div(ceil_div(nb[k], p->S[k] - 1), kind[k].step) * kind[k].step;
+        };
+        while ((size_t)(p->S[0] + p->S[1] + 1) > most) {
+            const int bps[2] = {fewer(0), fewer(1)};
+            const int k = (long long)bps[0] * p->bps[1] <= (long long)bps[1] * p->bps[0] ? 0 : 1;
+            p->bps[k] = bps[k];
+            p->S[k] = ceil_div(nb[k], bps[k]);
+        }
+    }
     p->items0 = tiles[0] * p->S[0];
     p->items1 = tiles[1] * p->S[1];
     p->image_items = (kind[0].direct ? 0 : p->items0) + (kind[1].direct ? 0 : p->items1);
@@ -238,7 +255,7 @@ void shared_plan(SharedParams* p, int D, int B, int kernels)
     p->parts = p->S[0] + p->S[1] + tree;
 }
 
-size_t shared_partials_bound(int B, int H, int D, int C, int G)
+size_t shared_partials_bound(int B, int H, int D, int C, int G, bool tree)
 {
     // A segment of `units` units of u rows is cut into S <= max(1, round / tiles)
     // ranges, its tiles never fewer than units ceil(u / per) (the groups' not fewer
@@ -252,8 +269,12 @@ size_t shared_partials_bound(int B, int H, int D, int C, int G)
         }
         return most;
     };
-    // (and one of a tree's drafts)
-    return segment(H, B * C * G) + segment((size_t)B * H, C * G) + (size_t)B * H * C * G;
+    // A tree's drafts have a partial of their own.  Where a row has many its plan takes
+    // ranges from the others instead (two caches of 8192 tokens: 129 partials 23.1 us, 97
+    // 21.3; but 8 to 7 ranges of 16000 tokens 221 to 241).  (A row's do not become more as C
+    // grows.)
+    const size_t rows = (size_t)B * H * C * G, both = segment(H, B * C * G) + segment((size_t)B * H, C * G);
+    return both + (tree && both < kManyParts * rows ? rows : 0);
 }
 
 hipError_t launch_shared(const SharedParams& p, int D, hipStream_t stream)
