@@ -227,17 +227,10 @@ struct RowStage {
     __device__ static int row(int k) { return ((int)threadIdx.x + kThreads * k) / (D / 8); }
     __device__ static int chan(int k) { return 8 * (((int)threadIdx.x + kThreads * k) % (D / 8)); }
 
-    // The angles of step k's row.
-    template <typename P>
-    __device__ static __forceinline__ auto angles(const P& p, int b, int tb, int k)
+    // The angles of step k's row, a token of this call.
+    __device__ static __forceinline__ Angles angles(const AppendRopeParams& p, int b, int tb, int k)
     {
-        if constexpr (kRope<P>) {
-            const int t = tb + row(k);
-            const bool input = t >= p.q0 && t < p.q1 && t >= p.n0;  // (all lanes of a row or none)
-            return input ? Angles(p.rope, input_position(p, b, t - p.n0), chan(k) >> 3) : Angles();
-        } else {
-            return NoAngles();
-        }
+        return Angles(p.rope, input_position(p, b, tb + row(k) - p.n0), chan(k) >> 3);
     }
 
     // Issue the loads (bf16 input for tokens of this call, fp16 window slots
@@ -313,8 +306,8 @@ __device__ __forceinline__ void copy_out(const uint8_t* src, uint8_t* dst, int b
 // per-channel keys is one whole group), written piece by piece: value pieces
 // keep the bits of tokens appended earlier.  vcode: 32 D bytes of LDS for the
 // value codes [token][D].
-template <int D, typename Params>
-__device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, uint8_t* vcode)
+template <int D>
+__device__ __forceinline__ void edge_block(const AppendParams& p, int unit, int tb, uint8_t* vcode)
 {
     const int b = unit / p.H, h = unit % p.H;
     const int lo = max(p.q0, tb), hi = min(p.q1, tb + kBlockTok);
@@ -332,7 +325,7 @@ __device__ __forceinline__ void edge_block(const Params& p, int unit, int tb, ui
         for (int k = 0; k < RowStage<D>::kSteps; ++k) {
             const int i = RowStage<D>::row(k), P = RowStage<D>::chan(k) / 8, t = tb + i;
             float x[8];
-            kst.widen(p, tb, k, x, RowStage<D>::angles(p, b, tb, k));
+            kst.widen(p, tb, k, x, NoAngles());
             float s, z;
             piece_group_stats(x, lanes, p.k_mode, kb, &s, &z);
             round_meta(p.meta16, &s, &z);
@@ -1100,8 +1093,8 @@ __device__ __forceinline__ void code_heads(const AppendRopeParams& p, int b, int
 // bits of tokens appended earlier and clear later ones; those of the first octet are
 // loaded first, with the rows.  Bound by latency: five tokens of 16 x 8 heads of 128 take
 // 5.2 us; 7.0 where a thread codes a key and then a value, which more tokens than T / 2
-// do (31 of 8 x 8 heads of 256: 10.4, 12.7 with keys and values apart); 11.0 as edge_block,
-// which takes all 32 rows and loads old pieces when it needs them.
+// do (31 of 8 x 8 heads of 256: 10.4, 12.7 with keys and values apart); 11.0 where all 32
+// rows are taken and old pieces are loaded when they are needed.
 template <int D, int KB, int VB, bool PLAIN>
 __device__ __forceinline__ void code_edge(const AppendRopeParams& p, int unit, int tb)
 {

@@ -1,7 +1,7 @@
 // Rotary positions of queries and keys with the RMS norm of each head in the
 // same pass (kvq_rope_qk): rope_rows in rope.h, a wave per token and some of its
 // heads.  Bound by HBM: 16384 tokens of 24 normed heads of 256 (402 MB) take 80 us,
-// 5.0 TB/s, as a copy of 1 GiB does; small calls by the launch (one token 2.6 us).
+// 5.0 TB/s, as a copy of 1 GiB does; small calls by the launch (one token 2.3 us).
 #include "rope.h"
 
 namespace kvq {
