@@ -205,7 +205,8 @@ def _weights(w, D: int, what: str, device: int) -> int:
 
 class Rope:
     """Rotary positions of `rot` channels of a head (kvq_rope): frequencies base^(-2 i / rot), scaled for contexts
-    `factor` times `original`, or `turns`, turns per position of each of the rot / 2 pairs; and the norms' eps."""
+    `factor` times `original` (low, high: the waves in it between which "bands" and "yarn" go over; 32 is yarn's usual
+    high, bands' is 4), or `turns`, turns per position of each of the rot / 2 pairs; and the norms' eps."""
 
     def __init__(self, rot: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "plain",
                  factor: float = 1.0, original: float = 0.0, low: float = 1.0, high: float = 32.0, scale=None,
