@@ -289,7 +289,7 @@ kvq_status kvq_rope_init(kvq_rope* rope, int rot, int layout, double base, int s
  *                   aligned to 4 bytes; NULL: token i of every sequence is at
  *                   pos0 + i
  * D 64, 128 or 256; rope->rot <= D; B n (H_q + H_kv) below 2^31.  n == 0 is a
- * no-op. */
+ * no-op, whose tensors may be NULL. */
 kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B, int n, int H_q, int H_kv, int D,
                        const void* q_norm, const void* k_norm, const int32_t* pos, int pos0, void* Qo, void* Ko,
                        void* stream);

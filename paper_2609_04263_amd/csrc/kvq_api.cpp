@@ -728,10 +728,13 @@ kvq_status rope_args(const kvq_rope* rope, int D, const void* q_norm, const void
     return KVQ_OK;
 }
 
-// Whether the B n rows of H heads can be rotated from x to y.
-bool rope_rows_ok(const void* x, const void* y, int H)
+// Whether the rows of H heads of so many tokens can be rotated from x to y (of no
+// tokens there is no address).
+bool rope_rows_ok(const void* x, const void* y, int H, long long tokens)
 {
-    return H == 0 ? !x && !y : H > 0 && x && y && aligned16(x) && aligned16(y);
+    if (H == 0)
+        return !x && !y;
+    return H > 0 && (tokens == 0 || (x && y)) && aligned16(x) && aligned16(y);
 }
 
 }  // namespace
@@ -744,9 +747,9 @@ kvq_status kvq_rope_qk(const kvq_rope* rope, const void* Q, const void* K, int B
 {
     if (B < 1 || n < 0 || (D != 64 && D != 128 && D != 256))
         return KVQ_ERR_ARG;
-    if (!rope_rows_ok(Q, Qo, H_q) || !rope_rows_ok(K, Ko, H_kv) || (!Q && !K))
-        return KVQ_ERR_ARG;
     const long long tokens = (long long)B * n, heads = (long long)H_q + H_kv;
+    if (!rope_rows_ok(Q, Qo, H_q, tokens) || !rope_rows_ok(K, Ko, H_kv, tokens) || heads == 0)
+        return KVQ_ERR_ARG;
     if (tokens > INT32_MAX || heads > INT32_MAX || tokens * heads >= kvq::kRopeRows)
         return KVQ_ERR_ARG;
     kvq::RopeQkParams p = {};
@@ -774,9 +777,9 @@ kvq_status kvq_append_rope(kvq_cache* c, const kvq_rope* rope, const void* K, co
     if (st != KVQ_OK)
         return st;
     // (checked for no tokens too: a wrong call is refused at any size)
-    if ((uintptr_t)rows % 4 || (rows ? n_in < 1 || Q : n_in < n_new) || !rope_rows_ok(Q, Qo, H_q))
-        return KVQ_ERR_ARG;
     const long long tokens = (long long)c->B * n_new;
+    if ((uintptr_t)rows % 4 || (rows ? n_in < 1 || H_q != 0 : n_in < n_new) || !rope_rows_ok(Q, Qo, H_q, tokens))
+        return KVQ_ERR_ARG;
     if (tokens * ((long long)H_q + c->H) >= kvq::kRopeRows || (long long)c->B * n_in > INT32_MAX)
         return KVQ_ERR_ARG;
     kvq::AppendRopeParams p = {};

@@ -116,6 +116,25 @@ def test_positions_beyond_32_bits(kvq):
     assert c.n == 4
 
 
+def test_no_tokens(kvq):
+    # (torch has no address for a tensor without elements)
+    rope, none = kvq.Rope(D), bf16(B, 0, H_Q, D)
+    assert none.data_ptr() == 0
+    rope.qk(none, bf16(B, 0, H, D), stream=0)
+    rope.qk(none, None, Qo=bf16(B, 0, H_Q, D), q_norm=bf16(D), stream=0)
+    rope.qk(None, bf16(B, 0, H, D), pos=torch.zeros((B, 0), dtype=torch.int32), stream=0)
+    c = cache(kvq, configs.make_format(), B, H, D, 100, n=4)
+    k = bf16(B, 0, H, D)
+    c.append_rope(rope, k, k, stream=0)
+    c.append_rope(rope, k, k, Q=none, Qo=none, q_norm=bf16(D), k_norm=bf16(D), stream=0)
+    some = bf16(B, N, H, D)
+    c.append_rope(rope, some, some, rows=torch.zeros((B, 0), dtype=torch.int32), stream=0)
+    assert c.n == 4
+    f = kvq.lib().kvq_rope_qk
+    for heads in ((0, 0), (-1, 1), (1, -1)):
+        assert f(rope._ref, None, None, B, 0, *heads, D, None, None, None, 0, None, None, 0) == kvq.ERR_ARG
+
+
 @pytest.mark.gpu
 def test_on_the_device():
     from paper_2609_04263_amd import kvq
