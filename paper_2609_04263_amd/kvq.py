@@ -182,15 +182,17 @@ def _positions(t, count: int, what: str, beside) -> None:
 _bf16, _Tensor = torch.bfloat16, torch.Tensor
 
 
-def _rows(x, y, count: int, what: str, device: int) -> None:
-    """Refuses tensors that are not `count` bf16 numbers in one piece each (x by its shape) on that device: the library
-    sees addresses alone.  (What is no tensor is taken at its word.)"""
+def _rows(x, y, count: int, what: str, device: int | None = None) -> int:
+    """The device of x and y, refused if they are not `count` bf16 numbers in one piece each (x by its shape) on one
+    device, or not on that given: the library sees addresses alone.  (What is no tensor is taken at its word.)"""
+    at = x.get_device()
     if isinstance(x, _Tensor):
         if x.dtype is not _bf16 or not x.is_contiguous() or (
                 y is not x and (y.dtype is not _bf16 or y.numel() != count or not y.is_contiguous())):
             raise ValueError(f"{what}: {count} contiguous bf16 numbers each expected")
-        if x.get_device() != device or y is not x and y.get_device() != device:
+        if y is not x and y.get_device() != at or device is not None and device != at:
             raise ValueError(f"{what}: on another device than the tensors beside it")
+    return at
 
 
 def _weights(w, D: int, what: str, device: int) -> int:
@@ -232,20 +234,19 @@ class Rope:
         q = k = qo = ko = H_q = H = 0
         if Q is not None:
             B, n, H_q, D = Q.shape
-            device = Q.get_device()
             if Qo is None:
                 Qo = Q
-            _rows(Q, Qo, B * n * H_q * D, "Q, Qo", device)
+            device = _rows(Q, Qo, B * n * H_q * D, "Q, Qo")
             q, qo = Q.data_ptr(), Qo.data_ptr()
         if K is not None:
             b, m, H, d = K.shape
             if Q is None:
-                B, n, D, device = b, m, d, K.get_device()
+                B, n, D, device = b, m, d, None
             elif b != B or m != n or d != D:
                 raise ValueError("Q and K are of different tokens or head sizes")
             if Ko is None:
                 Ko = K
-            _rows(K, Ko, B * n * H * D, "K, Ko", device)
+            device = _rows(K, Ko, B * n * H * D, "K, Ko", device)
             k, ko = K.data_ptr(), Ko.data_ptr()
         elif Q is None:
             raise ValueError("neither Q nor K")
@@ -326,19 +327,20 @@ class Cache:
     def append_rope(self, rope: "Rope", K, V, n_new: int | None = None, rows=None, Q=None, Qo=None, q_norm=None,
                     k_norm=None, pos=None, pos0: int = 0, fmt=None, stream=None) -> None:
         """append of keys that `rope` norms and rotates on the way.  bf16 K, V [B, n_in, H_kv, D]; with rows (device
-        int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]:
-        one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows; Qo may be Q and has to
+        int32 [B, n_new]) the tokens appended are those rows, else the first n_new (all by default; K, V [B, H_kv, D]
+        or [B, H_kv D]: one token).  Q, Qo [B, n_new, H_q, D]: these tokens' queries, rotated too (not with rows; Qo may be Q and has to
         be given).  pos: device int32 [B, n_new], or None for pos0, pos0 + 1, .. (pos0 = self.n where the cache holds
         all tokens before these)."""
         shape = K.shape
         if len(shape) == 4:
             B, n_in, H, D = shape
+            fits = B == self.B and H == self.H and D == self.D
         else:
-            (B, H, D), n_in = shape, 1
-        if B != self.B or H != self.H or D != self.D:
+            B, n_in, H, D = self.B, 1, self.H, self.D
+            fits = not isinstance(K, _Tensor) or K.numel() == B * H * D
+        if not fits:
             raise ValueError(f"K: rows of {self.B} sequences, {self.H} heads of {self.D} expected")
-        device = K.get_device()
-        _rows(K, V, B * n_in * H * D, "K, V", device)
+        device = _rows(K, V, B * n_in * H * D, "K, V")
         if n_new is None:
             n_new = n_in if rows is None else rows.shape[1]
         if rows is not None:

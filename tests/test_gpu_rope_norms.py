@@ -90,7 +90,8 @@ def rows(D, rot, k=3):
 
 
 # (rotated channels: all, a power of two of them and not)
-CASES = [(64, 64), (64, 48), (128, 128), (128, 64), (128, 96), (256, 256), (256, 208)]
+CASES = [(64, 64), (64, 32), (64, 48), (128, 128), (128, 32), (128, 64), (128, 96), (256, 256), (256, 32), (256, 64), (256, 128),
+         (256, 208)]
 
 
 @pytest.mark.parametrize("D,rot", CASES)

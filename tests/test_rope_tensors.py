@@ -63,7 +63,8 @@ def check_append(kvq, c, device):
 
     def append(K=K, V=V, **kw):
         c.append_rope(rope, K, V, stream=0, **kw)
-    for s in ((B + 1, N, H, D), (B, N, H + 1, D), (B, N, H, 2 * D), (B, H + 1, D), (B, H, 2 * D), (2 * B, H, D)):
+    for s in ((B + 1, N, H, D), (B, N, H + 1, D), (B, N, H, 2 * D), (B, H + 1, D), (B, H, 2 * D), (2 * B, H, D),
+              (B, H * D + 8), (B + 1, H * D)):
         t = bf16(*s, device=device)
         refused(lambda: append(K=t, V=t))
     for t in wrong(*k, device=device):
@@ -156,4 +157,6 @@ def test_on_the_device():
     parts = qkv.split((H_Q, H, H), 2)
     refused(lambda: c.append_rope(kvq.Rope(D), parts[1], parts[2]))
     c.append_rope(kvq.Rope(D), parts[1].contiguous(), parts[2].contiguous())
-    assert c.n == 2 * N
+    # one token in the projection's own shape
+    c.append_rope(kvq.Rope(D), bf16(B, H * D, device="cuda"), bf16(B, H * D, device="cuda"))
+    assert c.n == 2 * N + 1
